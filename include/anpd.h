@@ -351,6 +351,88 @@ int32_t anpd_linear(const float *X, const void *W, float *Y, int32_t M, int32_t 
 int32_t anpd_linear_static(const float *X, const void *W, float *Y, int32_t M, int32_t N, int32_t K,
                            void *stream);
 
+/* ------------------------------------------------------------------------
+ * Operators on caches, one layer at a time: attention of new rows over the cached keys and values, the weight that
+ * every cached key receives, and the eviction of the keys that receive little.  For programs whose layers are their
+ * own (other projections, capped or biased scores, sliding windows, packed documents), beside anpd_linear, and to
+ * shorten the cache that anpd_prefill has filled before the steps that follow.
+ * Head dims 64 and 128.  Sums, maxima and outputs are formed in 32 bits; results do not depend on timing (no
+ * floating-point atomics), but on how the keys are divided among blocks, which depends on the sizes of a call.
+ * ---------------------------------------------------------------------- */
+
+/* A cache without a model.  All anpd_kv_* functions take it; steps and prompts do not. */
+typedef struct {
+    int32_t n_layers, n_heads, head_dim;
+    int32_t n_kv_heads;     /* 0 = n_heads; must divide n_heads */
+    int32_t dtype;          /* ANPD_F32 | ANPD_BF16 */
+    int32_t page_tokens;    /* power of two in 8..256; bf16 pages of 16 are kept in matrix-core order, which is the faster form */
+} anpd_cache_cfg;
+/* As anpd_kv_pool_bytes / anpd_kv_create; max_tokens in 1..2^20.  Destroy with anpd_kv_destroy. */
+size_t anpd_cache_pool_bytes(const anpd_cache_cfg *cfg, int32_t max_tokens);
+int32_t anpd_cache_create(const anpd_cache_cfg *cfg, void *pool, size_t pool_bytes, int32_t max_tokens, anpd_kv_t **out);
+
+#define ANPD_ATTN_MAX_SEQS 64
+
+/* Rules of the scores; all zero (or a NULL pointer in place of the struct): causal attention scaled by 1 / sqrt(head_dim).
+ *   t = scale * q.k;  cap > 0: t = cap * tanh(t / cap);  t -= slopes[head] * |p - j|
+ * A row at position p sees key j if j >= first_key[row] and (j < prefix or (j <= p and (window == 0 or j > p - window))). */
+typedef struct {
+    float scale;                /* 0 = 1 / sqrt(head_dim) */
+    float cap;                  /* 0 = none */
+    int32_t window;             /* 0 = none */
+    int32_t prefix;             /* keys below it are seen from every position */
+    const float *slopes;        /* DEVICE, n_heads floats, or NULL */
+    const int32_t *first_key;   /* DEVICE, one per row of the call, or NULL.  Documents packed one after the other: where the
+                                   row's own begins.  A value above the row's position (and the prefix) leaves the row
+                                   without a key, as for the padding of a batch. */
+} anpd_attn_rules;
+
+/* Attention of a chunk of new rows of one or several sequences.
+ *   kvs (host, n_seq handles of caches of the same shape; one cache may occur twice), n_seq 1..ANPD_ATTN_MAX_SEQS.
+ *   n_rows (host, n_seq ints): new rows of each, >= 0.  They stand at positions pos0[s] .. pos0[s] + n_rows[s] - 1 (pos0:
+ *     host, nullable: the committed length), and their keys and values lie in the cache already (anpd_kv_write).
+ *   q, out: DEVICE, the rows of all sequences one after the other, n_heads * head_dim elements of dtype (ANPD_F32 |
+ *     ANPD_BF16, whatever the cache's) each, ldq / ldo elements apart; out may be q itself.  No alignment is needed beyond
+ *     the type's; rows that begin on 16 bytes are moved faster.
+ *   lse (nullable, DEVICE): [rows][n_heads] logarithms of the sums of exp(t).
+ *   A row that sees no key gets 0 and an lse of -infinity.  Keys that a row does not see take no part, whatever their
+ *   contents (infinities and NaN included).
+ *   workspace: DEVICE, 256-byte aligned, >= anpd_attention_workspace_bytes() for the same arguments (often 0, then it may be
+ *   NULL), used during the call only: calls that may overlap need one each, replays of captured calls included.
+ * Rows of bf16 have their weights rounded to bf16 for the second product; rows of fp32 are as exact as sums in fp32.
+ * Asynchronous on stream; may be captured into a graph (which then holds these positions; the page table is read when it
+ * runs).  Errors: ANPD_E_CAPACITY (positions, workspace), ANPD_E_INVAL (also: a position without a page), ANPD_E_HIP. */
+size_t anpd_attention_workspace_bytes(const anpd_kv_t *const *kvs, int32_t n_seq, const int32_t *n_rows, const int32_t *pos0,
+                                      const anpd_attn_rules *rules);
+int32_t anpd_attention(const anpd_kv_t *const *kvs, int32_t n_seq, const int32_t *n_rows, const int32_t *pos0, int32_t layer,
+                       const void *q, int64_t ldq, int32_t dtype, const anpd_attn_rules *rules, void *out, int64_t ldo,
+                       float *lse, void *workspace, size_t workspace_bytes, void *stream);
+
+/* What the rows' weights add up to, per cached key: mass[g][j] += sum of exp(t - lse) over the rows and the query heads
+ * that share key / value head g.  Arguments as in anpd_attention, whose lse this takes (rows with an lse of -infinity add nothing).
+ *   mass (host, n_seq DEVICE pointers): [n_kv_heads][ld_mass] floats per sequence, ld_mass >= pos0[s] + n_rows[s]; no two
+ *   sequences may share any of it.  Columns from pos0[s] + n_rows[s] on are left as they are. */
+size_t anpd_key_mass_workspace_bytes(const anpd_kv_t *const *kvs, int32_t n_seq, const int32_t *n_rows, const int32_t *pos0,
+                                     const anpd_attn_rules *rules);
+int32_t anpd_key_mass(const anpd_kv_t *const *kvs, int32_t n_seq, const int32_t *n_rows, const int32_t *pos0, int32_t layer,
+                      const void *q, int64_t ldq, int32_t dtype, const anpd_attn_rules *rules, const float *lse,
+                      float *const *mass, int64_t ld_mass, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Eviction: of src's committed positions `keep` stay, per layer and key / value head those with the largest mass
+ * (equal ones: the lowest position; NaN counts as less than every number), the first `first` and the last `last` in any case.  They
+ * move together, in their order, into positions 0 .. keep - 1 of dst, whose length becomes keep; what dst held is
+ * gone.  dst may be src, or another cache of the same shape (a smaller one, say).
+ *   mass: DEVICE, [n_layers][n_kv_heads][ld_mass] floats, ld_mass >= src's length.
+ *   rope_base: 0 = keys are moved as they are; > 1 = a key that moves from position p to slot i is turned by i - p positions
+ *   (half-split pairing, as the model's own keys), so that it is the key of a token at position i, which is what
+ *   the steps that follow take it for.
+ *   out_kept: DEVICE, [n_layers][n_kv_heads][keep] ints, the positions that stayed, ascending.
+ *   out_mass (nullable): DEVICE, [n_layers][n_kv_heads][ld_out] floats, ld_out >= keep: their mass.  Must not overlap mass.
+ * 0 <= first + last <= keep <= length.  Blocks until it is done.
+ * Errors: ANPD_E_INVAL, ANPD_E_CAPACITY (keep against length or dst), ANPD_E_HIP (contents and length of dst undefined). */
+int32_t anpd_kv_evict(const anpd_kv_t *src, anpd_kv_t *dst, const float *mass, int64_t ld_mass, int32_t keep, int32_t first,
+                      int32_t last, float rope_base, int32_t *out_kept, float *out_mass, int64_t ld_out, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

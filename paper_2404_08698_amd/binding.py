@@ -33,6 +33,8 @@ EXPORTS = (
     "anpd_verify", "anpd_verify_tree", "anpd_verify_batch", "anpd_prefill_workspace_bytes", "anpd_prefill", "anpd_linear_workspace_bytes", "anpd_linear",
     "anpd_model_profile", "anpd_model_profile_read", "anpd_packed_bytes", "anpd_pack_weights",
     "anpd_model_trace", "anpd_model_set_barrier_spin_limit", "anpd_linear_static",
+    "anpd_cache_pool_bytes", "anpd_cache_create", "anpd_attention_workspace_bytes", "anpd_attention",
+    "anpd_key_mass_workspace_bytes", "anpd_key_mass", "anpd_kv_evict",
 )
 PROF_CATEGORIES = ("gemm_qkv", "gemm_o", "gemm_gate_up", "gemm_down", "gemm_lm_head", "attn", "other", "step")
 
@@ -49,6 +51,15 @@ class ModelCfg(C.Structure):
                 ("rms_eps", C.c_float), ("rope_base", C.c_float), ("dtype", C.c_int32),
                 ("page_tokens", C.c_int32), ("max_window", C.c_int32), ("max_positions", C.c_int32),
                 ("gemm_path", C.c_int32), ("n_kv_heads", C.c_int32)]
+
+
+class CacheCfg(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_layers", "n_heads", "head_dim", "n_kv_heads", "dtype", "page_tokens")]
+
+
+class AttnRules(C.Structure):
+    _fields_ = [("scale", C.c_float), ("cap", C.c_float), ("window", C.c_int32), ("prefix", C.c_int32),
+                ("slopes", C.c_void_p), ("first_key", C.c_void_p)]
 
 
 class Weights(C.Structure):
@@ -146,6 +157,21 @@ def lib():
     L.anpd_model_profile.argtypes = [vp, C.c_int32]
     L.anpd_model_profile_read.restype = C.c_int32
     L.anpd_model_profile_read.argtypes = [vp, C.POINTER(C.c_double), C.POINTER(C.c_int64), C.POINTER(C.c_int64)]
+    seqs = [vp, C.c_int32, vp, vp]
+    L.anpd_cache_pool_bytes.restype = C.c_size_t
+    L.anpd_cache_pool_bytes.argtypes = [C.POINTER(CacheCfg), C.c_int32]
+    L.anpd_cache_create.restype = C.c_int32
+    L.anpd_cache_create.argtypes = [C.POINTER(CacheCfg), vp, C.c_size_t, C.c_int32, C.POINTER(vp)]
+    L.anpd_attention_workspace_bytes.restype = C.c_size_t
+    L.anpd_attention_workspace_bytes.argtypes = seqs + [vp]
+    L.anpd_attention.restype = C.c_int32
+    L.anpd_attention.argtypes = seqs + [C.c_int32, vp, C.c_int64, C.c_int32, vp, vp, C.c_int64, vp, vp, C.c_size_t, vp]
+    L.anpd_key_mass_workspace_bytes.restype = C.c_size_t
+    L.anpd_key_mass_workspace_bytes.argtypes = seqs + [vp]
+    L.anpd_key_mass.restype = C.c_int32
+    L.anpd_key_mass.argtypes = seqs + [C.c_int32, vp, C.c_int64, C.c_int32, vp, vp, vp, C.c_int64, vp, C.c_size_t, vp]
+    L.anpd_kv_evict.restype = C.c_int32
+    L.anpd_kv_evict.argtypes = [vp, vp, vp, C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_float, vp, vp, C.c_int64, vp]
     _lib = L
     return L
 
@@ -324,6 +350,7 @@ class KVCache:
         _check(lib().anpd_kv_create(model._h, self.pool.data_ptr(), nbytes, max_tokens, C.byref(h)))
         self._h = h
         self.max_tokens = max_tokens
+        self.n_layers = model.shape.n_layers
 
     def close(self):
         try:
@@ -472,6 +499,175 @@ def linear_static(X, packed, N: int, Y, stream=None):
     M, K = X.shape
     _check(lib().anpd_linear_static(X.data_ptr(), packed.data_ptr(), Y.data_ptr(), M, N, K, _stream_ptr(stream)))
     return Y
+
+
+# ------------------------------------------------------ operators on caches
+
+class LayerCache(KVCache):
+    """anpd_cache_create: a paged cache without a model, for programs whose layers are their own.  All of KVCache's
+    methods; verify and prefill do not take it."""
+
+    def __init__(self, n_layers: int, n_heads: int, head_dim: int, max_tokens: int, n_kv_heads: int = 0, dtype: str = "bf16",
+                 page_tokens: int = 16, device="cuda"):
+        import torch
+        from types import SimpleNamespace
+        cfg = CacheCfg(n_layers, n_heads, head_dim, n_kv_heads, BF16 if dtype == "bf16" else F32, page_tokens)
+        nbytes = lib().anpd_cache_pool_bytes(C.byref(cfg), max_tokens)
+        if nbytes == 0:
+            _check(E_INVAL)
+        self.pool = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        # (what KVCache asks of its model)
+        self.model = SimpleNamespace(shape=SimpleNamespace(n_layers=n_layers, n_heads=n_heads, head_dim=head_dim, n_kv_heads=n_kv_heads or n_heads, dtype=dtype),
+                                     device=self.pool.device)
+        h = C.c_void_p()
+        with torch.cuda.device(self.pool.device):
+            _check(lib().anpd_cache_create(C.byref(cfg), self.pool.data_ptr(), nbytes, max_tokens, C.byref(h)))
+        self._h = h
+        self.max_tokens = max_tokens
+        self.n_layers = n_layers
+
+
+class AttentionRules:
+    """anpd_attn_rules: the rules of the scores for attention() and key_mass(); keeps its tensors alive."""
+
+    def __init__(self, scale: float = 0.0, cap: float = 0.0, window: int = 0, prefix: int = 0, slopes=None, first_key=None):
+        import torch
+        for t, dtype in ((slopes, torch.float32), (first_key, torch.int32)):
+            if t is not None and not (t.is_cuda and t.dtype == dtype and t.is_contiguous()):
+                raise ValueError("slopes: contiguous CUDA float32, first_key: contiguous CUDA int32")
+        self.slopes, self.first_key = slopes, first_key
+        self.struct = AttnRules(scale, cap, window, prefix, None if slopes is None else slopes.data_ptr(),
+                                None if first_key is None else first_key.data_ptr())
+        self.ref = C.addressof(self.struct)
+
+
+def _sequences(kvs, q, n_rows, pos0, rules):
+    """(first cache, n_seq, handles, rows, positions or None) for the calls on several caches."""
+    import torch
+    if isinstance(kvs, KVCache):
+        kvs = (kvs,)
+    n = len(kvs)
+    if n == 0:
+        raise ValueError("no cache")
+    first = kvs[0]
+    shape = first.model.shape
+    if not (q.is_cuda and q.device == first.pool.device and q.dim() == 2 and q.stride(1) == 1 and q.shape[1] == shape.n_heads * shape.head_dim
+            and q.dtype in (torch.float32, torch.bfloat16)):
+        raise ValueError("rows must be a 2-d float32 or bfloat16 tensor on the caches' device, n_heads * head_dim wide")
+    handles = (C.c_void_p * n)(*[kv._h.value for kv in kvs])
+    if n_rows is None:      # the same number of each sequence
+        if q.shape[0] % n:
+            raise ValueError("n_rows is needed: %d rows do not divide among %d sequences" % (q.shape[0], n))
+        counts = (C.c_int32 * n)(*([q.shape[0] // n] * n))
+    else:
+        if len(n_rows) != n or sum(n_rows) != q.shape[0] or min(n_rows) < 0:
+            raise ValueError("n_rows does not add up to the rows")
+        counts = (C.c_int32 * n)(*n_rows)
+    if pos0 is not None and len(pos0) != n:
+        raise ValueError("pos0: one per sequence")
+    if rules is not None:
+        if rules.slopes is not None and (rules.slopes.numel() < shape.n_heads or rules.slopes.device != q.device):
+            raise ValueError("slopes: one per head")
+        if rules.first_key is not None and (rules.first_key.numel() < q.shape[0] or rules.first_key.device != q.device):
+            raise ValueError("first_key: one per row")
+    return first, n, handles, counts, None if pos0 is None else (C.c_int32 * n)(*pos0)
+
+
+def _pitch(t) -> int:
+    """Elements between rows (of a single row, or none: its width)."""
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _workspace(workspace, nbytes, device):
+    import torch
+    if nbytes == 0:
+        return None, 0
+    if workspace is None:
+        workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    return workspace, workspace.numel() * workspace.element_size()
+
+
+def _on_device(device, stream):
+    """The stream of a call: the given one, or the device's current one."""
+    import torch
+    return (stream if stream is not None else torch.cuda.current_stream(device)).cuda_stream
+
+
+def attention_workspace_bytes(kvs, n_rows: Sequence[int], pos0: Optional[Sequence[int]] = None, rules: Optional[AttentionRules] = None) -> int:
+    """anpd_attention_workspace_bytes (0: none is needed)."""
+    kvs = (kvs,) if isinstance(kvs, KVCache) else kvs
+    return int(lib().anpd_attention_workspace_bytes((C.c_void_p * len(kvs))(*[kv._h.value for kv in kvs]), len(kvs), _ints(n_rows),
+                                                    None if pos0 is None else _ints(pos0), None if rules is None else rules.ref))
+
+
+def attention(kvs, layer: int, q, n_rows: Optional[Sequence[int]] = None, pos0: Optional[Sequence[int]] = None,
+              rules: Optional[AttentionRules] = None, out=None, lse=None, want_lse: bool = False, workspace=None, stream=None):
+    """anpd_attention: new rows of one cache or of a list of caches over what is cached.  q: CUDA float32 or bfloat16
+    [rows of all sequences][n_heads * head_dim].  Returns out, or (out, lse) where lse was given or asked for."""
+    import torch
+    first, n, handles, counts, at = _sequences(kvs, q, n_rows, pos0, rules)
+    if out is None:
+        out = torch.empty((q.shape[0], q.shape[1]), dtype=q.dtype, device=q.device)
+    elif not (out.device == q.device and out.dtype == q.dtype and out.shape == q.shape and out.stride(1) == 1):
+        raise ValueError("out must be like the rows")
+    if lse is None and want_lse:
+        lse = torch.empty((q.shape[0], first.model.shape.n_heads), dtype=torch.float32, device=q.device)
+    elif lse is not None and not (lse.device == q.device and lse.dtype == torch.float32 and lse.is_contiguous()
+                                  and tuple(lse.shape) == (q.shape[0], first.model.shape.n_heads)):
+        raise ValueError("lse: contiguous float32 [rows][n_heads]")
+    L, ref = lib(), None if rules is None else rules.ref
+    ws, nbytes = _workspace(workspace, L.anpd_attention_workspace_bytes(handles, n, counts, at, ref), q.device)
+    _check(L.anpd_attention(handles, n, counts, at, layer, q.data_ptr(), _pitch(q), F32 if q.dtype == torch.float32 else BF16, ref,
+                            out.data_ptr(), _pitch(out), None if lse is None else lse.data_ptr(), None if ws is None else ws.data_ptr(), nbytes,
+                            _on_device(q.device, stream)))
+    return out if lse is None else (out, lse)
+
+
+def key_mass(kvs, layer: int, q, lse, mass, n_rows: Optional[Sequence[int]] = None, pos0: Optional[Sequence[int]] = None,
+             rules: Optional[AttentionRules] = None, workspace=None, stream=None):
+    """anpd_key_mass: adds the rows' weights to mass and returns it.  mass: CUDA float32 [n_kv_heads][>= keys] for one
+    cache, [sequences][n_kv_heads][>= keys] for several; rows apart as they like, keys side by side."""
+    import torch
+    first, n, handles, counts, at = _sequences(kvs, q, n_rows, pos0, rules)
+    shape = first.model.shape
+    each = mass if mass.dim() == 3 else mass[None]
+    kv_heads = getattr(shape, "n_kv_heads", 0) or shape.n_heads
+    if not (mass.dtype == torch.float32 and mass.device == q.device and each.dim() == 3 and each.shape[0] == n and each.shape[1] == kv_heads and each.stride(2) == 1):
+        raise ValueError("mass: float32 [sequences][n_kv_heads][keys] on the caches' device")
+    if not (lse.device == q.device and lse.dtype == torch.float32 and lse.is_contiguous() and tuple(lse.shape) == (q.shape[0], shape.n_heads)):
+        raise ValueError("lse: contiguous float32 [rows][n_heads]")
+    ld = each.stride(1) if kv_heads > 1 else each.shape[2]
+    if ld < each.shape[2] or any(c + (kv.length if at is None else at[i]) > each.shape[2]
+                                 for i, (c, kv) in enumerate(zip(counts, (kvs,) if isinstance(kvs, KVCache) else kvs))):
+        raise ValueError("mass has fewer columns than there are keys")
+    step, base = each.stride(0) * 4, each.data_ptr()
+    ptrs = (C.c_void_p * n)(*[base + i * step for i in range(n)])
+    L, ref = lib(), None if rules is None else rules.ref
+    ws, nbytes = _workspace(workspace, L.anpd_key_mass_workspace_bytes(handles, n, counts, at, ref), q.device)
+    _check(L.anpd_key_mass(handles, n, counts, at, layer, q.data_ptr(), _pitch(q), F32 if q.dtype == torch.float32 else BF16, ref,
+                           lse.data_ptr(), ptrs, ld, None if ws is None else ws.data_ptr(), nbytes, _on_device(q.device, stream)))
+    return mass
+
+
+def evict(src: KVCache, mass, keep: int, first: int = 0, last: int = 0, into: Optional[KVCache] = None, rope_base: float = 0.0, stream=None):
+    """anpd_kv_evict: `keep` positions of src stay, per layer and key / value head those with the largest mass, the
+    first and last ones in any case; into: the cache that they move into (src itself if absent).  mass: CUDA float32
+    [n_layers][n_kv_heads][>= length].  Returns (positions [n_layers][n_kv_heads][keep] int32, their mass)."""
+    import torch
+    if not (mass.is_cuda and mass.device == src.pool.device and mass.dtype == torch.float32 and mass.dim() == 3 and mass.stride(2) == 1):
+        raise ValueError("mass: float32 [n_layers][n_kv_heads][positions] on the cache's device")
+    shape = src.model.shape
+    kv_heads = getattr(shape, "n_kv_heads", 0) or shape.n_heads
+    layers = src.n_layers
+    if mass.shape[:2] != (layers, kv_heads) or mass.shape[2] < src.length or (layers > 1 and mass.stride(0) != kv_heads * mass.stride(1)):
+        raise ValueError("mass: one row of at least the cache's length per layer and key / value head, equally far apart")
+    ld = mass.stride(1) if layers * kv_heads > 1 else mass.shape[2]
+    kept = torch.empty((layers, kv_heads, max(0, keep)), dtype=torch.int32, device=mass.device)
+    out = torch.empty((layers, kv_heads, max(0, keep)), dtype=torch.float32, device=mass.device)
+    dst = src if into is None else into
+    _check(lib().anpd_kv_evict(src._h, dst._h, mass.data_ptr(), ld, keep, first, last, rope_base, kept.data_ptr(), out.data_ptr(), max(0, keep),
+                               _on_device(mass.device, stream)))
+    return kept, out
 
 
 # ------------------------------------------------------------ decode loops

@@ -1,0 +1,963 @@
+// Attention of new rows over paged caches, and the weight that every cached key receives, for gfx950.
+//
+//   t_rj = scale q_r . k_j,   cap > 0: t = cap tanh(t / cap),   t -= slope_h |p_r - j|
+//   out_r = sum_j exp(t_rj - lse_r) v_j,   lse_r = log sum_j exp t_rj        over the keys that row r sees
+//   mass_gj += sum over the rows r and query heads h of group g of exp(t_rj - lse_r)
+//
+// Rows.  The query heads that share a key / value head read the same keys, so they are rows of one matrix: "virtual row"
+// v = r * group + h stands for head h of the group in row r.  Keys are then read once for all of them, and a token of a
+// model with 16 query heads per key / value head is 16 rows of a matrix product and not 16 products of one row.
+//
+// Products.  S^T = K q^T with 32x32 matrix instructions: a lane has 16 keys (8 (i / 4) + 4 half + i % 4, half = lane / 32) of
+// ONE row (lane % 32), so a row's maximum and sum are in-lane but for one exchange of the wave's halves, and the weights are,
+// as they stand in registers, the operand of O^T += V^T P: two groups of four keys per 16-key page and half.  The cache's
+// fragment order has both operands ready: K in 16-byte pieces of 8 dims of a key, V in 8-byte pieces of 4 keys of a dim.
+//
+// Precision.  Scores, maxima, sums and outputs are held in 32 bits.  bf16 rows meet bf16 keys exactly; their weights are
+// rounded to bf16 for the second product (2^-9 of a weight, as much as the output's own rounding).  fp32 rows are three bf16
+// terms, 24 bits, and so are their weights: two terms keep 2^-18 of every weight, which was ten times the error of fp32 sums.
+#pragma once
+#include "anpd_layout.h"
+
+namespace anpd {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kAttnMaxSeqs = ANPD_ATTN_MAX_SEQS;
+constexpr int kRowTile = 32;              // virtual rows of a wave
+constexpr float kNoKey = -3.0e38f;        // a row's reference before it has seen a key
+constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
+
+struct SeqView {
+    const void *pool;
+    const int32_t *table;   // physical pages
+    int32_t pos0, n, row0;  // position of the first new row, new rows, the first one's place among the rows of all sequences
+    int32_t block0;         // first row block
+};
+
+struct AttnArgs {
+    SeqView seq[kAttnMaxSeqs];
+    const void *q;
+    void *out;
+    float *lse;                 // [rows][heads]; may be NULL in attention
+    const float *slopes;        // [heads] or NULL
+    const int32_t *first_key;   // [rows] or NULL
+    float *part;                // attention: partial results of splits, or NULL; mass: partial sums, or NULL
+    int64_t ldq, ldo;           // elements between rows
+    float scale, cap;
+    int32_t window, prefix;     // 0: none
+    int32_t layer, n_layers, n_heads, n_kv_heads, group, page_tokens;
+    int32_t q_f32, q_wide;      // type of the rows and outputs; whether rows and outputs may be moved 16 bytes at a time
+    int32_t n_seq, n_blocks, n_splits, chunk;   // row blocks of all sequences; splits of the keys, tiles in each
+};
+
+struct MassOut {
+    float *mass[kAttnMaxSeqs];   // [kv head][ld]
+    int64_t ld;
+};
+
+// ------------------------------------------------------------------ rows and their keys
+
+// What a lane knows of its row.
+struct RowInfo {
+    int v;        // virtual row of the sequence (the last one again for lanes beyond it)
+    int row, head;   // its row among those of all sequences, its query head
+    int p;        // position
+    int fk, lo;   // first visible key; the same with the window
+    float slope;
+    bool live;    // a row of its own
+};
+template <bool RULES>
+__device__ __forceinline__ RowInfo row_info(const AttnArgs &a, const SeqView &s, int kvh, int v0)
+{
+    const int total = s.n * a.group, v = v0 + (threadIdx.x & 31);
+    RowInfo r;
+    r.live = v < total;
+    r.v = r.live ? v : total - 1;
+    r.row = r.v / a.group;
+    r.head = kvh * a.group + (r.v - r.row * a.group);
+    r.p = s.pos0 + r.row;
+    r.row += s.row0;
+    r.fk = 0;
+    r.lo = 0;
+    r.slope = 0.f;
+    if (RULES) {
+        if (a.slopes) r.slope = a.slopes[r.head];
+        if (a.first_key) r.fk = a.first_key[r.row];
+        r.lo = r.fk;
+        if (a.window > 0) { const int lo = r.p - a.window + 1; r.lo = lo > r.fk ? lo : r.fk; }
+    }
+    return r;
+}
+
+template <bool RULES>
+__device__ __forceinline__ bool sees(const RowInfo &r, int pre, int j)
+{
+    return RULES ? (j <= r.p && j >= r.lo) || (j < pre && j >= r.fk) : j <= r.p;
+}
+// Of the 32 keys from `base` on: does any of the wave's rows see one, do all see all?
+template <bool RULES>
+__device__ __forceinline__ bool any_seen(const RowInfo &r, int pre, int base)
+{
+    return __builtin_amdgcn_ballot_w64(RULES ? (base <= r.p && base + 31 >= r.lo && r.lo <= r.p) || (base < pre && base + 31 >= r.fk) : base <= r.p) != 0;
+}
+template <bool RULES>
+__device__ __forceinline__ bool all_seen(const RowInfo &r, int pre, int base)
+{
+    return __builtin_amdgcn_ballot_w64(!(RULES ? (base + 31 <= r.p && base >= r.lo) || (base + 31 < pre && base >= r.fk) : base + 31 <= r.p)) == 0;
+}
+
+// The key tiles (of `tile` keys) that rows with positions p_lo .. p_hi can see: the prefix, then what the window leaves.
+// Known on the host as well (first_key is not looked at).
+struct KeyTiles {
+    int a, b0, n;   // tiles of the prefix; the first one behind them that is visited; how many are visited
+    __host__ __device__ int at(int i) const { return i < a ? i : b0 + (i - a); }
+};
+__host__ __device__ __forceinline__ KeyTiles key_tiles(int p_lo, int p_hi, int total, int window, int prefix, int tile)
+{
+    KeyTiles k;
+    const int pre = prefix < total ? prefix : total;
+    const int lo = window > 0 && p_lo - window + 1 > 0 ? p_lo - window + 1 : 0;
+    k.a = (pre + tile - 1) / tile;
+    k.b0 = lo / tile > k.a ? lo / tile : k.a;
+    const int b1 = p_hi / tile + 1;
+    k.n = k.a + (b1 > k.b0 ? b1 - k.b0 : 0);
+    return k;
+}
+
+// tanh, to 2^-23 of its value: a sum of powers where 1 - 2 / (1 + e^2x) would lose them
+__device__ __forceinline__ float tanh_f32(float x)
+{
+    const float y = x * x;
+    float s = fmaf(y, -1382.0f / 155925.0f, 62.0f / 2835.0f);
+    s = fmaf(y, s, -17.0f / 315.0f);
+    s = fmaf(y, s, 2.0f / 15.0f);
+    s = fmaf(y, s, -1.0f / 3.0f);
+    s = fmaf(y * x, s, x);
+    const float e = __builtin_amdgcn_exp2f(fabsf(x) * (2.0f * kLog2e));
+    const float t = 1.0f - 2.0f / (1.0f + e);
+    return y < 0.08f ? s : copysignf(t, x);
+}
+
+// Products to scores where there are rules (cap, bias): natural units.
+__device__ __forceinline__ float ruled_score(const AttnArgs &a, float product, float slope, int distance)
+{
+    float t = product * a.scale;
+    if (a.cap > 0.f) t = a.cap * tanh_f32(t / a.cap);
+    if (a.slopes) t = fmaf(-slope, (float)(distance < 0 ? -distance : distance), t);
+    return t;
+}
+
+// ------------------------------------------------------------------ operands
+
+__device__ __forceinline__ bf16x8 as_bf16(u32x4 v) { return __builtin_bit_cast(bf16x8, v); }
+__device__ __forceinline__ f32x16 mfma32(bf16x8 x, bf16x8 y, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, y, c, 0, 0, 0); }
+
+// Eight numbers as TERMS bf16 operands that add up to them (1: rounded; 3: exact but for the smallest of numbers).
+template <int TERMS>
+__device__ __forceinline__ void split_terms(const float (&x)[8], u32x4 (&t)[TERMS])
+{
+    float r[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r[i] = x[i];
+#pragma unroll
+    for (int k = 0; k < TERMS; ++k)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t w = pack_bf16(r[2 * i], r[2 * i + 1]);
+            t[k][i] = w;
+            if (k + 1 < TERMS) {
+                r[2 * i] -= __uint_as_float(w << 16);
+                r[2 * i + 1] -= __uint_as_float(w & 0xffff0000u);
+            }
+        }
+}
+
+// Eight dims of a row, whatever its type and alignment.
+__device__ __forceinline__ void load_q8(const AttnArgs &a, size_t at, float (&x)[8])
+{
+    if (a.q_f32) {
+        const float *p = (const float *)a.q + at;
+        if (a.q_wide) {
+            const f32x4 u = *(const f32x4 *)p, v = *(const f32x4 *)(p + 4);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { x[i] = u[i]; x[4 + i] = v[i]; }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = p[i];
+        }
+    } else {
+        const bf16_t *p = (const bf16_t *)a.q + at;
+        if (a.q_wide) {
+            const u32x4 u = *(const u32x4 *)p;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(u[i] << 16); x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u); }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = bf16_to_f32(p[i]);
+        }
+    }
+}
+template <int TERMS>
+__device__ __forceinline__ void load_q8(const AttnArgs &a, size_t at, u32x4 (&t)[TERMS])
+{
+    if constexpr (TERMS == 1) {   // (bf16 rows are the operand as they are)
+        const bf16_t *p = (const bf16_t *)a.q + at;
+        if (a.q_wide) t[0] = *(const u32x4 *)p;
+        else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) t[0][i] = (uint32_t)p[2 * i] | ((uint32_t)p[2 * i + 1] << 16);
+        }
+    } else {
+        float x[8];
+        load_q8(a, at, x);
+        split_terms<TERMS>(x, t);
+    }
+}
+// ------------------------------------------------------------------ the running softmax of a wave's rows
+
+// A lane's numbers: the row's reference (base 2), the sum of its own half's weights, the output's 16 dims per tile of 32.
+template <int NDT>
+struct Running {
+    float m, l;
+    f32x16 o[NDT];
+    __device__ __forceinline__ void start()
+    {
+        m = kNoKey;
+        l = 0.f;
+#pragma unroll
+        for (int d = 0; d < NDT; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
+    }
+};
+
+__device__ __forceinline__ float both_halves_max(float v)
+{
+    const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
+}
+__device__ __forceinline__ float both_halves_sum(float v)
+{
+    const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(x[0]) + __uint_as_float(x[1]);
+}
+
+// Products of NB x 32 keys -> weights, in place; the row's reference, sum and output move along.  Keys that the row does not
+// see have weight 0.  The reference follows the row's maximum only when that is more than 2^8 above it: weights are at most 2^8
+// then, which costs no precision, and the output is rescaled a few times instead of at every other tile.
+template <bool RULES, int NB, int NDT>
+__device__ __forceinline__ void weigh(const AttnArgs &a, const RowInfo &r, int pre, int base, f32x16 (&s)[NB], Running<NDT> &run)
+{
+    const int half = (threadIdx.x >> 5) & 1;
+    float factor = a.scale * kLog2e;
+    if (RULES && (a.cap > 0.f || a.slopes)) {   // (the same for all)
+        factor = kLog2e;
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[b][i] = ruled_score(a, s[b][i], r.slope, r.p - (base + 32 * b + 8 * (i >> 2) + 4 * half + (i & 3)));
+    }
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+        if (all_seen<RULES>(r, pre, base + 32 * b)) continue;   // (the same for the whole wave)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            if (!sees<RULES>(r, pre, base + 32 * b + 8 * (i >> 2) + 4 * half + (i & 3))) s[b][i] = -INFINITY;
+    }
+    float mx = -INFINITY;
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; i += 2) mx = fmaxf(fmaxf(mx, s[b][i]), s[b][i + 1]);
+    mx = both_halves_max(mx) * factor;
+    const float m_new = mx > run.m + 8.f ? mx : run.m, alpha = __builtin_amdgcn_exp2f(run.m - m_new);
+    run.m = m_new;
+    // (where the reference is huge, the fused product is not the product that it was rounded from, and the difference, up to 2^-24
+    // of it, would be the largest key's exponent)
+    if (__builtin_amdgcn_ballot_w64(fabsf(m_new) > 0x1p28f) != 0) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                float t = s[b][i] * factor;
+                asm volatile("" : "+v"(t));
+                s[b][i] = __builtin_amdgcn_exp2f(t - m_new);
+            }
+    } else {
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[b][i] = __builtin_amdgcn_exp2f(fmaf(s[b][i], factor, -m_new));
+    }
+    float sum = 0.f;
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+        float t[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) t[i] = (s[b][4 * i] + s[b][4 * i + 1]) + (s[b][4 * i + 2] + s[b][4 * i + 3]);
+        sum += (t[0] + t[1]) + (t[2] + t[3]);
+    }
+    run.l = fmaf(run.l, alpha, sum);
+    if (__builtin_amdgcn_ballot_w64(alpha != 1.f) != 0) {   // (a factor of 1 changes nothing)
+#pragma unroll
+        for (int d = 0; d < NDT; ++d) run.o[d] = run.o[d] * alpha;
+    }
+}
+
+// bf16 operands whose numbers are all finite?
+__device__ __forceinline__ bool finite8(u32x4 v)
+{
+    bool ok = true;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) ok = ok && (v[i] & 0x7f80u) != 0x7f80u && (v[i] & 0x7f800000u) != 0x7f800000u;
+    return ok;
+}
+
+// O += V^T P where some key of the page is hidden from some row and some value is not finite: 0 times an infinity would put
+// NaN into rows that do not see it.  The finite values as ever; of the others, how many a row sees of each kind.
+template <int TERMS>
+__device__ __forceinline__ void add_values_careful(f32x16 &o, u32x4 v, const u32x4 (&w)[TERMS], u32x4 seen)
+{
+    u32x4 fin, up, down, nan;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        fin[i] = up[i] = down[i] = nan[i] = 0;
+#pragma unroll
+        for (int h = 0; h < 32; h += 16) {
+            const uint32_t x = (v[i] >> h) & 0xffffu, one = 0x3f80u << h;
+            if ((x & 0x7f80u) != 0x7f80u) fin[i] |= x << h;
+            else if (x & 0x7fu) nan[i] |= one;
+            else if (x & 0x8000u) down[i] |= one;
+            else up[i] |= one;
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < TERMS; ++k) o = mfma32(as_bf16(fin), as_bf16(w[k]), o);
+    const f32x16 zero = {};
+    const f32x16 n_up = mfma32(as_bf16(up), as_bf16(seen), zero), n_down = mfma32(as_bf16(down), as_bf16(seen), zero), n_nan = mfma32(as_bf16(nan), as_bf16(seen), zero);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        if (n_up[i] > 0.f) o[i] += INFINITY;
+        if (n_down[i] > 0.f) o[i] -= INFINITY;
+        if (n_nan[i] > 0.f) o[i] += __builtin_nanf("");
+    }
+}
+
+// A lane's eight keys of page g (0, 1) of a 32-key tile: 1 where the row sees them, 0 elsewhere.
+template <bool RULES>
+__device__ __forceinline__ u32x4 seen_operand(const RowInfo &r, int pre, int base, int g)
+{
+    const int half = (threadIdx.x >> 5) & 1;
+    u32x4 m;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int j = base + 16 * g + 8 * (i >> 1) + 4 * half + 2 * (i & 1);
+        m[i] = (sees<RULES>(r, pre, j) ? 0x3f80u : 0u) | (sees<RULES>(r, pre, j + 1) ? 0x3f800000u : 0u);
+    }
+    return m;
+}
+
+// ------------------------------------------------------------------ results
+
+// Four adjacent dims of a row.
+__device__ __forceinline__ void store_out4(const AttnArgs &a, int head_dim, int row, int head, int dim, f32x4 x)
+{
+    const size_t at = (size_t)row * a.ldo + (size_t)head * head_dim + dim;
+    if (a.q_f32) {
+        float *p = (float *)a.out + at;
+        if (a.q_wide) *(f32x4 *)p = x;
+        else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) p[i] = x[i];
+        }
+    } else {
+        bf16_t *p = (bf16_t *)a.out + at;
+        const uint2 w = make_uint2(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]));
+        if (a.q_wide) *(uint2 *)p = w;
+        else {
+            p[0] = (bf16_t)w.x; p[1] = (bf16_t)(w.x >> 16); p[2] = (bf16_t)w.y; p[3] = (bf16_t)(w.y >> 16);
+        }
+    }
+}
+__device__ __forceinline__ void store_lse(const AttnArgs &a, int row, int head, float m, float l)
+{
+    // (a row without a key: -infinity)
+    if (a.lse) a.lse[(size_t)row * a.n_heads + head] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+}
+__device__ __forceinline__ float inverse_sum(float l) { return l == 0.f ? 0.f : 1.0f / l; }
+
+// Where a split's results lie: per (row block, kv head, split) [row][dim] and then [row] of (reference, sum).
+__host__ __device__ __forceinline__ size_t part_floats(int rows, int head_dim) { return (size_t)rows * (head_dim + 2); }
+
+// The sequence of a row block (the last one whose blocks begin at or before it; sequences without rows have none).
+__device__ __forceinline__ int seq_of_block(const AttnArgs &a, int block)
+{
+    int lo = 0, hi = a.n_seq - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (a.seq[mid].block0 <= block) lo = mid;
+        else hi = mid - 1;
+    }
+    return lo;
+}
+
+// ------------------------------------------------------------------ keys and values straight into registers
+//
+// Block = (32 virtual rows, kv head, split of the keys), four waves; wave w takes keys 32 w .. of every 128.  Nothing is shared
+// while the keys go by: a wave's loads are the operands, the next keys are requested when this tile's scores are done, its values
+// when its output is, and the waves meet at the end.   grid: n_blocks * n_splits * n_kv_heads
+constexpr int kStreamWaves = 4, kStreamTile = 32 * kStreamWaves;
+
+template <int DH, int TERMS, bool RULES>
+__global__ __launch_bounds__(256, TERMS == 1 ? 2 : 1) void cache_attn_stream_kernel(const AttnArgs a)
+{
+    constexpr int NKS = DH / 16, NDT = DH / 32, NDB = DH / 64;
+    __shared__ float part[kStreamWaves][2][16][64];   // the waves' outputs, 64 dims at a time
+    __shared__ float wm[kStreamWaves][32], wl[kStreamWaves][32];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, m = lane & 31;
+    const int kvh = blockIdx.x % a.n_kv_heads, rest = blockIdx.x / a.n_kv_heads;
+    const int split = rest % a.n_splits, block = a.n_blocks - 1 - rest / a.n_splits;
+    const SeqView s = a.seq[seq_of_block(a, block)];
+    const int v0 = (block - s.block0) * kRowTile, total = s.pos0 + s.n;
+    const RowInfo r = row_info<RULES>(a, s, kvh, v0);
+    const int pre = RULES && a.prefix > 0 ? (a.prefix < total ? a.prefix : total) : 0;
+    const KeyTiles tiles = key_tiles(__builtin_amdgcn_readlane(r.p, 0), __builtin_amdgcn_readlane(r.p, 31), total, RULES ? a.window : 0, RULES ? a.prefix : 0, kStreamTile);
+    const int i0 = split * a.chunk, i1 = i0 + a.chunk < tiles.n ? i0 + a.chunk : tiles.n;
+    if (i0 >= tiles.n) return;   // (the whole block; what joins the splits does not look at this one)
+
+    u32x4 q[NKS][TERMS];
+    {
+        const size_t at = (size_t)r.row * a.ldq + (size_t)r.head * DH + 8 * half;
+#pragma unroll
+        for (int ks = 0; ks < NKS; ++ks) load_q8<TERMS>(a, at + 16 * ks, q[ks]);
+    }
+    Running<NDT> run;
+    run.start();
+
+    const int last_page = (total - 1) >> 4;
+    const bf16_t *pool = (const bf16_t *)s.pool;
+    const size_t page_elems = (size_t)a.n_layers * 2 * a.n_kv_heads * 16 * DH;
+    const bf16_t *k_of = pool + ((size_t)a.layer * 2 * a.n_kv_heads + kvh) * (16 * DH), *v_of = k_of + (size_t)a.n_kv_heads * (16 * DH);
+    // physical pages of the wave's next 64 tiles, a tile per lane (beyond the last key: the last page again)
+    int ida = 0, idb = 0;
+    auto fetch_ids = [&](int i) __attribute__((always_inline)) {
+        const int t = i + lane < i1 ? i + lane : i1 - 1;
+        const int page = tiles.at(t) * (kStreamTile / 16) + 2 * wave;
+        ida = s.table[page < last_page ? page : last_page];
+        idb = s.table[page + 1 < last_page ? page + 1 : last_page];
+    };
+    u32x4 kf[NKS], vf[2][NDB][2];   // values: [page][64 dims][keys 4 half.., 8 + 4 half..], two dims side by side
+    auto load_k = [&](int pa, int pb) __attribute__((always_inline)) {
+        const u32x4 *p = (const u32x4 *)(k_of + (size_t)(lane & 16 ? pb : pa) * page_elems) + half * 16 + (lane & 15);
+#pragma unroll
+        for (int ks = 0; ks < NKS; ++ks) kf[ks] = p[(ks >> 1) * 64 + (ks & 1) * 32];
+    };
+    auto load_v = [&](int pa, int pb) __attribute__((always_inline)) {
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+            const u32x4 *p = (const u32x4 *)(v_of + (size_t)(g ? pb : pa) * page_elems) + (m >> 3) * 32 + half * 8 + (m & 7);
+#pragma unroll
+            for (int d = 0; d < NDB; ++d)
+#pragma unroll
+                for (int x = 0; x < 2; ++x) vf[g][d][x] = p[d * 128 + x * 16];
+        }
+    };
+    {
+        fetch_ids(i0);
+        const int pa = __builtin_amdgcn_readlane(ida, 0), pb = __builtin_amdgcn_readlane(idb, 0);
+        load_k(pa, pb);
+        load_v(pa, pb);
+        for (int i = i0; i < i1; ++i) {
+            const int base = tiles.at(i) * kStreamTile + 32 * wave;
+            const int nx = (i + 1 - i0) & 63;
+            if (nx == 0) fetch_ids(i + 1);
+            const int na = __builtin_amdgcn_readlane(ida, nx), nb = __builtin_amdgcn_readlane(idb, nx);
+            f32x16 sc[1];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) sc[0][e] = 0.f;
+#pragma unroll
+            for (int t = TERMS - 1; t >= 0; --t)
+#pragma unroll
+                for (int ks = 0; ks < NKS; ++ks) sc[0] = mfma32(as_bf16(kf[ks]), as_bf16(q[ks][t]), sc[0]);
+            load_k(na, nb);
+            if (any_seen<RULES>(r, pre, base)) {
+                weigh<RULES, 1, NDT>(a, r, pre, base, sc, run);
+                const bool hidden = !all_seen<RULES>(r, pre, base);
+#pragma unroll
+                for (int g = 0; g < 2; ++g) {
+                    float x[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[e] = sc[0][8 * g + e];
+                    u32x4 w[TERMS];
+                    split_terms<TERMS>(x, w);
+                    bool careful = false;
+                    if (hidden) {
+                        bool ok = true;
+#pragma unroll
+                        for (int d = 0; d < NDB; ++d) ok = ok && finite8(vf[g][d][0]) && finite8(vf[g][d][1]);
+                        careful = __builtin_amdgcn_ballot_w64(!ok) != 0;
+                    }
+                    const u32x4 seen = careful ? seen_operand<RULES>(r, pre, base, g) : (u32x4){0, 0, 0, 0};
+#pragma unroll
+                    for (int d = 0; d < NDB; ++d)
+#pragma unroll
+                        for (int odd = 0; odd < 2; ++odd) {
+                            const u32x4 v = {vf[g][d][0][2 * odd], vf[g][d][0][2 * odd + 1], vf[g][d][1][2 * odd], vf[g][d][1][2 * odd + 1]};
+                            f32x16 &o = run.o[2 * d + odd];
+                            if (careful) add_values_careful<TERMS>(o, v, w, seen);
+                            else {
+#pragma unroll
+                                for (int t = TERMS - 1; t >= 0; --t) o = mfma32(as_bf16(v), as_bf16(w[t]), o);
+                            }
+                        }
+                }
+            }
+            load_v(na, nb);
+        }
+    }
+    // ---- the waves meet: every wave scales to the row's reference, the sums are formed in wave order
+    const float l = both_halves_sum(run.l);
+    if (half == 0) { wm[wave][m] = run.m; wl[wave][m] = l; }
+    __syncthreads();
+    float top = wm[0][m];
+#pragma unroll
+    for (int w = 1; w < kStreamWaves; ++w) top = fmaxf(top, wm[w][m]);
+    const float f = __builtin_amdgcn_exp2f(run.m - top);
+    float sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < kStreamWaves; ++w) sum = fmaf(wl[w][m], __builtin_amdgcn_exp2f(wm[w][m] - top), sum);
+    float *to = a.part ? a.part + (((size_t)block * a.n_kv_heads + kvh) * a.n_splits + split) * part_floats(kRowTile, DH) : nullptr;
+    if (wave == 0 && half == 0) {
+        if (to) *(float2 *)(to + kRowTile * DH + 2 * m) = make_float2(top, sum);
+        else if (r.live) store_lse(a, r.row, r.head, top, sum);
+    }
+    const float inv = inverse_sum(sum);
+#pragma unroll
+    for (int d = 0; d < NDB; ++d) {
+        if (d > 0) __syncthreads();
+#pragma unroll
+        for (int odd = 0; odd < 2; ++odd) {
+            const f32x16 o = run.o[2 * d + odd] * f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) part[wave][odd][i][lane] = o[i];
+        }
+        __syncthreads();
+        // wave w finishes registers 4 w .. 4 w + 3 of both tiles: eight adjacent dims of the lane's row
+        f32x4 x[2];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int odd = 0; odd < 2; ++odd) {
+                float t = part[0][odd][4 * wave + i][lane];
+#pragma unroll
+                for (int w = 1; w < kStreamWaves; ++w) t += part[w][odd][4 * wave + i][lane];
+                x[i >> 1][2 * (i & 1) + odd] = t;
+            }
+        const int dim = 64 * d + 16 * wave + 8 * half;
+        if (to) {
+            *(f32x4 *)(to + m * DH + dim) = x[0];
+            *(f32x4 *)(to + m * DH + dim + 4) = x[1];
+        } else if (r.live) {
+            store_out4(a, DH, r.row, r.head, dim, x[0] * inv);
+            store_out4(a, DH, r.row, r.head, dim + 4, x[1] * inv);
+        }
+    }
+}
+
+// ------------------------------------------------------------------ caches in plain order
+//
+// Blocks of [token][dim] in fp32 or bf16, pages of 8 to 256 tokens: exact fp32 products (v_mfma_f32_32x32x2_f32, whose lanes hold
+// the same rows and keys as above).  The two contracted numbers of an instruction are dims t and t + head_dim / 2 of a key, so a lane
+// reads half a key in one piece.  Blocks, waves and splits as above.
+// grid: n_blocks * n_splits * n_kv_heads
+__device__ __forceinline__ f32x16 mfma32f(float x, float y, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x2f32(x, y, c, 0, 0, 0); }
+
+template <int DH>
+__device__ __forceinline__ void load_half(const float *p, float (&x)[DH / 2])
+{
+#pragma unroll
+    for (int i = 0; i < DH / 8; ++i) {
+        const f32x4 u = ((const f32x4 *)p)[i];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[4 * i + e] = u[e];
+    }
+}
+template <int DH>
+__device__ __forceinline__ void load_half(const bf16_t *p, float (&x)[DH / 2])
+{
+#pragma unroll
+    for (int i = 0; i < DH / 16; ++i) {
+        const u32x4 u = ((const u32x4 *)p)[i];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { x[8 * i + 2 * e] = __uint_as_float(u[e] << 16); x[8 * i + 2 * e + 1] = __uint_as_float(u[e] & 0xffff0000u); }
+    }
+}
+
+template <typename KT, int DH>
+__global__ __launch_bounds__(256, 1) void cache_attn_plain_kernel(const AttnArgs a)
+{
+    constexpr int NDT = DH / 32;
+    __shared__ float part[kStreamWaves][16][64];
+    __shared__ float wm[kStreamWaves][32], wl[kStreamWaves][32];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, m = lane & 31;
+    const int kvh = blockIdx.x % a.n_kv_heads, rest = blockIdx.x / a.n_kv_heads;
+    const int split = rest % a.n_splits, block = a.n_blocks - 1 - rest / a.n_splits;
+    const SeqView s = a.seq[seq_of_block(a, block)];
+    const int v0 = (block - s.block0) * kRowTile, total = s.pos0 + s.n, pt = a.page_tokens;
+    const RowInfo r = row_info<true>(a, s, kvh, v0);
+    const int pre = a.prefix > 0 ? (a.prefix < total ? a.prefix : total) : 0;
+    const KeyTiles tiles = key_tiles(__builtin_amdgcn_readlane(r.p, 0), __builtin_amdgcn_readlane(r.p, 31), total, a.window, a.prefix, kStreamTile);
+    const int i0 = split * a.chunk, i1 = i0 + a.chunk < tiles.n ? i0 + a.chunk : tiles.n;
+    if (i0 >= tiles.n) return;
+    float q[DH / 2];
+    {
+        const size_t at = (size_t)r.row * a.ldq + (size_t)r.head * DH + half * (DH / 2);
+#pragma unroll
+        for (int i = 0; i < DH / 16; ++i) {
+            float x[8];
+            load_q8(a, at + 8 * i, x);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) q[8 * i + e] = x[e];
+        }
+    }
+    Running<NDT> run;
+    run.start();
+    const KT *pool = (const KT *)s.pool;
+    for (int i = i0; i < i1; ++i) {
+        const int base = tiles.at(i) * kStreamTile + 32 * wave;
+        if (!any_seen<true>(r, pre, base)) continue;
+        f32x16 sc[1];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sc[0][e] = 0.f;
+        {
+            const int key = base + m < total ? base + m : total - 1;
+            float k[DH / 2];
+            load_half<DH>(pool + kv_offset(s.table[key / pt], a.layer, a.n_layers, 0, kvh, a.n_kv_heads, key % pt, pt, DH) + half * (DH / 2), k);
+#pragma unroll
+            for (int t = 0; t < DH / 2; ++t) sc[0] = mfma32f(k[t], q[t], sc[0]);
+        }
+        weigh<true, 1, NDT>(a, r, pre, base, sc, run);
+        const bool hidden = !all_seen<true>(r, pre, base);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const int j = base + 8 * (e >> 2) + 4 * half + (e & 3), key = j < total ? j : total - 1;
+            const KT *p = pool + kv_offset(s.table[key / pt], a.layer, a.n_layers, 1, kvh, a.n_kv_heads, key % pt, pt, DH) + m;
+#pragma unroll
+            for (int d = 0; d < NDT; ++d) {
+                const float v = load_f32(p, 32 * d);
+                if (hidden && __builtin_amdgcn_ballot_w64(!(fabsf(v) <= 3.4028234e38f)) != 0) {
+                    // 0 times an infinity would put NaN into rows that do not see the key: see add_values_careful
+                    const bool fin = fabsf(v) <= 3.4028234e38f;
+                    const f32x16 zero = {};
+                    const float seen = sees<true>(r, pre, j) ? 1.f : 0.f;
+                    run.o[d] = mfma32f(fin ? v : 0.f, sc[0][e], run.o[d]);
+                    const f32x16 n_up = mfma32f(v == INFINITY ? 1.f : 0.f, seen, zero), n_down = mfma32f(v == -INFINITY ? 1.f : 0.f, seen, zero),
+                                 n_nan = mfma32f(v != v ? 1.f : 0.f, seen, zero);
+#pragma unroll
+                    for (int x = 0; x < 16; ++x) {
+                        if (n_up[x] > 0.f) run.o[d][x] += INFINITY;
+                        if (n_down[x] > 0.f) run.o[d][x] -= INFINITY;
+                        if (n_nan[x] > 0.f) run.o[d][x] += __builtin_nanf("");
+                    }
+                } else run.o[d] = mfma32f(v, sc[0][e], run.o[d]);
+            }
+        }
+    }
+    const float l = both_halves_sum(run.l);
+    if (half == 0) { wm[wave][m] = run.m; wl[wave][m] = l; }
+    __syncthreads();
+    float top = wm[0][m];
+#pragma unroll
+    for (int w = 1; w < kStreamWaves; ++w) top = fmaxf(top, wm[w][m]);
+    const float f = __builtin_amdgcn_exp2f(run.m - top);
+    float sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < kStreamWaves; ++w) sum = fmaf(wl[w][m], __builtin_amdgcn_exp2f(wm[w][m] - top), sum);
+    float *to = a.part ? a.part + (((size_t)block * a.n_kv_heads + kvh) * a.n_splits + split) * part_floats(kRowTile, DH) : nullptr;
+    if (wave == 0 && half == 0) {
+        if (to) *(float2 *)(to + kRowTile * DH + 2 * m) = make_float2(top, sum);
+        else if (r.live) store_lse(a, r.row, r.head, top, sum);
+    }
+    const float inv = inverse_sum(sum);
+#pragma unroll
+    for (int d = 0; d < NDT; ++d) {
+        if (d > 0) __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 16; ++i) part[wave][i][lane] = run.o[d][i] * f;
+        __syncthreads();
+        f32x4 x;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[i] = part[0][4 * wave + i][lane];
+#pragma unroll
+            for (int w = 1; w < kStreamWaves; ++w) x[i] += part[w][4 * wave + i][lane];
+        }
+        const int dim = 32 * d + 8 * wave + 4 * half;
+        if (to) *(f32x4 *)(to + m * DH + dim) = x;
+        else if (r.live) store_out4(a, DH, r.row, r.head, dim, x * inv);
+    }
+}
+
+// ------------------------------------------------------------------ the splits meet
+//
+// Block = (32 virtual rows, kv head): four adjacent dims of a row per thread, the splits in their order.
+// grid: n_kv_heads * n_blocks
+template <int DH>
+__global__ __launch_bounds__(256) void cache_attn_join_kernel(const AttnArgs a)
+{
+    constexpr int TPR = DH / 4, RPP = 256 / TPR;   // threads of a row, rows at a time
+    const int kvh = blockIdx.x % a.n_kv_heads, block = blockIdx.x / a.n_kv_heads;
+    const SeqView s = a.seq[seq_of_block(a, block)];
+    const int vb = (block - s.block0) * kRowTile, rows = s.n * a.group;
+    const int p_lo = s.pos0 + vb / a.group, p_hi = s.pos0 + (vb + kRowTile <= rows ? vb + kRowTile - 1 : rows - 1) / a.group;
+    const KeyTiles tiles = key_tiles(p_lo, p_hi, s.pos0 + s.n, a.window, a.prefix, kStreamTile);
+    const int used = (tiles.n + a.chunk - 1) / a.chunk;
+    const size_t stride = part_floats(kRowTile, DH);
+    const float *from = a.part + ((size_t)block * a.n_kv_heads + kvh) * a.n_splits * stride;
+    for (int i = 0; i < kRowTile; i += RPP) {
+        const int row = i + (int)threadIdx.x / TPR, dim = (int)threadIdx.x % TPR * 4, v = vb + row;
+        if (v >= rows) continue;
+        const float *ml = from + kRowTile * DH + 2 * row, *o = from + row * DH + dim;
+        float top = kNoKey;
+        for (int k = 0; k < used; ++k) top = fmaxf(top, ml[k * stride]);
+        float sum = 0.f;
+        f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+        for (int k = 0; k < used; ++k) {
+            const float2 t = *(const float2 *)(ml + k * stride);
+            const float f = __builtin_amdgcn_exp2f(t.x - top);
+            sum = fmaf(t.y, f, sum);
+            x += *(const f32x4 *)(o + k * stride) * f;
+        }
+        const int r = v / a.group, out_row = s.row0 + r, head = kvh * a.group + (v - r * a.group);
+        if (dim == 0) store_lse(a, out_row, head, top, sum);
+        store_out4(a, DH, out_row, head, dim, x * inverse_sum(sum));
+    }
+}
+
+// ------------------------------------------------------------------ the weight of every key
+//
+// Block = (128 keys, kv head, part of the rows), four waves of 32 keys, whose operands a wave holds in registers while the rows go by
+// in tiles of 32 through LDS (fp32 rows are split into their terms there, once for the four waves).  A lane adds the weights of its
+// row's 16 keys to 16 sums over all tiles; the lanes meet at the end.  One block owns a key's sum, so there are no atomics and
+// the order is always the same; where keys are too few for all compute units, the rows are dealt to several blocks whose sums are
+// added in order by a second kernel.  exp(t - lse) is formed from the difference, not from two numbers scaled to base 2 first,
+// whose roundings would stay in it.
+// a.block0 / n_blocks / n_splits / chunk: blocks of keys; parts of the rows, row tiles in each.
+// grid: n_blocks * n_splits * n_kv_heads
+constexpr int kMassKeys = 128;
+
+// The row tiles that can see keys kb .. kb + 127: first one and one behind the last.
+struct RowTiles {
+    int t0, t1;
+};
+__host__ __device__ __forceinline__ RowTiles row_tiles(int kb, int pos0, int n, int group, int window, int prefix)
+{
+    const long long rows = (long long)n * group;
+    long long v0 = 0, v1 = rows;
+    if (kb >= prefix) {
+        v0 = (long long)(kb - pos0) * group;
+        if (v0 < 0) v0 = 0;
+        if (window > 0) {
+            v1 = ((long long)kb + kMassKeys - 1 + window - pos0) * group;
+            if (v1 > rows) v1 = rows;
+        }
+    }
+    RowTiles t;
+    t.t0 = (int)(v0 / kRowTile);
+    t.t1 = v1 > v0 ? (int)((v1 + kRowTile - 1) / kRowTile) : t.t0;
+    return t;
+}
+
+// Weights of the lane's 16 keys, added to `acc`.
+template <bool RULES>
+__device__ __forceinline__ void add_weights(const AttnArgs &a, const RowInfo &r, float lse, int pre, int base, const f32x16 &s, f32x16 &acc)
+{
+    const int half = (threadIdx.x >> 5) & 1;
+    const bool scored = RULES && (a.cap > 0.f || a.slopes);
+    if (!scored && all_seen<RULES>(r, pre, base)) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[i] += __builtin_amdgcn_exp2f(fmaf(s[i], a.scale, -lse) * kLog2e);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const int j = base + 8 * (i >> 2) + 4 * half + (i & 3);
+        const float t = scored ? ruled_score(a, s[i], r.slope, r.p - j) - lse : fmaf(s[i], a.scale, -lse);
+        acc[i] += sees<RULES>(r, pre, j) ? __builtin_amdgcn_exp2f(t * kLog2e) : 0.f;
+    }
+}
+
+// The lanes' sums meet: key k of the wave's 32 for lanes 0 .. 31; `red`: the wave's own kilobytes.
+__device__ __forceinline__ float meet_lanes(const f32x16 &acc, float (&red)[16][64])
+{
+    const int lane = threadIdx.x & 63, k = lane & 31, from = (k >> 3) * 4 + (k & 3), half = (k >> 2) & 1;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) red[i][lane] = acc[i];
+    __syncthreads();
+    float sum = 0.f;
+#pragma unroll
+    for (int x = 0; x < 32; ++x) sum += red[from][half * 32 + ((x + k) & 31)];   // (turned by k: every lane its own bank)
+    return sum;
+}
+__device__ __forceinline__ void store_mass(const AttnArgs &a, const MassOut &to, int seq, int total, int kvh, int block, int split, int key, float sum)
+{
+    if (a.part) a.part[(((size_t)block * a.n_kv_heads + kvh) * a.n_splits + split) * kMassKeys + key % kMassKeys] = sum;
+    else if (key < total) to.mass[seq][(size_t)kvh * to.ld + key] += sum;
+}
+
+template <int DH, int TERMS, bool RULES>
+__global__ __launch_bounds__(256, TERMS == 1 ? 2 : 1) void cache_mass_kernel(const AttnArgs a, const MassOut to)
+{
+    constexpr int NKS = DH / 16, UNITS = NKS * 64 / 256;   // pieces of eight dims of a row tile per thread
+    __shared__ union {
+        u32x4 q[2][TERMS][NKS][64];
+        float red[4][16][64];
+    } lds;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, m = lane & 31;
+    const int kvh = blockIdx.x % a.n_kv_heads, rest = blockIdx.x / a.n_kv_heads;
+    const int split = rest % a.n_splits, block = rest / a.n_splits, seq = seq_of_block(a, block);
+    const SeqView s = a.seq[seq];
+    const int kb = (block - s.block0) * kMassKeys, base = kb + 32 * wave, total = s.pos0 + s.n;
+    const int pre = RULES && a.prefix > 0 ? (a.prefix < total ? a.prefix : total) : 0;
+    const RowTiles tiles = row_tiles(kb, s.pos0, s.n, a.group, RULES ? a.window : 0, pre);
+    const int t0 = tiles.t0 + split * a.chunk, t1 = t0 + a.chunk < tiles.t1 ? t0 + a.chunk : tiles.t1;
+    if (t0 >= tiles.t1) return;   // (the whole block)
+
+    u32x4 kf[NKS];
+    {
+        const int last_page = (total - 1) >> 4, page = (base >> 4) + ((lane >> 4) & 1);
+        const int id = s.table[page < last_page ? page : last_page];
+        const bf16_t *pool = (const bf16_t *)s.pool + kvf_base(id, a.layer, a.n_layers, 0, kvh, a.n_kv_heads, DH);
+        const u32x4 *p = (const u32x4 *)pool + half * 16 + (lane & 15);
+#pragma unroll
+        for (int ks = 0; ks < NKS; ++ks) kf[ks] = p[(ks >> 1) * 64 + (ks & 1) * 32];
+    }
+    // what the next tile is made of: its rows' pieces, and every lane's row
+    u32x4 piece[UNITS][TERMS];
+    RowInfo r_next;
+    float lse_next = 0.f;
+    auto request = [&](int t) __attribute__((always_inline)) {
+        r_next = row_info<RULES>(a, s, kvh, t * kRowTile);
+        const size_t at = (size_t)r_next.row * a.ldq + (size_t)r_next.head * DH + 8 * half;
+#pragma unroll
+        for (int u = 0; u < UNITS; ++u) load_q8<TERMS>(a, at + 16 * (wave + 4 * u), piece[u]);
+        const float lse = a.lse[(size_t)r_next.row * a.n_heads + r_next.head];
+        lse_next = r_next.live && lse != -INFINITY ? lse : INFINITY;   // (no row, or one without keys: weights of 0)
+    };
+    auto put = [&](int buf) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < UNITS; ++u)
+#pragma unroll
+            for (int k = 0; k < TERMS; ++k) lds.q[buf][k][wave + 4 * u][lane] = piece[u][k];
+    };
+    f32x16 acc = {};
+    request(t0);
+    put(0);
+    for (int t = t0; t < t1; ++t) {
+        const int buf = (t - t0) & 1;
+        const RowInfo r = r_next;
+        const float lse = lse_next;
+        __syncthreads();
+        if (t + 1 < t1) request(t + 1);
+        if (base < total && any_seen<RULES>(r, pre, base)) {
+            f32x16 sc = {};
+#pragma unroll
+            for (int k = TERMS - 1; k >= 0; --k)
+#pragma unroll
+                for (int ks = 0; ks < NKS; ++ks) sc = mfma32(as_bf16(kf[ks]), as_bf16(lds.q[buf][k][ks][lane]), sc);
+            add_weights<RULES>(a, r, lse, pre, base, sc, acc);
+        }
+        if (t + 1 < t1) put(buf ^ 1);
+    }
+    __syncthreads();
+    const float sum = meet_lanes(acc, lds.red[wave]);
+    if (half == 0) store_mass(a, to, seq, total, kvh, block, split, base + m, sum);
+}
+
+// The same for caches in plain order (exact fp32 products).
+template <typename KT, int DH>
+__global__ __launch_bounds__(256, 1) void cache_mass_plain_kernel(const AttnArgs a, const MassOut to)
+{
+    constexpr int N8 = DH / 16, UNITS = N8 * 64 / 256;
+    __shared__ union {
+        f32x4 q[2][DH / 8][64];   // [four of the lane's half row][lane]
+        float red[4][16][64];
+    } lds;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, m = lane & 31;
+    const int kvh = blockIdx.x % a.n_kv_heads, rest = blockIdx.x / a.n_kv_heads;
+    const int split = rest % a.n_splits, block = rest / a.n_splits, seq = seq_of_block(a, block);
+    const SeqView s = a.seq[seq];
+    const int kb = (block - s.block0) * kMassKeys, base = kb + 32 * wave, total = s.pos0 + s.n, pt = a.page_tokens;
+    const int pre = a.prefix > 0 ? (a.prefix < total ? a.prefix : total) : 0;
+    const RowTiles tiles = row_tiles(kb, s.pos0, s.n, a.group, a.window, pre);
+    const int t0 = tiles.t0 + split * a.chunk, t1 = t0 + a.chunk < tiles.t1 ? t0 + a.chunk : tiles.t1;
+    if (t0 >= tiles.t1) return;   // (the whole block)
+    float k[DH / 2];
+    {
+        const int key = base + m < total ? base + m : total - 1;
+        load_half<DH>((const KT *)s.pool + kv_offset(s.table[key / pt], a.layer, a.n_layers, 0, kvh, a.n_kv_heads, key % pt, pt, DH) + half * (DH / 2), k);
+    }
+    float piece[UNITS][8];
+    RowInfo r_next;
+    float lse_next = 0.f;
+    auto request = [&](int t) __attribute__((always_inline)) {
+        r_next = row_info<true>(a, s, kvh, t * kRowTile);
+        const size_t at = (size_t)r_next.row * a.ldq + (size_t)r_next.head * DH + half * (DH / 2);
+#pragma unroll
+        for (int u = 0; u < UNITS; ++u) load_q8(a, at + 8 * (wave + 4 * u), piece[u]);
+        const float lse = a.lse[(size_t)r_next.row * a.n_heads + r_next.head];
+        lse_next = r_next.live && lse != -INFINITY ? lse : INFINITY;
+    };
+    auto put = [&](int buf) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < UNITS; ++u)
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+                lds.q[buf][2 * (wave + 4 * u) + e][lane] = (f32x4){piece[u][4 * e], piece[u][4 * e + 1], piece[u][4 * e + 2], piece[u][4 * e + 3]};
+    };
+    f32x16 acc = {};
+    request(t0);
+    put(0);
+    for (int t = t0; t < t1; ++t) {
+        const int buf = (t - t0) & 1;
+        const RowInfo r = r_next;
+        const float lse = lse_next;
+        __syncthreads();
+        if (t + 1 < t1) request(t + 1);
+        if (base < total && any_seen<true>(r, pre, base)) {
+            f32x16 sc = {};
+#pragma unroll
+            for (int i = 0; i < DH / 8; ++i) {
+                const f32x4 q = lds.q[buf][i][lane];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sc = mfma32f(k[4 * i + e], q[e], sc);
+            }
+            add_weights<true>(a, r, lse, pre, base, sc, acc);
+        }
+        if (t + 1 < t1) put(buf ^ 1);
+    }
+    __syncthreads();
+    const float sum = meet_lanes(acc, lds.red[wave]);
+    if (half == 0) store_mass(a, to, seq, total, kvh, block, split, base + m, sum);
+}
+
+// The parts of the rows meet, in their order.   grid: n_blocks * n_kv_heads
+__global__ __launch_bounds__(kMassKeys) void cache_mass_join_kernel(const AttnArgs a, const MassOut to)
+{
+    const int kvh = blockIdx.x % a.n_kv_heads, block = blockIdx.x / a.n_kv_heads, seq = seq_of_block(a, block);
+    const SeqView s = a.seq[seq];
+    const int kb = (block - s.block0) * kMassKeys, total = s.pos0 + s.n, key = kb + (int)threadIdx.x;
+    const int pre = a.prefix < total ? a.prefix : total;
+    const RowTiles tiles = row_tiles(kb, s.pos0, s.n, a.group, a.window, pre);
+    const int used = (tiles.t1 - tiles.t0 + a.chunk - 1) / a.chunk;
+    const float *from = a.part + ((size_t)block * a.n_kv_heads + kvh) * a.n_splits * kMassKeys + threadIdx.x;
+    float sum = 0.f;
+#pragma unroll 4
+    for (int k = 0; k < used; ++k) sum += from[(size_t)k * kMassKeys];
+    if (key < total && used > 0) to.mass[seq][(size_t)kvh * to.ld + key] += sum;
+}
+
+}  // namespace anpd

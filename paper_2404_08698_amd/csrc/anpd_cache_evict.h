@@ -1,0 +1,274 @@
+// Eviction from a cache: which positions stay, and their keys and values moved together, for gfx950.
+//
+// Per layer and key / value head the first `first` positions, the last `last` and, of those between, the ones with the largest mass
+// stay (equal ones: the lowest position), in their order: the positions of a head's slots differ from head to head.
+// A key that moves from position p to slot i can be turned by the difference, k' = R((i - p) theta) k, theta_n = base^(-2 n / dim), so
+// that it is the key of a token at position i.
+#pragma once
+#include "anpd_layout.h"
+
+namespace anpd {
+
+constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64;
+
+// Numbers as integers of the same order; NaN below all of them, -0 is 0.
+__device__ __forceinline__ uint32_t mass_rank(float x)
+{
+    if (x != x) return 0;
+    const uint32_t u = __float_as_uint(x + 0.0f);
+    return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+
+struct SelectArgs {
+    const float *mass;   // [layer][head][ld]
+    int32_t *kept;       // [layer][head][keep]
+    float *out_mass;     // [layer][head][ld_out] or NULL
+    int64_t ld, ld_out;
+    int32_t len, keep, first, last;
+};
+
+// Block = (layer, head).  The smallest rank that stays is found a byte at a time from the top (a histogram of the candidates'
+// next byte in LDS, whole numbers, so the order of the counts does not matter); then every wave counts what stays of its stretch of
+// positions, the counts are summed over the waves, and each wave writes its own.
+// grid: n_layers * n_kv_heads
+__global__ __launch_bounds__(kSelectThreads) void cache_select_kernel(const SelectArgs a)
+{
+    __shared__ uint32_t bins[256], above[kSelectWaves], equal[kSelectWaves], choice[2];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const float *mass = a.mass + (size_t)blockIdx.x * a.ld;
+    int32_t *kept = a.kept + (size_t)blockIdx.x * a.keep;
+    float *out = a.out_mass ? a.out_mass + (size_t)blockIdx.x * a.ld_out : nullptr;
+    const int lo = a.first, hi = a.len - a.last;
+    const uint32_t want = (uint32_t)(a.keep - a.first - a.last);   // of the positions lo .. hi - 1
+    uint32_t limit = 0, left = want;   // ranks above `limit` stay, and `left` of those equal to it
+    if (want > 0) {
+        for (int shift = 24; shift >= 0; shift -= 8) {
+            for (int i = tid; i < 256; i += kSelectThreads) bins[i] = 0;
+            __syncthreads();
+            const uint32_t mask = shift == 24 ? 0u : ~0u << (shift + 8);
+            for (int i0 = lo + wave * 64; i0 < hi; i0 += kSelectThreads) {
+                const int i = i0 + lane;
+                const uint32_t rank = i < hi ? mass_rank(mass[i]) : 0;
+                const bool in = i < hi && (rank & mask) == limit;
+                const uint32_t bin = (rank >> shift) & 255u;
+                // (the first candidate's bin at once for all lanes that share it: positions that nothing looked at are all 0)
+                const unsigned long long some = __builtin_amdgcn_ballot_w64(in);
+                if (some == 0) continue;
+                const uint32_t one = (uint32_t)__builtin_amdgcn_readlane((int)bin, __builtin_ctzll(some));
+                const unsigned long long same = __builtin_amdgcn_ballot_w64(in && bin == one);
+                if (lane == 0) atomicAdd(&bins[one], (uint32_t)__builtin_popcountll(same));
+                if (in && bin != one) atomicAdd(&bins[bin], 1u);
+            }
+            __syncthreads();
+            if (wave == 0) {
+                // from the top bin down: the one in which the `left`th candidate lies.  Lane: four bins, the highest first.
+                uint32_t n[4], sum = 0;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) { n[k] = bins[255 - 4 * lane - k]; sum += n[k]; }
+                uint32_t before = sum;
+#pragma unroll
+                for (int o = 1; o < 64; o <<= 1) { const uint32_t t = (uint32_t)__shfl_up((int)before, o, 64); if (lane >= o) before += t; }
+                before -= sum;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    if (before < left && left <= before + n[k]) { choice[0] = 255 - 4 * lane - k; choice[1] = left - before; }
+                    before += n[k];
+                }
+            }
+            __syncthreads();
+            limit |= choice[0] << shift;
+            left = choice[1];
+        }
+    }
+    // stretches of whole 64s
+    const int each = ((a.len + kSelectWaves - 1) / kSelectWaves + 63) / 64 * 64, p0 = wave * each, p1 = p0 + each < a.len ? p0 + each : a.len;
+    auto look = [&](int i, bool &gt, bool &eq, float &x) __attribute__((always_inline)) {
+        const bool in = i < p1;
+        x = in ? mass[i] : 0.f;
+        const bool middle = in && i >= lo && i < hi;
+        const uint32_t rank = mass_rank(x);
+        gt = (in && !middle) || (middle && want > 0 && rank > limit);
+        eq = middle && want > 0 && rank == limit;
+    };
+    uint32_t n_gt = 0, n_eq = 0;
+    for (int i0 = p0; i0 < p1; i0 += 64) {
+        bool gt, eq;
+        float x;
+        look(i0 + lane, gt, eq, x);
+        n_gt += (uint32_t)__builtin_popcountll(__builtin_amdgcn_ballot_w64(gt));
+        n_eq += (uint32_t)__builtin_popcountll(__builtin_amdgcn_ballot_w64(eq));
+    }
+    if (lane == 0) { above[wave] = n_gt; equal[wave] = n_eq; }
+    __syncthreads();
+    uint32_t at = 0, ties = 0;
+    for (int w = 0; w < wave; ++w) { at += above[w]; ties += equal[w]; }
+    at += ties < left ? ties : left;
+    const unsigned long long below = (1ull << lane) - 1;
+    for (int i0 = p0; i0 < p1; i0 += 64) {
+        bool gt, eq;
+        float x;
+        look(i0 + lane, gt, eq, x);
+        const unsigned long long e = __builtin_amdgcn_ballot_w64(eq);
+        const bool stays = gt || (eq && ties + (uint32_t)__builtin_popcountll(e & below) < left);
+        const unsigned long long g = __builtin_amdgcn_ballot_w64(stays);
+        if (stays) {
+            const uint32_t to = at + (uint32_t)__builtin_popcountll(g & below);
+            kept[to] = i0 + lane;
+            if (out) out[to] = x;
+        }
+        at += (uint32_t)__builtin_popcountll(g);
+        ties += (uint32_t)__builtin_popcountll(e);
+    }
+}
+
+struct MoveArgs {
+    const void *src;
+    void *dst;
+    const int32_t *src_table, *dst_table, *kept;
+    double turn[64];    // theta / (2 pi) of every rotary pair
+    int32_t rotate, keep, n_layers, n_kv_heads, page_tokens;
+};
+
+constexpr int kMoveThreads = 512, kMovePages = 8;   // pages of 16 tokens at a time
+
+// cos and sin of the turn by `moved` positions, the angle reduced in 64 bits
+__device__ __forceinline__ void turn_of(const MoveArgs &a, int moved, int pair, float &c, float &s)
+{
+    const double t = (double)moved * a.turn[pair];
+    sincospif((float)(2.0 * (t - rint(t))), &s, &c);
+}
+
+// The cache in matrix-core order.  Block = (layer, head; keys or values; every gridDim.z-th group of eight pages): all that goes into the
+// group is read before any of it is written, and a position never moves up, so a cache may be moved into itself with one block
+// per layer, head and kind (gridDim.z = 1).   grid: (n_layers * n_kv_heads, 2, groups)
+template <int DH>
+__global__ __launch_bounds__(kMoveThreads) void cache_move_kernel(const MoveArgs a)
+{
+    const int tid = threadIdx.x, layer = blockIdx.x / a.n_kv_heads, head = blockIdx.x - layer * a.n_kv_heads, kind = blockIdx.y;
+    const int32_t *kept = a.kept + (size_t)blockIdx.x * a.keep;
+    const int pages = (a.keep + 15) / 16;
+    const bf16_t *src = (const bf16_t *)a.src;
+    bf16_t *dst = (bf16_t *)a.dst;
+    __shared__ int pos[kMovePages * 16], page[kMovePages * 16];
+    for (int g = blockIdx.z; g * kMovePages < pages; g += gridDim.z) {
+        const int first = g * kMovePages * 16;
+        if (tid < kMovePages * 16) {
+            const int i = first + tid;
+            pos[tid] = i < a.keep ? kept[i] : -1;
+            page[tid] = i < a.keep ? a.src_table[kept[i] >> 4] : 0;
+        }
+        __syncthreads();
+        if (kind == 0) {
+            // 16 bytes of a key and the 16 that they turn with
+            constexpr int PAIRS = DH / 16, STEPS = kMovePages * 16 * PAIRS / kMoveThreads;
+            uint4 lo[STEPS], hi[STEPS];
+#pragma unroll
+            for (int u = 0; u < STEPS; ++u) {
+                const int x = u * kMoveThreads + tid, t = x & 15, c = (x >> 4) % PAIRS, slot = (x >> 4) / PAIRS * 16 + t, p = pos[slot];
+                lo[u] = hi[u] = make_uint4(0, 0, 0, 0);
+                if (p < 0) continue;
+                const bf16_t *from = src + kvf_base(page[slot], layer, a.n_layers, 0, head, a.n_kv_heads, DH);
+                lo[u] = *(const uint4 *)(from + kf_elem(p & 15, 8 * c));
+                hi[u] = *(const uint4 *)(from + kf_elem(p & 15, 8 * c + DH / 2));
+            }
+            __syncthreads();
+#pragma unroll
+            for (int u = 0; u < STEPS; ++u) {
+                const int x = u * kMoveThreads + tid, t = x & 15, c = (x >> 4) % PAIRS, slot = (x >> 4) / PAIRS * 16 + t, p = pos[slot];
+                if (p < 0) continue;
+                const int to = first + slot;
+                if (a.rotate && p != to) {
+                    uint32_t *l = &lo[u].x, *h = &hi[u].x;
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) {
+                        float r[2][2];
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const float x0 = e ? __uint_as_float(l[w] & 0xffff0000u) : __uint_as_float(l[w] << 16);
+                            const float x1 = e ? __uint_as_float(h[w] & 0xffff0000u) : __uint_as_float(h[w] << 16);
+                            float cs, sn;
+                            turn_of(a, to - p, 8 * c + 2 * w + e, cs, sn);
+                            r[0][e] = x0 * cs - x1 * sn;   // (the cache's own type is what there is room for)
+                            r[1][e] = x1 * cs + x0 * sn;
+                        }
+                        l[w] = pack_bf16(r[0][0], r[0][1]);
+                        h[w] = pack_bf16(r[1][0], r[1][1]);
+                    }
+                }
+                bf16_t *put = dst + kvf_base(a.dst_table[to >> 4], layer, a.n_layers, 0, head, a.n_kv_heads, DH);
+                *(uint4 *)(put + kf_elem(to & 15, 8 * c)) = lo[u];
+                *(uint4 *)(put + kf_elem(to & 15, 8 * c + DH / 2)) = hi[u];
+            }
+        } else {
+            // one dim of four tokens
+            constexpr int UNITS = DH * 4, STEPS = kMovePages * UNITS / kMoveThreads;
+            bf16_t v[STEPS][4];
+#pragma unroll
+            for (int u = 0; u < STEPS; ++u) {
+                const int x = u * kMoveThreads + tid, dim = (x & 15) + 16 * ((x >> 6) % (DH / 16)), slot = x / UNITS * 16 + ((x >> 4) & 3) * 4;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int p = pos[slot + e];
+                    v[u][e] = p < 0 ? 0 : src[kvf_base(page[slot + e], layer, a.n_layers, 1, head, a.n_kv_heads, DH) + vf_elem(p & 15, dim)];
+                }
+            }
+            __syncthreads();
+#pragma unroll
+            for (int u = 0; u < STEPS; ++u) {
+                const int x = u * kMoveThreads + tid, dim = (x & 15) + 16 * ((x >> 6) % (DH / 16)), slot = x / UNITS * 16 + ((x >> 4) & 3) * 4;
+                if (pos[slot] < 0) continue;
+                const int to = first + slot;
+                bf16_t *put = dst + kvf_base(a.dst_table[to >> 4], layer, a.n_layers, 1, head, a.n_kv_heads, DH) + vf_elem(to & 15, dim);
+                *(uint2 *)put = make_uint2((uint32_t)v[u][0] | ((uint32_t)v[u][1] << 16), (uint32_t)v[u][2] | ((uint32_t)v[u][3] << 16));
+            }
+        }
+        __syncthreads();   // (the list is about to be replaced)
+    }
+}
+
+// Caches in plain order: rows of [dim], whatever the page size.   grid: as above
+template <typename KT, int DH>
+__global__ __launch_bounds__(kMoveThreads) void cache_move_plain_kernel(const MoveArgs a)
+{
+    constexpr int PAIRS = DH / 2, TOKENS = kMovePages * 16, STEPS = TOKENS * PAIRS / kMoveThreads;
+    const int tid = threadIdx.x, layer = blockIdx.x / a.n_kv_heads, head = blockIdx.x - layer * a.n_kv_heads, kind = blockIdx.y, pt = a.page_tokens;
+    const int32_t *kept = a.kept + (size_t)blockIdx.x * a.keep;
+    const KT *src = (const KT *)a.src;
+    KT *dst = (KT *)a.dst;
+    __shared__ int pos[TOKENS];
+    for (int g = blockIdx.z; g * TOKENS < a.keep; g += gridDim.z) {
+        const int first = g * TOKENS;
+        if (tid < TOKENS) pos[tid] = first + tid < a.keep ? kept[first + tid] : -1;
+        __syncthreads();
+        KT lo[STEPS], hi[STEPS];
+#pragma unroll
+        for (int u = 0; u < STEPS; ++u) {
+            const int x = u * kMoveThreads + tid, i = x % PAIRS, p = pos[x / PAIRS];
+            lo[u] = hi[u] = KT(0);
+            if (p < 0) continue;
+            const KT *from = src + kv_offset(a.src_table[p / pt], layer, a.n_layers, kind, head, a.n_kv_heads, p % pt, pt, DH);
+            lo[u] = from[i];
+            hi[u] = from[i + PAIRS];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < STEPS; ++u) {
+            const int x = u * kMoveThreads + tid, i = x % PAIRS, p = pos[x / PAIRS], to = first + x / PAIRS;
+            if (p < 0) continue;
+            KT *put = dst + kv_offset(a.dst_table[to / pt], layer, a.n_layers, kind, head, a.n_kv_heads, to % pt, pt, DH);
+            if (kind == 0 && a.rotate && p != to) {
+                float cs, sn;
+                turn_of(a, to - p, i, cs, sn);
+                const float x0 = load_f32(&lo[u], 0), x1 = load_f32(&hi[u], 0);
+                store_kv(put, i, x0 * cs - x1 * sn);
+                store_kv(put, i + PAIRS, x1 * cs + x0 * sn);
+            } else {
+                put[i] = lo[u];
+                put[i + PAIRS] = hi[u];
+            }
+        }
+        __syncthreads();
+    }
+}
+
+}  // namespace anpd

@@ -15,6 +15,7 @@
 #include <new>
 #include <vector>
 
+#include "anpd_cache.h"
 #include "anpd_common.h"
 #include "anpd_kernels.h"
 #include "anpd_fast.h"
@@ -24,15 +25,7 @@
 
 using namespace anpd;
 
-#define HIP_TRY(expr)                                                                             \
-    do {                                                                                          \
-        hipError_t e_ = (expr);                                                                   \
-        if (e_ != hipSuccess) return fail(ANPD_E_HIP, "%s: %s", #expr, hipGetErrorString(e_));    \
-    } while (0)
-
 namespace {
-
-size_t align_up(size_t x, size_t a = 256) { return (x + a - 1) / a * a; }
 
 int kv_heads_of(const anpd_model_cfg &c) { return c.n_kv_heads > 0 ? c.n_kv_heads : c.n_heads; }
 int kv_dim_of(const anpd_model_cfg &c) { return kv_heads_of(c) * c.head_dim; }
@@ -250,24 +243,99 @@ struct anpd_model {
     int64_t prof_steps;
 };
 
-struct anpd_kv {
-    const anpd_model *m;
-    char *pool;
-    int32_t n_pages, max_tokens, len;
-    size_t page_bytes;
-    std::vector<int32_t> table;      // logical -> physical, -1 = none
-    std::vector<int32_t> dev_table;  // what the device copy currently holds
-    std::vector<int32_t> free_list;  // physical pages, handed out from the back
-    int32_t *d_table, *d_len;
-    int32_t *pin;                    // pinned staging: [0] length, [1..] table
-    bool table_dirty;
-};
+namespace anpd {
+
+// ---- cache pages ---------------------------------------------------------------
+
+// Make sure logical pages covering positions [0, upto) exist; refresh the device table if needed.
+int32_t ensure_pages(anpd_kv *kv, int32_t upto, hipStream_t st)
+{
+    const int pt = kv->shape.page_tokens;
+    const int need = (upto + pt - 1) / pt;
+    for (int lp = 0; lp < need; ++lp) {
+        if (kv->table[(size_t)lp] >= 0) continue;
+        if (kv->free_list.empty()) return fail(ANPD_E_CAPACITY, "KV pool has no free page");
+        kv->table[(size_t)lp] = kv->free_list.back();
+        kv->free_list.pop_back();
+        if (kv->table[(size_t)lp] != kv->dev_table[(size_t)lp]) kv->table_dirty = true;
+    }
+    if (kv->table_dirty) {
+        // the staging buffer is free: every call that uses it synchronises before returning
+        for (size_t i = 0; i < kv->table.size(); ++i) {
+            if (kv->table[i] >= 0) kv->dev_table[i] = kv->table[i];
+            kv->pin[1 + i] = kv->dev_table[i] < 0 ? 0 : kv->dev_table[i];
+        }
+        HIP_TRY(hipMemcpyAsync(kv->d_table, kv->pin + 1, kv->table.size() * sizeof(int32_t), hipMemcpyHostToDevice, st));
+        kv->table_dirty = false;
+    }
+    return ANPD_OK;
+}
+
+// Return pages wholly beyond `len` to the free list.
+void release_pages(anpd_kv *kv, int32_t len)
+{
+    const int pt = kv->shape.page_tokens;
+    const int keep = (len + pt - 1) / pt;
+    for (int lp = (int)kv->table.size() - 1; lp >= keep; --lp) {
+        if (kv->table[(size_t)lp] >= 0) {
+            kv->free_list.push_back(kv->table[(size_t)lp]);
+            kv->table[(size_t)lp] = -1;
+        }
+    }
+}
+
+// The cache itself, for a model and for programs whose layers are their own.
+int32_t make_cache(const char *who, const anpd_model *m, const CacheShape &shape, void *pool, size_t pool_bytes, int32_t max_tokens, anpd_kv **out)
+{
+    if (((uintptr_t)pool & 255) != 0) return fail(ANPD_E_INVAL, "%s: pool must be 256-byte aligned", who);
+    const size_t need = shape.pool_bytes(max_tokens);
+    if (pool_bytes < need) return fail(ANPD_E_CAPACITY, "%s: pool has %zu bytes, %zu needed", who, pool_bytes, need);
+    anpd_kv *kv = new (std::nothrow) anpd_kv;
+    if (!kv) return fail(ANPD_E_NOMEM, "%s: out of memory", who);
+    kv->m = m;
+    kv->shape = shape;
+    int dev = 0;
+    if (hipGetDevice(&dev) != hipSuccess) (void)hipGetLastError();
+    hipPointerAttribute_t at;
+    kv->device = dev;
+    if (hipPointerGetAttributes(&at, pool) == hipSuccess) kv->device = at.device;
+    else (void)hipGetLastError();
+    kv->n_cu = 256;
+    if (hipDeviceGetAttribute(&kv->n_cu, hipDeviceAttributeMultiprocessorCount, kv->device) != hipSuccess) (void)hipGetLastError();
+    kv->pool = (char *)pool;
+    kv->n_pages = (max_tokens + shape.page_tokens - 1) / shape.page_tokens;
+    kv->max_tokens = max_tokens;
+    kv->len = 0;
+    kv->table.assign((size_t)kv->n_pages, -1);
+    kv->dev_table.assign((size_t)kv->n_pages, -1);
+    for (int p = kv->n_pages - 1; p >= 0; --p) kv->free_list.push_back(p);  // page 0 is handed out first
+    char *tail = kv->pool + align_up((size_t)kv->n_pages * shape.page_bytes());
+    kv->d_len = (int32_t *)tail;
+    kv->d_table = kv->d_len + 1;
+    kv->table_dirty = true;
+    kv->pin = nullptr;
+    hipError_t e = hipHostMalloc((void **)&kv->pin, ((size_t)kv->n_pages + 1) * sizeof(int32_t), hipHostMallocDefault);
+    if (e == hipSuccess) e = hipMemset(kv->pool, 0, need);  // unwritten slots must read as zeros, never as NaN patterns
+    if (e == hipSuccess) {
+        kv->pin[0] = 0;
+        e = hipMemcpy(kv->d_len, kv->pin, sizeof(int32_t), hipMemcpyHostToDevice);
+    }
+    if (e != hipSuccess) {
+        if (kv->pin) (void)hipHostFree(kv->pin);
+        delete kv;
+        return fail(ANPD_E_HIP, "%s: %s", who, hipGetErrorString(e));
+    }
+    *out = kv;
+    return ANPD_OK;
+}
+
+}  // namespace anpd
 
 namespace {
 
-size_t page_bytes_of(const anpd_model_cfg &c)
+CacheShape cache_shape(const anpd_model_cfg &c)
 {
-    return (size_t)c.n_layers * 2 * kv_dim_of(c) * c.page_tokens * (c.dtype == ANPD_BF16 ? 2 : 4);
+    return {c.n_layers, c.n_heads, kv_heads_of(c), c.head_dim, c.dtype, c.page_tokens, wants_mfma(&c)};
 }
 
 // ---- GEMM dispatch -----------------------------------------------------------
@@ -423,45 +491,6 @@ int32_t launch_pack(const void *s0, const void *s1, const void *s2, void *dst, i
                        (const bf16_t *)s1, (const bf16_t *)s2, (uint4 *)dst, mode, n_tiles, K, nks, d, head_dim, kvd);
     HIP_TRY(hipGetLastError());
     return ANPD_OK;
-}
-
-// ---- cache pages ---------------------------------------------------------------
-
-// Make sure logical pages covering positions [0, upto) exist; refresh the device table if needed.
-int32_t ensure_pages(anpd_kv *kv, int32_t upto, hipStream_t st)
-{
-    const int pt = kv->m->cfg.page_tokens;
-    const int need = (upto + pt - 1) / pt;
-    for (int lp = 0; lp < need; ++lp) {
-        if (kv->table[(size_t)lp] >= 0) continue;
-        if (kv->free_list.empty()) return fail(ANPD_E_CAPACITY, "KV pool has no free page");
-        kv->table[(size_t)lp] = kv->free_list.back();
-        kv->free_list.pop_back();
-        if (kv->table[(size_t)lp] != kv->dev_table[(size_t)lp]) kv->table_dirty = true;
-    }
-    if (kv->table_dirty) {
-        // the staging buffer is free: every call that uses it synchronises before returning
-        for (size_t i = 0; i < kv->table.size(); ++i) {
-            if (kv->table[i] >= 0) kv->dev_table[i] = kv->table[i];
-            kv->pin[1 + i] = kv->dev_table[i] < 0 ? 0 : kv->dev_table[i];
-        }
-        HIP_TRY(hipMemcpyAsync(kv->d_table, kv->pin + 1, kv->table.size() * sizeof(int32_t), hipMemcpyHostToDevice, st));
-        kv->table_dirty = false;
-    }
-    return ANPD_OK;
-}
-
-// Return pages wholly beyond `len` to the free list.
-void release_pages(anpd_kv *kv, int32_t len)
-{
-    const int pt = kv->m->cfg.page_tokens;
-    const int keep = (len + pt - 1) / pt;
-    for (int lp = (int)kv->table.size() - 1; lp >= keep; --lp) {
-        if (kv->table[(size_t)lp] >= 0) {
-            kv->free_list.push_back(kv->table[(size_t)lp]);
-            kv->table[(size_t)lp] = -1;
-        }
-    }
 }
 
 // Timing mark: an event after the launches of category `cat` (-1 = start of the step).
@@ -1634,9 +1663,7 @@ size_t anpd_kv_pool_bytes(const anpd_model_t *m, int32_t max_tokens)
         fail(ANPD_E_INVAL, "anpd_kv_pool_bytes: bad argument");
         return 0;
     }
-    const int pt = m->cfg.page_tokens;
-    size_t pages = (size_t)(max_tokens + pt - 1) / pt;
-    return align_up(pages * page_bytes_of(m->cfg)) + align_up((pages + 1) * sizeof(int32_t));
+    return cache_shape(m->cfg).pool_bytes(max_tokens);
 }
 
 int32_t anpd_kv_create(const anpd_model_t *m, void *pool, size_t pool_bytes, int32_t max_tokens, anpd_kv_t **out)
@@ -1646,39 +1673,7 @@ int32_t anpd_kv_create(const anpd_model_t *m, void *pool, size_t pool_bytes, int
     if (!m || !pool) return fail(ANPD_E_INVAL, "anpd_kv_create: NULL model or pool");
     if (max_tokens < 1 || max_tokens > m->cfg.max_positions)
         return fail(ANPD_E_CAPACITY, "anpd_kv_create: max_tokens %d outside 1..max_positions (%d)", max_tokens, m->cfg.max_positions);
-    if (((uintptr_t)pool & 255) != 0) return fail(ANPD_E_INVAL, "anpd_kv_create: pool must be 256-byte aligned");
-    size_t need = anpd_kv_pool_bytes(m, max_tokens);
-    if (pool_bytes < need) return fail(ANPD_E_CAPACITY, "anpd_kv_create: pool has %zu bytes, %zu needed", pool_bytes, need);
-    anpd_kv *kv = new (std::nothrow) anpd_kv;
-    if (!kv) return fail(ANPD_E_NOMEM, "anpd_kv_create: out of memory");
-    const int pt = m->cfg.page_tokens;
-    kv->m = m;
-    kv->pool = (char *)pool;
-    kv->n_pages = (max_tokens + pt - 1) / pt;
-    kv->max_tokens = max_tokens;
-    kv->len = 0;
-    kv->page_bytes = page_bytes_of(m->cfg);
-    kv->table.assign((size_t)kv->n_pages, -1);
-    kv->dev_table.assign((size_t)kv->n_pages, -1);
-    for (int p = kv->n_pages - 1; p >= 0; --p) kv->free_list.push_back(p);  // page 0 is handed out first
-    char *tail = kv->pool + align_up((size_t)kv->n_pages * kv->page_bytes);
-    kv->d_len = (int32_t *)tail;
-    kv->d_table = kv->d_len + 1;
-    kv->table_dirty = true;
-    kv->pin = nullptr;
-    hipError_t e = hipHostMalloc((void **)&kv->pin, ((size_t)kv->n_pages + 1) * sizeof(int32_t), hipHostMallocDefault);
-    if (e == hipSuccess) e = hipMemset(kv->pool, 0, need);  // unwritten slots must read as zeros, never as NaN patterns
-    if (e == hipSuccess) {
-        kv->pin[0] = 0;
-        e = hipMemcpy(kv->d_len, kv->pin, sizeof(int32_t), hipMemcpyHostToDevice);
-    }
-    if (e != hipSuccess) {
-        if (kv->pin) (void)hipHostFree(kv->pin);
-        delete kv;
-        return fail(ANPD_E_HIP, "anpd_kv_create: %s", hipGetErrorString(e));
-    }
-    *out = kv;
-    return ANPD_OK;
+    return make_cache("anpd_kv_create", m, cache_shape(m->cfg), pool, pool_bytes, max_tokens, out);
 }
 
 void anpd_kv_destroy(anpd_kv_t *kv)
@@ -1726,7 +1721,7 @@ int32_t anpd_kv_truncate(anpd_kv_t *kv, int32_t new_len, void *stream)
 static int32_t kv_copy(anpd_kv *kv, int32_t layer, int32_t pos0, int32_t n, float *k, float *v, bool to_cache, void *stream)
 {
     if (!kv || ((!k || !v) && n != 0)) return fail(ANPD_E_INVAL, "anpd_kv_read/write: NULL argument");
-    const anpd_model_cfg &c = kv->m->cfg;
+    const CacheShape &c = kv->shape;
     if (layer < 0 || layer >= c.n_layers || pos0 < 0 || n < 0 || pos0 + n > kv->max_tokens)
         return fail(ANPD_E_CAPACITY, "anpd_kv_read/write: layer %d, positions %d..%d out of range", layer, pos0, pos0 + n);
     if (n == 0) return ANPD_OK;
@@ -1741,14 +1736,14 @@ static int32_t kv_copy(anpd_kv *kv, int32_t layer, int32_t pos0, int32_t n, floa
     }
 #define KV_COPY(KT, TO)                                                                                          \
     hipLaunchKernelGGL((kv_copy_kernel<KT, TO>), dim3(n), dim3(256), 0, st, (KT *)kv->pool, kv->d_table, k, v, pos0, \
-                       layer, c.n_layers, kv_heads_of(c), c.head_dim, c.page_tokens)
-    if (kv->m->mfma) {
+                       layer, c.n_layers, c.n_kv_heads, c.head_dim, c.page_tokens)
+    if (c.fragments) {
         if (to_cache)
             hipLaunchKernelGGL((kvf_copy_kernel<true>), dim3(n), dim3(256), 0, st, (bf16_t *)kv->pool, kv->d_table, k, v, pos0,
-                               layer, c.n_layers, kv_heads_of(c), c.head_dim);
+                               layer, c.n_layers, c.n_kv_heads, c.head_dim);
         else
             hipLaunchKernelGGL((kvf_copy_kernel<false>), dim3(n), dim3(256), 0, st, (bf16_t *)kv->pool, kv->d_table, k, v, pos0,
-                               layer, c.n_layers, kv_heads_of(c), c.head_dim);
+                               layer, c.n_layers, c.n_kv_heads, c.head_dim);
     } else if (c.dtype == ANPD_BF16) { if (to_cache) KV_COPY(bf16_t, true); else KV_COPY(bf16_t, false); }
     else { if (to_cache) KV_COPY(float, true); else KV_COPY(float, false); }
 #undef KV_COPY

@@ -49,27 +49,6 @@ __device__ __forceinline__ void xp_store4(bf16_t *xp, int cls, int m, int k, f32
     stc8<COH>(xp + xp_offset(cls, m, k, 1), pl);
 }
 
-// ------------------------------------------------------ fast-path KV cache
-//
-// The fast path keeps K and V in MFMA-fragment order inside each (page, layer,
-// k|v, head) block of 16 tokens x head_dim (page_tokens is 16 on this path):
-//   K: [dim / 32][lane = 16 * ((dim % 32) / 8) + token][dim % 8]     A operand of 16x16x32 (rows = keys)
-//   V: [dim / 16][lane = 16 * (token / 4) + dim % 16][token % 4]     A operand of 16x16x16 (rows = dims)
-// so a wave loads a page's K (and V) tile with fully coalesced reads.
-__host__ __device__ __forceinline__ size_t kvf_base(int page, int layer, int n_layers, int kv, int head, int n_heads,
-                                                    int head_dim)
-{
-    return ((((size_t)page * n_layers + layer) * 2 + kv) * n_heads + head) * ((size_t)16 * head_dim);
-}
-__host__ __device__ __forceinline__ size_t kf_elem(int tok, int dim)
-{
-    return ((size_t)(dim >> 5) * 64 + (size_t)((dim >> 3) & 3) * 16 + tok) * 8 + (dim & 7);
-}
-__host__ __device__ __forceinline__ size_t vf_elem(int tok, int dim)
-{
-    return ((size_t)(dim >> 4) * 64 + (size_t)(tok >> 2) * 16 + (dim & 15)) * 4 + (tok & 3);
-}
-
 // bf16-element offset of q (row m, head, dim, hi|lo) in the packed query operand
 // qp[head][m / 8][dim / 32][lane][8]: groups of 8 window rows in class-8 packing.
 __host__ __device__ __forceinline__ size_t qp_offset(int head, int head_dim, int m, int dim, int lo)

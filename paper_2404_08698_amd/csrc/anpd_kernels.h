@@ -15,32 +15,15 @@
 
 #include <type_traits>
 
-namespace anpd {
+#include "anpd_layout.h"
 
-typedef uint16_t bf16_t;  // bfloat16 storage
-typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
-typedef __attribute__((ext_vector_type(4))) float f32x4;
+namespace anpd {
 
 constexpr int kWave = 64;
 constexpr int kAttnSplit = 64;        // keys per attention split (fixed: part of the numerics)
 constexpr float kMasked = -1.0e30f;   // score of a key a row must not see
 
 // ---------------------------------------------------------------- scalars
-
-__device__ __forceinline__ float bf16_to_f32(bf16_t b) { return __uint_as_float((uint32_t)b << 16); }
-
-// round to nearest, ties to even (finite inputs)
-__device__ __forceinline__ bf16_t f32_to_bf16(float f)
-{
-    uint32_t u = __float_as_uint(f);
-    u += 0x7fffu + ((u >> 16) & 1u);
-    return (bf16_t)(u >> 16);
-}
-
-__device__ __forceinline__ float load_f32(const float *p, size_t i) { return p[i]; }
-__device__ __forceinline__ float load_f32(const bf16_t *p, size_t i) { return bf16_to_f32(p[i]); }
-__device__ __forceinline__ void store_kv(float *p, size_t i, float v) { p[i] = v; }
-__device__ __forceinline__ void store_kv(bf16_t *p, size_t i, float v) { p[i] = f32_to_bf16(v); }
 
 // eight consecutive elements, widened to float
 __device__ __forceinline__ void load8(const float *p, float (&o)[8])
@@ -272,14 +255,6 @@ struct UploadWords {
 __global__ __launch_bounds__(kUploadWords) void upload_kernel(uint32_t *__restrict__ dst, UploadWords words, int n)
 {
     if ((int)threadIdx.x < n) dst[threadIdx.x] = words.w[threadIdx.x];
-}
-
-// Page layout of the generic path: [page][layer][k|v][head][token in page][head_dim].
-__device__ __forceinline__ size_t kv_offset(int page, int layer, int n_layers, int kv, int head, int n_heads,
-                                            int tok_in_page, int page_tokens, int head_dim)
-{
-    return ((((size_t)page * n_layers + layer) * 2 + kv) * n_heads + head) * ((size_t)page_tokens * head_dim) +
-           (size_t)tok_in_page * head_dim;
 }
 
 // ------------------------------------------------------------------ embed

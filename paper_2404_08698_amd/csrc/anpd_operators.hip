@@ -1,0 +1,387 @@
+// Operators on caches: host half (arguments, how the work is divided, launches).  The kernels and their reasons are in
+// anpd_cache_attn.h and anpd_cache_evict.h.
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <cstring>
+
+#include "anpd_cache.h"
+#include "anpd_cache_attn.h"
+#include "anpd_cache_evict.h"
+
+using namespace anpd;
+
+namespace {
+
+// The caches' device is the current one while a call lasts.
+struct OnDevice {
+    int before = -1;
+    int32_t enter(const char *who, int device)
+    {
+        int cur = 0;
+        hipError_t e = hipGetDevice(&cur);
+        if (e == hipSuccess && cur != device) {
+            e = hipSetDevice(device);
+            if (e == hipSuccess) before = cur;
+        }
+        return e == hipSuccess ? ANPD_OK : fail(ANPD_E_HIP, "%s: %s", who, hipGetErrorString(e));
+    }
+    ~OnDevice()
+    {
+        if (before >= 0) (void)hipSetDevice(before);
+    }
+};
+
+bool same_shape(const CacheShape &a, const CacheShape &b)
+{
+    return a.n_layers == b.n_layers && a.n_heads == b.n_heads && a.n_kv_heads == b.n_kv_heads && a.head_dim == b.head_dim && a.dtype == b.dtype &&
+           a.page_tokens == b.page_tokens && a.fragments == b.fragments;
+}
+
+// What anpd_attention and anpd_key_mass have in common: the sequences and rules, checked, as the kernels take them.
+int32_t gather(const char *who, const anpd_kv *const *kvs, int32_t n_seq, const int32_t *n_rows, const int32_t *pos0, const anpd_attn_rules *rules,
+               AttnArgs &a, int64_t &rows)
+{
+    if (!kvs || !n_rows) return fail(ANPD_E_INVAL, "%s: NULL argument", who);
+    if (n_seq < 1 || n_seq > kAttnMaxSeqs) return fail(ANPD_E_INVAL, "%s: n_seq must be in 1..%d", who, kAttnMaxSeqs);
+    for (int s = 0; s < n_seq; ++s)
+        if (!kvs[s]) return fail(ANPD_E_INVAL, "%s: NULL cache", who);
+    const CacheShape &c = kvs[0]->shape;
+    std::memset(&a, 0, sizeof(a));
+    a.n_seq = n_seq;
+    a.n_layers = c.n_layers;
+    a.n_heads = c.n_heads;
+    a.n_kv_heads = c.n_kv_heads;
+    a.group = c.n_heads / c.n_kv_heads;
+    a.page_tokens = c.page_tokens;
+    a.scale = 1.0f / std::sqrt((float)c.head_dim);
+    rows = 0;
+    for (int s = 0; s < n_seq; ++s) {
+        const anpd_kv *kv = kvs[s];
+        if (!same_shape(kv->shape, c) || kv->device != kvs[0]->device) return fail(ANPD_E_INVAL, "%s: cache %d has another shape or device than the first", who, s);
+        const int32_t n = n_rows[s], at = pos0 ? pos0[s] : kv->len;
+        if (n < 0 || at < 0) return fail(ANPD_E_INVAL, "%s: sequence %d: %d rows from position %d on", who, s, n, at);
+        if ((int64_t)at + n > kv->max_tokens)
+            return fail(ANPD_E_CAPACITY, "%s: sequence %d: position %d + %d rows exceeds capacity %d", who, s, at, n, kv->max_tokens);
+        if (n > 0)
+            for (int lp = (at + n - 1) / c.page_tokens; lp >= 0; --lp)
+                if (kv->table[(size_t)lp] < 0) return fail(ANPD_E_INVAL, "%s: sequence %d: position %d has no page", who, s, lp * c.page_tokens);
+        if ((int64_t)n * a.group >= (1 << 30)) return fail(ANPD_E_CAPACITY, "%s: sequence %d has too many rows", who, s);
+        a.seq[s] = {kv->pool, kv->d_table, at, n, (int32_t)rows, 0};
+        rows += n;
+    }
+    if (rows >= (1 << 30)) return fail(ANPD_E_CAPACITY, "%s: too many rows", who);
+    if (rules) {
+        if (!(rules->scale >= 0.f) || !(rules->cap >= 0.f) || std::isinf(rules->scale) || std::isinf(rules->cap) || rules->window < 0 || rules->prefix < 0)
+            return fail(ANPD_E_INVAL, "%s: scale, cap, window and prefix must be finite and >= 0", who);
+        if (rules->scale > 0.f) a.scale = rules->scale;
+        a.cap = rules->cap;
+        a.window = rules->window;
+        a.prefix = rules->prefix;
+        a.slopes = rules->slopes;
+        a.first_key = rules->first_key;
+    }
+    return ANPD_OK;
+}
+
+bool ruled(const AttnArgs &a) { return a.cap > 0.f || a.slopes || a.window > 0 || a.prefix > 0 || a.first_key; }
+
+int32_t rows_in(const char *who, const CacheShape &c, int32_t layer, const void *q, int64_t ldq, int32_t dtype, AttnArgs &a)
+{
+    if (layer < 0 || layer >= c.n_layers) return fail(ANPD_E_INVAL, "%s: layer %d outside [0, %d)", who, layer, c.n_layers);
+    if (dtype != ANPD_F32 && dtype != ANPD_BF16) return fail(ANPD_E_INVAL, "%s: unknown dtype", who);
+    const int64_t width = (int64_t)c.n_heads * c.head_dim;
+    if (ldq < width) return fail(ANPD_E_INVAL, "%s: rows are %lld elements wide and %lld apart", who, (long long)width, (long long)ldq);
+    if (((uintptr_t)q & (dtype == ANPD_F32 ? 3 : 1)) != 0) return fail(ANPD_E_INVAL, "%s: rows are not aligned to their type", who);
+    a.layer = layer;
+    a.q = q;
+    a.ldq = ldq;
+    a.q_f32 = dtype == ANPD_F32;
+    a.q_wide = ((uintptr_t)q & 15) == 0 && ldq % (a.q_f32 ? 4 : 8) == 0;
+    return ANPD_OK;
+}
+
+// ---- attention: how the work is divided
+
+// Sets the row blocks of a's sequences, the splits and their size; returns the workspace that the splits need.
+size_t plan_attention(AttnArgs &a, const CacheShape &c, int n_cu)
+{
+    a.n_blocks = 0;
+    int most = 0;   // tiles of a row block
+    for (int s = 0; s < a.n_seq; ++s) {
+        SeqView &v = a.seq[s];
+        v.block0 = a.n_blocks;
+        if (v.n == 0) continue;
+        a.n_blocks += (int32_t)(((int64_t)v.n * a.group + kRowTile - 1) / kRowTile);
+        const int total = v.pos0 + v.n, pre = a.prefix < total ? a.prefix : total, pre_tiles = (pre + kStreamTile - 1) / kStreamTile;
+        const int all = (total - 1) / kStreamTile + 1;
+        int64_t tiles = all > pre_tiles ? all : pre_tiles;
+        if (a.window > 0) {
+            const int64_t some = pre_tiles + ((int64_t)a.window + kRowTile / a.group + 1) / kStreamTile + 2;
+            if (some < tiles) tiles = some;
+        }
+        if (tiles > most) most = (int)tiles;
+    }
+    const int64_t items = (int64_t)a.n_blocks * a.n_kv_heads;
+    int64_t splits = items > 0 ? (2 * n_cu + items - 1) / items : 1;
+    if (splits > most / 2) splits = most / 2;
+    if (splits < 1) splits = 1;
+    a.chunk = most > 0 ? (int)((most + splits - 1) / splits) : 1;
+    a.n_splits = most > 0 ? (most + a.chunk - 1) / a.chunk : 1;
+    return a.n_splits > 1 ? align_up((size_t)items * a.n_splits * part_floats(kRowTile, c.head_dim) * sizeof(float)) : 0;
+}
+
+template <int DH>
+int32_t launch_attention(const AttnArgs &a, const CacheShape &c, hipStream_t st)
+{
+    const dim3 grid((unsigned)((int64_t)a.n_blocks * a.n_splits * a.n_kv_heads)), block(256);
+    const bool rules = ruled(a);
+    if (c.fragments) {
+        if (a.q_f32) {
+            if (rules) hipLaunchKernelGGL((cache_attn_stream_kernel<DH, 3, true>), grid, block, 0, st, a);
+            else hipLaunchKernelGGL((cache_attn_stream_kernel<DH, 3, false>), grid, block, 0, st, a);
+        } else if (rules) hipLaunchKernelGGL((cache_attn_stream_kernel<DH, 1, true>), grid, block, 0, st, a);
+        else hipLaunchKernelGGL((cache_attn_stream_kernel<DH, 1, false>), grid, block, 0, st, a);
+    } else if (c.dtype == ANPD_BF16) hipLaunchKernelGGL((cache_attn_plain_kernel<bf16_t, DH>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((cache_attn_plain_kernel<float, DH>), grid, block, 0, st, a);
+    HIP_TRY(hipGetLastError());
+    if (a.part) {
+        hipLaunchKernelGGL((cache_attn_join_kernel<DH>), dim3((unsigned)((int64_t)a.n_blocks * a.n_kv_heads)), block, 0, st, a);
+        HIP_TRY(hipGetLastError());
+    }
+    return ANPD_OK;
+}
+
+// ---- key mass: how the work is divided
+
+size_t plan_mass(AttnArgs &a, int n_cu)
+{
+    a.n_blocks = 0;
+    int most = 0;   // row tiles of a block of keys
+    for (int s = 0; s < a.n_seq; ++s) {
+        SeqView &v = a.seq[s];
+        v.block0 = a.n_blocks;
+        if (v.n == 0) continue;
+        const int total = v.pos0 + v.n, pre = a.prefix < total ? a.prefix : total, blocks = (total + kMassKeys - 1) / kMassKeys;
+        a.n_blocks += blocks;
+        for (int b = 0; b < blocks; ++b) {
+            const RowTiles t = row_tiles(b * kMassKeys, v.pos0, v.n, a.group, a.window, pre);
+            if (t.t1 - t.t0 > most) most = t.t1 - t.t0;
+        }
+    }
+    const int64_t items = (int64_t)a.n_blocks * a.n_kv_heads;
+    int64_t splits = items > 0 ? (2 * n_cu + items - 1) / items : 1;
+    if (splits > most / 4) splits = most / 4;
+    if (splits < 1) splits = 1;
+    a.chunk = most > 0 ? (int)((most + splits - 1) / splits) : 1;
+    a.n_splits = most > 0 ? (most + a.chunk - 1) / a.chunk : 1;
+    return a.n_splits > 1 ? align_up((size_t)items * a.n_splits * kMassKeys * sizeof(float)) : 0;
+}
+
+template <int DH>
+int32_t launch_mass(const AttnArgs &a, const MassOut &to, const CacheShape &c, hipStream_t st)
+{
+    const dim3 grid((unsigned)((int64_t)a.n_blocks * a.n_splits * a.n_kv_heads));
+    const bool rules = ruled(a);
+    if (c.fragments) {
+        if (a.q_f32) {
+            if (rules) hipLaunchKernelGGL((cache_mass_kernel<DH, 3, true>), grid, dim3(256), 0, st, a, to);
+            else hipLaunchKernelGGL((cache_mass_kernel<DH, 3, false>), grid, dim3(256), 0, st, a, to);
+        } else if (rules) hipLaunchKernelGGL((cache_mass_kernel<DH, 1, true>), grid, dim3(256), 0, st, a, to);
+        else hipLaunchKernelGGL((cache_mass_kernel<DH, 1, false>), grid, dim3(256), 0, st, a, to);
+    } else if (c.dtype == ANPD_BF16) hipLaunchKernelGGL((cache_mass_plain_kernel<bf16_t, DH>), grid, dim3(256), 0, st, a, to);
+    else hipLaunchKernelGGL((cache_mass_plain_kernel<float, DH>), grid, dim3(256), 0, st, a, to);
+    HIP_TRY(hipGetLastError());
+    if (a.part) {
+        hipLaunchKernelGGL(cache_mass_join_kernel, dim3((unsigned)((int64_t)a.n_blocks * a.n_kv_heads)), dim3(kMassKeys), 0, st, a, to);
+        HIP_TRY(hipGetLastError());
+    }
+    return ANPD_OK;
+}
+
+int32_t workspace_of(const char *who, AttnArgs &a, size_t need, void *workspace, size_t workspace_bytes)
+{
+    if (need == 0) return ANPD_OK;
+    if (!workspace || ((uintptr_t)workspace & 255) != 0) return fail(ANPD_E_INVAL, "%s: workspace must be a 256-byte aligned device buffer", who);
+    if (workspace_bytes < need) return fail(ANPD_E_CAPACITY, "%s: workspace has %zu bytes, %zu needed", who, workspace_bytes, need);
+    a.part = (float *)workspace;
+    return ANPD_OK;
+}
+
+bool overlap(const void *a, size_t na, const void *b, size_t nb)
+{
+    return (const char *)a < (const char *)b + nb && (const char *)b < (const char *)a + na;
+}
+
+bool cache_cfg_ok(const char *who, const anpd_cache_cfg *c, int32_t max_tokens, CacheShape *out)
+{
+#define REQ(cond, msg) if (!(cond)) { fail(ANPD_E_INVAL, "%s: " msg, who); return false; }
+    REQ(c, "cfg is NULL");
+    REQ(c->n_layers >= 1 && c->n_heads >= 1, "non-positive dimension");
+    REQ(c->n_kv_heads >= 0 && (c->n_kv_heads == 0 || c->n_heads % c->n_kv_heads == 0), "n_kv_heads must be 0 or divide n_heads");
+    REQ(c->n_heads <= (1 << 16) && c->n_layers <= (1 << 16), "more than 2^16 heads or layers");
+    REQ(c->head_dim == 64 || c->head_dim == 128, "head_dim must be 64 or 128");
+    REQ(c->dtype == ANPD_F32 || c->dtype == ANPD_BF16, "dtype must be ANPD_F32 or ANPD_BF16");
+    REQ(c->page_tokens >= 8 && c->page_tokens <= 256 && (c->page_tokens & (c->page_tokens - 1)) == 0, "page_tokens must be a power of two in 8..256");
+    REQ(max_tokens >= 1 && max_tokens <= (1 << 20), "max_tokens must be in 1..2^20");
+#undef REQ
+    *out = {c->n_layers, c->n_heads, c->n_kv_heads > 0 ? c->n_kv_heads : c->n_heads, c->head_dim, c->dtype, c->page_tokens,
+            c->dtype == ANPD_BF16 && c->page_tokens == 16};
+    return true;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t anpd_cache_pool_bytes(const anpd_cache_cfg *cfg, int32_t max_tokens)
+{
+    CacheShape shape;
+    return cache_cfg_ok("anpd_cache_pool_bytes", cfg, max_tokens, &shape) ? shape.pool_bytes(max_tokens) : 0;
+}
+
+int32_t anpd_cache_create(const anpd_cache_cfg *cfg, void *pool, size_t pool_bytes, int32_t max_tokens, anpd_kv_t **out)
+{
+    if (!out) return fail(ANPD_E_INVAL, "anpd_cache_create: out is NULL");
+    *out = nullptr;
+    CacheShape shape;
+    if (!cache_cfg_ok("anpd_cache_create", cfg, max_tokens, &shape)) return ANPD_E_INVAL;
+    if (!pool) return fail(ANPD_E_INVAL, "anpd_cache_create: pool is NULL");
+    return make_cache("anpd_cache_create", nullptr, shape, pool, pool_bytes, max_tokens, out);
+}
+
+size_t anpd_attention_workspace_bytes(const anpd_kv_t *const *kvs, int32_t n_seq, const int32_t *n_rows, const int32_t *pos0, const anpd_attn_rules *rules)
+{
+    AttnArgs a;
+    int64_t rows;
+    if (gather("anpd_attention_workspace_bytes", kvs, n_seq, n_rows, pos0, rules, a, rows) != ANPD_OK) return 0;
+    return plan_attention(a, kvs[0]->shape, kvs[0]->n_cu);
+}
+
+int32_t anpd_attention(const anpd_kv_t *const *kvs, int32_t n_seq, const int32_t *n_rows, const int32_t *pos0, int32_t layer, const void *q, int64_t ldq,
+                       int32_t dtype, const anpd_attn_rules *rules, void *out, int64_t ldo, float *lse, void *workspace, size_t workspace_bytes, void *stream)
+{
+    const char *who = "anpd_attention";
+    AttnArgs a;
+    int64_t rows;
+    int32_t rc = gather(who, kvs, n_seq, n_rows, pos0, rules, a, rows);
+    if (rc != ANPD_OK) return rc;
+    const CacheShape &c = kvs[0]->shape;
+    if ((rc = rows_in(who, c, layer, q, ldq, dtype, a)) != ANPD_OK) return rc;
+    if (ldo < (int64_t)c.n_heads * c.head_dim) return fail(ANPD_E_INVAL, "%s: ldo %lld is less than a row", who, (long long)ldo);
+    if (rows == 0) return ANPD_OK;
+    if (!q || !out) return fail(ANPD_E_INVAL, "%s: NULL rows", who);
+    if (((uintptr_t)out & (a.q_f32 ? 3 : 1)) != 0) return fail(ANPD_E_INVAL, "%s: out is not aligned to its type", who);
+    a.out = out;
+    a.ldo = ldo;
+    a.lse = lse;
+    a.q_wide = a.q_wide && ((uintptr_t)out & 15) == 0 && ldo % (a.q_f32 ? 4 : 8) == 0;
+    const size_t need = plan_attention(a, c, kvs[0]->n_cu);
+    if ((rc = workspace_of(who, a, need, workspace, workspace_bytes)) != ANPD_OK) return rc;
+    OnDevice on;
+    if ((rc = on.enter(who, kvs[0]->device)) != ANPD_OK) return rc;
+    return c.head_dim == 128 ? launch_attention<128>(a, c, (hipStream_t)stream) : launch_attention<64>(a, c, (hipStream_t)stream);
+}
+
+size_t anpd_key_mass_workspace_bytes(const anpd_kv_t *const *kvs, int32_t n_seq, const int32_t *n_rows, const int32_t *pos0, const anpd_attn_rules *rules)
+{
+    AttnArgs a;
+    int64_t rows;
+    if (gather("anpd_key_mass_workspace_bytes", kvs, n_seq, n_rows, pos0, rules, a, rows) != ANPD_OK) return 0;
+    return plan_mass(a, kvs[0]->n_cu);
+}
+
+int32_t anpd_key_mass(const anpd_kv_t *const *kvs, int32_t n_seq, const int32_t *n_rows, const int32_t *pos0, int32_t layer, const void *q, int64_t ldq,
+                      int32_t dtype, const anpd_attn_rules *rules, const float *lse, float *const *mass, int64_t ld_mass, void *workspace,
+                      size_t workspace_bytes, void *stream)
+{
+    const char *who = "anpd_key_mass";
+    AttnArgs a;
+    int64_t rows;
+    int32_t rc = gather(who, kvs, n_seq, n_rows, pos0, rules, a, rows);
+    if (rc != ANPD_OK) return rc;
+    const CacheShape &c = kvs[0]->shape;
+    if ((rc = rows_in(who, c, layer, q, ldq, dtype, a)) != ANPD_OK) return rc;
+    if (rows == 0) return ANPD_OK;
+    if (!q || !lse || !mass) return fail(ANPD_E_INVAL, "%s: NULL argument", who);
+    MassOut to;
+    std::memset(&to, 0, sizeof(to));
+    to.ld = ld_mass;
+    for (int s = 0; s < n_seq; ++s) {
+        if (a.seq[s].n == 0) continue;
+        const int total = a.seq[s].pos0 + a.seq[s].n;
+        if (!mass[s]) return fail(ANPD_E_INVAL, "%s: sequence %d: NULL mass", who, s);
+        if (ld_mass < total) return fail(ANPD_E_CAPACITY, "%s: sequence %d has %d keys, ld_mass is %lld", who, s, total, (long long)ld_mass);
+        for (int t = 0; t < s; ++t) {
+            if (a.seq[t].n == 0) continue;
+            const int other = a.seq[t].pos0 + a.seq[t].n;
+            if (overlap(mass[s], ((size_t)(c.n_kv_heads - 1) * ld_mass + total) * sizeof(float), mass[t], ((size_t)(c.n_kv_heads - 1) * ld_mass + other) * sizeof(float)))
+                return fail(ANPD_E_INVAL, "%s: sequences %d and %d share mass", who, t, s);
+        }
+        to.mass[s] = mass[s];
+    }
+    a.lse = const_cast<float *>(lse);   // (read only)
+    const size_t need = plan_mass(a, kvs[0]->n_cu);
+    if ((rc = workspace_of(who, a, need, workspace, workspace_bytes)) != ANPD_OK) return rc;
+    OnDevice on;
+    if ((rc = on.enter(who, kvs[0]->device)) != ANPD_OK) return rc;
+    return c.head_dim == 128 ? launch_mass<128>(a, to, c, (hipStream_t)stream) : launch_mass<64>(a, to, c, (hipStream_t)stream);
+}
+
+int32_t anpd_kv_evict(const anpd_kv_t *src, anpd_kv_t *dst, const float *mass, int64_t ld_mass, int32_t keep, int32_t first, int32_t last, float rope_base,
+                      int32_t *out_kept, float *out_mass, int64_t ld_out, void *stream)
+{
+    const char *who = "anpd_kv_evict";
+    if (!src || !dst) return fail(ANPD_E_INVAL, "%s: NULL cache", who);
+    const CacheShape &c = src->shape;
+    if (!same_shape(c, dst->shape) || src->device != dst->device) return fail(ANPD_E_INVAL, "%s: the caches have different shapes or devices", who);
+    const int len = src->len;
+    if (first < 0 || last < 0 || keep < 0 || (int64_t)first + last > keep) return fail(ANPD_E_INVAL, "%s: need 0 <= first + last <= keep", who);
+    if (keep > len || keep > dst->max_tokens) return fail(ANPD_E_CAPACITY, "%s: %d positions of %d, into a cache of %d", who, keep, len, dst->max_tokens);
+    if (!(rope_base == 0.f || rope_base > 1.f) || std::isinf(rope_base)) return fail(ANPD_E_INVAL, "%s: rope_base must be 0 or above 1", who);
+    const int64_t heads = (int64_t)c.n_layers * c.n_kv_heads;
+    if (keep > 0) {
+        if (!mass || !out_kept) return fail(ANPD_E_INVAL, "%s: NULL argument", who);
+        if (ld_mass < len || (out_mass && ld_out < keep)) return fail(ANPD_E_CAPACITY, "%s: rows of mass are shorter than their positions", who);
+        if (out_mass && overlap(mass, ((size_t)(heads - 1) * ld_mass + len) * sizeof(float), out_mass, ((size_t)(heads - 1) * ld_out + keep) * sizeof(float)))
+            return fail(ANPD_E_INVAL, "%s: out_mass overlaps mass", who);
+    }
+    OnDevice on;
+    int32_t rc = on.enter(who, src->device);
+    if (rc != ANPD_OK) return rc;
+    hipStream_t st = (hipStream_t)stream;
+    if (keep > 0) {
+        if ((rc = ensure_pages(dst, keep, st)) != ANPD_OK) return rc;
+        SelectArgs a = {mass, out_kept, out_mass, ld_mass, ld_out, len, keep, first, last};
+        hipLaunchKernelGGL(cache_select_kernel, dim3((unsigned)heads), dim3(kSelectThreads), 0, st, a);
+        HIP_TRY(hipGetLastError());
+        MoveArgs m;
+        std::memset(&m, 0, sizeof(m));
+        m.src = src->pool;
+        m.dst = dst->pool;
+        m.src_table = src->d_table;
+        m.dst_table = dst->d_table;
+        m.kept = out_kept;
+        m.rotate = rope_base > 0.f;
+        m.keep = keep;
+        m.n_layers = c.n_layers;
+        m.n_kv_heads = c.n_kv_heads;
+        m.page_tokens = c.page_tokens;
+        for (int i = 0; i < c.head_dim / 2 && m.rotate; ++i) m.turn[i] = std::pow((double)rope_base, -2.0 * i / c.head_dim) / (2.0 * 3.14159265358979323846);
+        const int groups = (keep + kMovePages * 16 - 1) / (kMovePages * 16);
+        // (into itself a cache moves in order, by one block per layer, head and kind)
+        const dim3 grid((unsigned)heads, 2, (unsigned)(dst == src ? 1 : groups));
+#define ANPD_MOVE(KERNEL) hipLaunchKernelGGL((KERNEL), grid, dim3(kMoveThreads), 0, st, m)
+        if (c.fragments) { if (c.head_dim == 128) ANPD_MOVE(cache_move_kernel<128>); else ANPD_MOVE(cache_move_kernel<64>); }
+        else if (c.dtype == ANPD_BF16) {
+            if (c.head_dim == 128) hipLaunchKernelGGL((cache_move_plain_kernel<bf16_t, 128>), grid, dim3(kMoveThreads), 0, st, m);
+            else hipLaunchKernelGGL((cache_move_plain_kernel<bf16_t, 64>), grid, dim3(kMoveThreads), 0, st, m);
+        } else if (c.head_dim == 128) hipLaunchKernelGGL((cache_move_plain_kernel<float, 128>), grid, dim3(kMoveThreads), 0, st, m);
+        else hipLaunchKernelGGL((cache_move_plain_kernel<float, 64>), grid, dim3(kMoveThreads), 0, st, m);
+#undef ANPD_MOVE
+        HIP_TRY(hipGetLastError());
+    }
+    return anpd_kv_truncate(dst, keep, stream);
+}
+
+}  // extern "C"

@@ -72,14 +72,6 @@ __host__ __device__ __forceinline__ size_t xq_offset(int nks, int m, int k, int 
     return ((((size_t)(m >> 4) * nks + (k >> 5)) * 2 + lo) * 64 + (size_t)((k >> 3) & 3) * 16 + (m & 15)) * 8 + (k & 7);
 }
 
-// two floats rounded to bf16 (nearest even) side by side, one instruction
-__device__ __forceinline__ uint32_t pack_bf16(float a, float b)
-{
-    typedef float f32x2 __attribute__((ext_vector_type(2)));
-    typedef __bf16 b16x2 __attribute__((ext_vector_type(2)));
-    return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){a, b}, b16x2));
-}
-
 // the rests of a and b behind their bf16 halves `hi`, rounded to bf16
 __device__ __forceinline__ uint32_t pack_lo(float a, float b, uint32_t hi)
 {

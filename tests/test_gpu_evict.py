@@ -1,0 +1,140 @@
+"""anpd_kv_evict: which positions stay, what is moved, and the steps that follow."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2404_08698_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+
+
+def expected(mass, keep, first, last):
+    """Positions that stay, by sorting (NaN below every number, -0 as 0, the lowest position among equal ones)."""
+    n = mass.shape[-1]
+    out = np.empty(mass.shape[:2] + (keep,), dtype=np.int64)
+    for i in np.ndindex(mass.shape[:2]):
+        m = mass[i]
+        value = np.where(np.isnan(m), -np.inf, m) + 0.0
+        middle = np.arange(first, n - last)
+        order = np.lexsort((middle, -value[middle], np.isnan(m[middle])))
+        best = np.sort(middle[order][:keep - first - last])
+        out[i] = np.concatenate([np.arange(first), best, np.arange(n - last, n)])
+    return out
+
+
+def filled(heads, dim, n, dtype, layers, page_tokens=16, capacity=None, seed=0):
+    gen = torch.Generator().manual_seed(seed)
+    kv = B.LayerCache(layers, heads, dim, capacity or n, dtype=dtype, page_tokens=page_tokens)
+    kv.set_page_order(torch.randperm(kv.num_pages, generator=gen).tolist())
+    contents = []
+    for layer in range(layers):
+        k, v = (torch.randn(n, heads * dim, generator=gen) for _ in range(2))
+        if dtype == "bf16":
+            k, v = k.bfloat16().float(), v.bfloat16().float()
+        kv.write(layer, 0, k.cuda(), v.cuda())
+        contents.append((k, v))
+    kv.truncate(n)
+    return kv, contents
+
+
+def check(heads, dim, n, keep, first=0, last=0, dtype="bf16", layers=2, page_tokens=16, into="other", rope_base=0.0, equal=0.3, mass=None, seed=0):
+    kv, contents = filled(heads, dim, n, dtype, layers, page_tokens, seed=seed)
+    if mass is None:
+        rng = np.random.RandomState(seed)
+        mass = np.exp(2 * rng.randn(layers, heads, n)).astype(np.float32)
+        mass[rng.rand(*mass.shape) < equal] = 0.0
+    dst = {"other": None, "self": kv}.get(into)
+    if dst is None:
+        dst = B.LayerCache(layers, heads, dim, max(keep, 1) + 3, dtype=dtype, page_tokens=page_tokens)
+    kept, out = B.evict(kv, torch.from_numpy(mass).cuda(), keep, first, last, into=dst, rope_base=rope_base)
+    want = expected(mass, keep, first, last)
+    assert np.array_equal(kept.cpu().numpy(), want)
+    assert np.array_equal(out.cpu().numpy(), np.take_along_axis(mass, want, -1), equal_nan=True)
+    assert dst.length == keep and (dst is kv or kv.length == n)
+    if keep == 0:
+        return
+    for layer, (k, v) in enumerate(contents):
+        got_k, got_v = (t.cpu().reshape(keep, heads, dim) for t in dst.read(layer, 0, keep))
+        for h in range(heads):
+            at = torch.from_numpy(want[layer, h])
+            ek, ev = (t.reshape(n, heads, dim)[at, h] for t in (k, v))
+            assert torch.equal(got_v[:, h], ev)
+            if not rope_base:
+                assert torch.equal(got_k[:, h], ek)
+                continue
+            theta = rope_base ** (-2.0 * torch.arange(dim // 2, dtype=torch.float64) / dim)
+            angle = (torch.arange(keep) - at).double()[:, None] * theta
+            a, b = ek[:, :dim // 2].double(), ek[:, dim // 2:].double()
+            turned = torch.cat([a * angle.cos() - b * angle.sin(), b * angle.cos() + a * angle.sin()], -1)
+            size = torch.cat([a.abs() + b.abs()] * 2, -1)
+            # cos and sin of an angle that is known to 2^-24 turns, four roundings; bf16: half a step of the result
+            allowed = size * (2 * math.pi + 6) * 2.0 ** -24
+            if dtype == "bf16":
+                allowed = allowed + 2.0 ** -8 * (turned.abs() + allowed)
+            stay = at == torch.arange(keep)
+            assert torch.equal(got_k[stay, h], ek[stay])
+            assert ((got_k[:, h].double() - turned).abs() <= allowed).all()
+
+
+FORMS = [("bf16", 16), ("f32", 16), ("bf16", 8), ("f32", 64)]
+
+
+@pytest.mark.parametrize("dtype,page_tokens", FORMS)
+@pytest.mark.parametrize("into", ["other", "self"])
+@pytest.mark.parametrize("rope_base", [0.0, 10000.0])
+@pytest.mark.parametrize("n,keep,first,last", [(1, 1, 0, 0), (1, 0, 0, 0), (20, 7, 2, 3), (300, 129, 4, 32), (300, 300, 0, 0), (300, 36, 4, 32), (1000, 17, 0, 0)])
+def test_sizes(n, keep, first, last, dtype, page_tokens, into, rope_base):
+    check(2, 64, n, keep, first, last, dtype, page_tokens=page_tokens, into=into, rope_base=rope_base, seed=n)
+
+
+@pytest.mark.parametrize("dtype,page_tokens", FORMS)
+@pytest.mark.parametrize("into", ["other", "self"])
+def test_heads_of_128(dtype, page_tokens, into):
+    check(3, 128, 2500, 1100, 4, 32, dtype, 1, page_tokens, into, rope_base=10000.0)
+
+
+@pytest.mark.parametrize("n,keep", [(5000, 4999), (20000, 1234), (70000, 40000)])
+def test_long_caches(n, keep):
+    check(1, 64, n, keep, 3, 9, layers=1, rope_base=500000.0)
+    check(1, 64, n, keep, 0, 0, layers=1, into="self", equal=0.9)
+
+
+def test_special_masses():
+    """Infinities, NaN, both zeros, subnormals, negative numbers, all the same."""
+    rng = np.random.RandomState(0)
+    pool = np.array([np.inf, -np.inf, np.nan, 0.0, -0.0, 1e-42, -1e-42, 1.0, -1.0, 3e38], dtype=np.float32)
+    for seed in range(4):
+        mass = pool[rng.randint(0, len(pool), (2, 2, 700))]
+        for keep in (1, 70, 350, 600, 699):
+            check(2, 64, 700, keep, mass=mass, seed=seed)
+    check(2, 64, 300, 100, 1, 1, mass=np.zeros((2, 2, 300), np.float32))
+    check(2, 64, 300, 100, mass=np.full((2, 2, 300), np.nan, np.float32))
+
+
+def test_mass_may_be_part_of_a_wider_tensor():
+    kv, _ = filled(2, 64, 100, "bf16", 1)
+    wide = torch.rand(1, 2, 130, device="cuda")
+    short = B.LayerCache(1, 2, 64, 40)
+    a = B.evict(kv, wide[:, :, 3:103], 40, into=short)
+    b = B.evict(kv, wide[:, :, 3:103].contiguous(), 40, into=short)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+def test_a_cache_goes_on_after_eviction():
+    """Growing again, in place, several times: pages that were handed back are handed out again."""
+    kv, contents = filled(2, 64, 200, "bf16", 1, capacity=200)
+    k, v = contents[0]
+    for turn in range(3):
+        n = kv.length
+        mass = torch.rand(1, 2, n, device="cuda")
+        kept, _ = B.evict(kv, mass, n // 2)
+        at = kept[0].cpu().long()
+        k, v = (torch.stack([t.reshape(n, 2, 64)[at[h], h] for h in range(2)], 1).reshape(n // 2, 128) for t in (k, v))
+        more = torch.randn(60, 128).bfloat16().float()
+        kv.write(0, n // 2, more.cuda(), more.cuda())
+        kv.truncate(n // 2 + 60)
+        k, v = torch.cat([k, more]), torch.cat([v, more])
+        got = kv.read(0, 0, n // 2 + 60)
+        assert torch.equal(got[0].cpu(), k) and torch.equal(got[1].cpu(), v)
