@@ -190,9 +190,10 @@ def prepare(case, seed):
         for i, (n, (k, v)) in enumerate(zip(lengths, caches)):
             kv = B.LayerCache(layers, heads, dim, n, n_kv_heads=kv_heads, dtype=case["cache"])
             kv.set_page_order(_page_order(_page_count(n), seed + i).tolist())
+            # (the new rows lie in the cache and are not committed: giving up a length gives up its pages)
+            kv.truncate(n if case["kind"] == "evict" else n - case["rows"])
             for layer in range(layers):
                 kv.write(layer, 0, k[layer].float(), v[layer].float())
-            kv.truncate(n if case["kind"] == "evict" else n - case["rows"])
             state["kvs"].append(kv)
         if case["kind"] == "evict":
             state["short"] = B.LayerCache(layers, heads, dim, case["keep"], n_kv_heads=kv_heads, dtype=case["cache"])
