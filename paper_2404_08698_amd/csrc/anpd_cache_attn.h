@@ -306,57 +306,42 @@ __device__ __forceinline__ void weigh(const AttnArgs &a, const RowInfo &r, int p
     }
 }
 
-// bf16 operands whose numbers are all finite?
-__device__ __forceinline__ bool finite8(u32x4 v)
+// Where some key of a tile is hidden from some row, its values must not meet a weight of 0 if they are infinite or NaN: that product
+// is NaN.  Such values are taken out of the tile (the return value says that there were any), and once the wave's tiles are through, added
+// to the outputs of the rows that see them, which are infinite or NaN from then on whatever else there is.
+template <int N>
+__device__ __forceinline__ bool take_out_unbounded(u32x4 (&v)[N])
 {
-    bool ok = true;
+    uint32_t found = 0;   // exponents of all ones, as carries out of them
 #pragma unroll
-    for (int i = 0; i < 4; ++i) ok = ok && (v[i] & 0x7f80u) != 0x7f80u && (v[i] & 0x7f800000u) != 0x7f800000u;
-    return ok;
-}
-
-// O += V^T P where some key of the page is hidden from some row and some value is not finite: 0 times an infinity would put
-// NaN into rows that do not see it.  The finite values as ever; of the others, how many a row sees of each kind.
-template <int TERMS>
-__device__ __forceinline__ void add_values_careful(f32x16 &o, u32x4 v, const u32x4 (&w)[TERMS], u32x4 seen)
-{
-    u32x4 fin, up, down, nan;
+    for (int n = 0; n < N; ++n)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        fin[i] = up[i] = down[i] = nan[i] = 0;
+        for (int i = 0; i < 4; ++i) found |= ((v[n][i] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+    if (__builtin_amdgcn_ballot_w64(found != 0) == 0) return false;
 #pragma unroll
-        for (int h = 0; h < 32; h += 16) {
-            const uint32_t x = (v[i] >> h) & 0xffffu, one = 0x3f80u << h;
-            if ((x & 0x7f80u) != 0x7f80u) fin[i] |= x << h;
-            else if (x & 0x7fu) nan[i] |= one;
-            else if (x & 0x8000u) down[i] |= one;
-            else up[i] |= one;
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t w = v[n][i];
+            v[n][i] = ((w & 0x7f80u) == 0x7f80u ? 0u : w & 0xffffu) | ((w & 0x7f800000u) == 0x7f800000u ? 0u : w & 0xffff0000u);
         }
-    }
-#pragma unroll
-    for (int k = 0; k < TERMS; ++k) o = mfma32(as_bf16(fin), as_bf16(w[k]), o);
-    const f32x16 zero = {};
-    const f32x16 n_up = mfma32(as_bf16(up), as_bf16(seen), zero), n_down = mfma32(as_bf16(down), as_bf16(seen), zero), n_nan = mfma32(as_bf16(nan), as_bf16(seen), zero);
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        if (n_up[i] > 0.f) o[i] += INFINITY;
-        if (n_down[i] > 0.f) o[i] -= INFINITY;
-        if (n_nan[i] > 0.f) o[i] += __builtin_nanf("");
-    }
+    return true;
 }
-
-// A lane's eight keys of page g (0, 1) of a 32-key tile: 1 where the row sees them, 0 elsewhere.
-template <bool RULES>
-__device__ __forceinline__ u32x4 seen_operand(const RowInfo &r, int pre, int base, int g)
+// The 32 keys from `base` on: value(j, dim) of key j, dim(d, i) of the lane's outputs.
+template <bool RULES, int NDT, typename Dim, typename Value>
+__device__ __forceinline__ void add_unbounded(const RowInfo &r, int pre, int base, Running<NDT> &run, Dim dim, Value value)
 {
-    const int half = (threadIdx.x >> 5) & 1;
-    u32x4 m;
+    for (int j = base; j < base + 32; ++j) {
+        if (!sees<RULES>(r, pre, j)) continue;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int j = base + 16 * g + 8 * (i >> 1) + 4 * half + 2 * (i & 1);
-        m[i] = (sees<RULES>(r, pre, j) ? 0x3f80u : 0u) | (sees<RULES>(r, pre, j + 1) ? 0x3f800000u : 0u);
+        for (int d = 0; d < NDT; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float v = value(j, dim(d, i));
+                if (!(fabsf(v) <= 3.4028234e38f)) run.o[d][i] += v;
+                if (i % 4 == 3) asm volatile("" ::: "memory");   // (four at a time: this is no place for registers)
+            }
     }
-    return m;
 }
 
 // ------------------------------------------------------------------ results
@@ -403,11 +388,12 @@ __device__ __forceinline__ int seq_of_block(const AttnArgs &a, int block)
     return lo;
 }
 
-// ------------------------------------------------------------------ keys and values straight into registers
+// ------------------------------------------------------------------ few rows: keys and values straight into registers
 //
 // Block = (32 virtual rows, kv head, split of the keys), four waves; wave w takes keys 32 w .. of every 128.  Nothing is shared
 // while the keys go by: a wave's loads are the operands, the next keys are requested when this tile's scores are done, its values
-// when its output is, and the waves meet at the end.   grid: n_blocks * n_splits * n_kv_heads
+// when its output is, and the waves meet at the end.  This is the form of single tokens, of windows and of prompts whose
+// blocks of 128 rows would leave compute units without one.   grid: n_blocks * n_splits * n_kv_heads
 constexpr int kStreamWaves = 4, kStreamTile = 32 * kStreamWaves;
 
 template <int DH, int TERMS, bool RULES>
@@ -435,6 +421,7 @@ __global__ __launch_bounds__(256, TERMS == 1 ? 2 : 1) void cache_attn_stream_ker
     }
     Running<NDT> run;
     run.start();
+    bool unbounded = false;
 
     const int last_page = (total - 1) >> 4;
     const bf16_t *pool = (const bf16_t *)s.pool;
@@ -490,33 +477,30 @@ __global__ __launch_bounds__(256, TERMS == 1 ? 2 : 1) void cache_attn_stream_ker
                     float x[8];
 #pragma unroll
                     for (int e = 0; e < 8; ++e) x[e] = sc[0][8 * g + e];
-                    u32x4 w[TERMS];
+                    u32x4 w[TERMS], v[NDT];
                     split_terms<TERMS>(x, w);
-                    bool careful = false;
-                    if (hidden) {
-                        bool ok = true;
 #pragma unroll
-                        for (int d = 0; d < NDB; ++d) ok = ok && finite8(vf[g][d][0]) && finite8(vf[g][d][1]);
-                        careful = __builtin_amdgcn_ballot_w64(!ok) != 0;
+                    for (int d = 0; d < NDT; ++d) {
+                        const int odd = 2 * (d & 1);
+                        v[d] = (u32x4){vf[g][d >> 1][0][odd], vf[g][d >> 1][0][odd + 1], vf[g][d >> 1][1][odd], vf[g][d >> 1][1][odd + 1]};
                     }
-                    const u32x4 seen = careful ? seen_operand<RULES>(r, pre, base, g) : (u32x4){0, 0, 0, 0};
+                    if (hidden) unbounded |= take_out_unbounded<NDT>(v);
 #pragma unroll
-                    for (int d = 0; d < NDB; ++d)
+                    for (int d = 0; d < NDT; ++d)
 #pragma unroll
-                        for (int odd = 0; odd < 2; ++odd) {
-                            const u32x4 v = {vf[g][d][0][2 * odd], vf[g][d][0][2 * odd + 1], vf[g][d][1][2 * odd], vf[g][d][1][2 * odd + 1]};
-                            f32x16 &o = run.o[2 * d + odd];
-                            if (careful) add_values_careful<TERMS>(o, v, w, seen);
-                            else {
-#pragma unroll
-                                for (int t = TERMS - 1; t >= 0; --t) o = mfma32(as_bf16(v), as_bf16(w[t]), o);
-                            }
-                        }
+                        for (int t = TERMS - 1; t >= 0; --t) run.o[d] = mfma32(as_bf16(v[d]), as_bf16(w[t]), run.o[d]);
                 }
             }
             load_v(na, nb);
         }
     }
+    if (unbounded)
+        for (int i = i0; i < i1; ++i) {
+            const int base = tiles.at(i) * kStreamTile + 32 * wave;
+            if (any_seen<RULES>(r, pre, base) && !all_seen<RULES>(r, pre, base))
+                add_unbounded<RULES, NDT>(r, pre, base, run, [&](int d, int e) { return 64 * (d >> 1) + 2 * (8 * (e >> 2) + 4 * half + (e & 3)) + (d & 1); },
+                                          [&](int j, int dim) { return bf16_to_f32(v_of[(size_t)s.table[j >> 4] * page_elems + vf_elem(j & 15, dim)]); });
+        }
     // ---- the waves meet: every wave scales to the row's reference, the sums are formed in wave order
     const float l = both_halves_sum(run.l);
     if (half == 0) { wm[wave][m] = run.m; wl[wave][m] = l; }
@@ -566,11 +550,146 @@ __global__ __launch_bounds__(256, TERMS == 1 ? 2 : 1) void cache_attn_stream_ker
     }
 }
 
+// ------------------------------------------------------------------ many rows: keys and values shared through LDS
+//
+// Block = (128 virtual rows, kv head, split of the keys), four waves of 32 rows each against the same 64 keys, which go from the
+// cache through registers into one of two LDS buffers while the other one is multiplied: a key is read from L2 once for 128 rows
+// where the form above reads it for 32, and a wave has the other block of its compute unit to cover its exponentials.
+// 32 heads, bf16, 3584 rows: 300 us in blocks of 32 rows, 143 us so (735 TFLOP/s).
+// grid: n_blocks * n_splits * n_kv_heads, blocks with the most keys first
+constexpr int kTileRows = 128, kTileKeys = 64;
+
+template <int DH, int TERMS, bool RULES>
+__global__ __launch_bounds__(256, TERMS == 1 ? 2 : 1) void cache_attn_tile_kernel(const AttnArgs a)
+{
+    constexpr int NKS = DH / 16, NDT = DH / 32, NCH = DH / 32;
+    __shared__ u32x4 lk[2][4][NCH][64], lv[2][4][NCH][64];   // [buffer][page][1 KB pieces][lane]
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, m = lane & 31;
+    const int kvh = blockIdx.x % a.n_kv_heads, rest = blockIdx.x / a.n_kv_heads;
+    const int split = rest % a.n_splits, block = a.n_blocks - 1 - rest / a.n_splits;
+    const SeqView s = a.seq[seq_of_block(a, block)];
+    const int vb = (block - s.block0) * kTileRows, rows = s.n * a.group, total = s.pos0 + s.n;
+    const int v0 = vb + kRowTile * wave;
+    const int p_lo = s.pos0 + vb / a.group, p_hi = s.pos0 + (vb + kTileRows <= rows ? vb + kTileRows - 1 : rows - 1) / a.group;
+    const int pre = RULES && a.prefix > 0 ? (a.prefix < total ? a.prefix : total) : 0;
+    const KeyTiles tiles = key_tiles(p_lo, p_hi, total, RULES ? a.window : 0, RULES ? a.prefix : 0, kTileKeys);
+    const int i0 = split * a.chunk, i1 = i0 + a.chunk < tiles.n ? i0 + a.chunk : tiles.n;
+    if (i0 >= tiles.n) return;   // (the whole block; what joins the splits does not look at this one)
+    const RowInfo r = row_info<RULES>(a, s, kvh, v0);
+
+    u32x4 q[NKS][TERMS];
+    {
+        const size_t at = (size_t)r.row * a.ldq + (size_t)r.head * DH + 8 * half;
+#pragma unroll
+        for (int ks = 0; ks < NKS; ++ks) load_q8<TERMS>(a, at + 16 * ks, q[ks]);
+    }
+    Running<NDT> run;
+    run.start();
+    bool unbounded = false;
+
+    const int last_page = (total - 1) >> 4;
+    const bf16_t *pool = (const bf16_t *)s.pool;
+    const size_t page_elems = (size_t)a.n_layers * 2 * a.n_kv_heads * 16 * DH;
+    const bf16_t *k_of = pool + ((size_t)a.layer * 2 * a.n_kv_heads + kvh) * (16 * DH), *v_of = k_of + (size_t)a.n_kv_heads * (16 * DH);
+    int ids = 0;
+    auto fetch_ids = [&](int i) __attribute__((always_inline)) {
+        const int t = i + lane < i1 ? i + lane : i1 - 1;
+        const int page = tiles.at(t) * (kTileKeys / 16) + wave;
+        ids = s.table[page < last_page ? page : last_page];
+    };
+    u32x4 sk[NCH], sv[NCH];
+    auto request = [&](int page) __attribute__((always_inline)) {
+        const u32x4 *pk = (const u32x4 *)(k_of + (size_t)page * page_elems) + lane, *pv = (const u32x4 *)(v_of + (size_t)page * page_elems) + lane;
+#pragma unroll
+        for (int c = 0; c < NCH; ++c) sk[c] = pk[c * 64];
+#pragma unroll
+        for (int c = 0; c < NCH; ++c) sv[c] = pv[c * 64];
+    };
+    auto put = [&](int buf) __attribute__((always_inline)) {
+#pragma unroll
+        for (int c = 0; c < NCH; ++c) lk[buf][wave][c][lane] = sk[c];
+#pragma unroll
+        for (int c = 0; c < NCH; ++c) lv[buf][wave][c][lane] = sv[c];
+    };
+    fetch_ids(i0);
+    request(__builtin_amdgcn_readlane(ids, 0));
+    put(0);
+    for (int i = i0; i < i1; ++i) {
+        const int buf = (i - i0) & 1, nx = (i + 1 - i0) & 63;
+        __syncthreads();   // this tile has arrived, and nobody reads the other buffer any more
+        if (nx == 0) fetch_ids(i + 1);
+        request(__builtin_amdgcn_readlane(ids, nx));   // (behind the last one: for nothing)
+        const int base = tiles.at(i) * kTileKeys;
+        if (v0 < rows && (any_seen<RULES>(r, pre, base) || any_seen<RULES>(r, pre, base + 32))) {
+            f32x16 sc[2];
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) sc[b][e] = 0.f;
+                const u32x4 *kp = &lk[buf][2 * b + ((lane >> 4) & 1)][0][half * 16 + (lane & 15)];
+#pragma unroll
+                for (int ks = 0; ks < NKS; ++ks) {
+                    const u32x4 k = kp[(ks >> 1) * 64 + (ks & 1) * 32];
+#pragma unroll
+                    for (int t = TERMS - 1; t >= 0; --t) sc[b] = mfma32(as_bf16(k), as_bf16(q[ks][t]), sc[b]);
+                }
+            }
+            weigh<RULES, 2, NDT>(a, r, pre, base, sc, run);
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                float x[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] = sc[g >> 1][8 * (g & 1) + e];
+                u32x4 w[TERMS];
+                split_terms<TERMS>(x, w);
+                const uint2 *vp = (const uint2 *)&lv[buf][g][0][0] + (m >> 4) * 64 + half * 16 + (m & 15);
+                u32x4 v[NDT];
+#pragma unroll
+                for (int d = 0; d < NDT; ++d) {
+                    const uint2 x0 = vp[d * 128], x1 = vp[d * 128 + 32];
+                    v[d] = (u32x4){x0.x, x0.y, x1.x, x1.y};
+                }
+                if (!all_seen<RULES>(r, pre, base + 32 * (g >> 1))) unbounded |= take_out_unbounded<NDT>(v);
+#pragma unroll
+                for (int d = 0; d < NDT; ++d)
+#pragma unroll
+                    for (int t = TERMS - 1; t >= 0; --t) run.o[d] = mfma32(as_bf16(v[d]), as_bf16(w[t]), run.o[d]);
+            }
+        }
+        put(buf ^ 1);
+    }
+    if (unbounded)
+        for (int i = i0; i < i1; ++i)
+            for (int base = tiles.at(i) * kTileKeys, end = base + kTileKeys; base < end; base += 32)
+                if (any_seen<RULES>(r, pre, base) && !all_seen<RULES>(r, pre, base))
+                    add_unbounded<RULES, NDT>(r, pre, base, run, [&](int d, int e) { return 32 * d + 8 * (e >> 2) + 4 * half + (e & 3); },
+                                              [&](int j, int dim) { return bf16_to_f32(v_of[(size_t)s.table[j >> 4] * page_elems + vf_elem(j & 15, dim)]); });
+    const float l = both_halves_sum(run.l);
+    if (a.part) {
+        float *to = a.part + (((size_t)block * a.n_kv_heads + kvh) * a.n_splits + split) * part_floats(kTileRows, DH);
+        const int row = kRowTile * wave + m;
+        if (half == 0) *(float2 *)(to + kTileRows * DH + 2 * row) = make_float2(run.m, l);
+#pragma unroll
+        for (int d = 0; d < NDT; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                *(f32x4 *)(to + row * DH + 32 * d + 8 * i + 4 * half) = (f32x4){run.o[d][4 * i], run.o[d][4 * i + 1], run.o[d][4 * i + 2], run.o[d][4 * i + 3]};
+    } else if (r.live) {
+        const float inv = inverse_sum(l);
+        if (half == 0) store_lse(a, r.row, r.head, run.m, l);
+#pragma unroll
+        for (int d = 0; d < NDT; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                store_out4(a, DH, r.row, r.head, 32 * d + 8 * i + 4 * half, (f32x4){run.o[d][4 * i], run.o[d][4 * i + 1], run.o[d][4 * i + 2], run.o[d][4 * i + 3]} * inv);
+    }
+}
+
 // ------------------------------------------------------------------ caches in plain order
 //
 // Blocks of [token][dim] in fp32 or bf16, pages of 8 to 256 tokens: exact fp32 products (v_mfma_f32_32x32x2_f32, whose lanes hold
 // the same rows and keys as above).  The two contracted numbers of an instruction are dims t and t + head_dim / 2 of a key, so a lane
-// reads half a key in one piece.  Blocks, waves and splits as above.
+// reads half a key in one piece.  Blocks, waves and splits as in the form for few rows, whatever the rows' number.
 // grid: n_blocks * n_splits * n_kv_heads
 __device__ __forceinline__ f32x16 mfma32f(float x, float y, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x2f32(x, y, c, 0, 0, 0); }
 
@@ -624,6 +743,7 @@ __global__ __launch_bounds__(256, 1) void cache_attn_plain_kernel(const AttnArgs
     }
     Running<NDT> run;
     run.start();
+    bool unbounded = false;
     const KT *pool = (const KT *)s.pool;
     for (int i = i0; i < i1; ++i) {
         const int base = tiles.at(i) * kStreamTile + 32 * wave;
@@ -646,25 +766,24 @@ __global__ __launch_bounds__(256, 1) void cache_attn_plain_kernel(const AttnArgs
             const KT *p = pool + kv_offset(s.table[key / pt], a.layer, a.n_layers, 1, kvh, a.n_kv_heads, key % pt, pt, DH) + m;
 #pragma unroll
             for (int d = 0; d < NDT; ++d) {
-                const float v = load_f32(p, 32 * d);
-                if (hidden && __builtin_amdgcn_ballot_w64(!(fabsf(v) <= 3.4028234e38f)) != 0) {
-                    // 0 times an infinity would put NaN into rows that do not see the key: see add_values_careful
+                float v = load_f32(p, 32 * d);
+                if (hidden) {
                     const bool fin = fabsf(v) <= 3.4028234e38f;
-                    const f32x16 zero = {};
-                    const float seen = sees<true>(r, pre, j) ? 1.f : 0.f;
-                    run.o[d] = mfma32f(fin ? v : 0.f, sc[0][e], run.o[d]);
-                    const f32x16 n_up = mfma32f(v == INFINITY ? 1.f : 0.f, seen, zero), n_down = mfma32f(v == -INFINITY ? 1.f : 0.f, seen, zero),
-                                 n_nan = mfma32f(v != v ? 1.f : 0.f, seen, zero);
-#pragma unroll
-                    for (int x = 0; x < 16; ++x) {
-                        if (n_up[x] > 0.f) run.o[d][x] += INFINITY;
-                        if (n_down[x] > 0.f) run.o[d][x] -= INFINITY;
-                        if (n_nan[x] > 0.f) run.o[d][x] += __builtin_nanf("");
-                    }
-                } else run.o[d] = mfma32f(v, sc[0][e], run.o[d]);
+                    unbounded |= __builtin_amdgcn_ballot_w64(!fin) != 0;
+                    v = fin ? v : 0.f;
+                }
+                run.o[d] = mfma32f(v, sc[0][e], run.o[d]);
             }
         }
     }
+    if (unbounded)
+        for (int i = i0; i < i1; ++i) {
+            const int base = tiles.at(i) * kStreamTile + 32 * wave;
+            if (any_seen<true>(r, pre, base) && !all_seen<true>(r, pre, base))
+                add_unbounded<true, NDT>(r, pre, base, run, [&](int d, int e) { return 32 * d + 8 * (e >> 2) + 4 * half + (e & 3); }, [&](int j, int dim) {
+                    return load_f32(pool + kv_offset(s.table[j / pt], a.layer, a.n_layers, 1, kvh, a.n_kv_heads, j % pt, pt, DH), dim);
+                });
+        }
     const float l = both_halves_sum(run.l);
     if (half == 0) { wm[wave][m] = run.m; wl[wave][m] = l; }
     __syncthreads();
@@ -703,23 +822,24 @@ __global__ __launch_bounds__(256, 1) void cache_attn_plain_kernel(const AttnArgs
 // ------------------------------------------------------------------ the splits meet
 //
 // Block = (32 virtual rows, kv head): four adjacent dims of a row per thread, the splits in their order.
-// grid: n_kv_heads * n_blocks
+// row_block: rows of the blocks that were split; tile: keys of their tiles.   grid: n_kv_heads * n_blocks * (row_block / 32)
 template <int DH>
-__global__ __launch_bounds__(256) void cache_attn_join_kernel(const AttnArgs a)
+__global__ __launch_bounds__(256) void cache_attn_join_kernel(const AttnArgs a, int row_block, int tile, int rules)
 {
     constexpr int TPR = DH / 4, RPP = 256 / TPR;   // threads of a row, rows at a time
-    const int kvh = blockIdx.x % a.n_kv_heads, block = blockIdx.x / a.n_kv_heads;
+    const int per = row_block / kRowTile;
+    const int kvh = blockIdx.x % a.n_kv_heads, sub = blockIdx.x / a.n_kv_heads % per, block = blockIdx.x / a.n_kv_heads / per;
     const SeqView s = a.seq[seq_of_block(a, block)];
-    const int vb = (block - s.block0) * kRowTile, rows = s.n * a.group;
-    const int p_lo = s.pos0 + vb / a.group, p_hi = s.pos0 + (vb + kRowTile <= rows ? vb + kRowTile - 1 : rows - 1) / a.group;
-    const KeyTiles tiles = key_tiles(p_lo, p_hi, s.pos0 + s.n, a.window, a.prefix, kStreamTile);
+    const int vb = (block - s.block0) * row_block, rows = s.n * a.group;
+    const int p_lo = s.pos0 + vb / a.group, p_hi = s.pos0 + (vb + row_block <= rows ? vb + row_block - 1 : rows - 1) / a.group;
+    const KeyTiles tiles = key_tiles(p_lo, p_hi, s.pos0 + s.n, rules ? a.window : 0, rules ? a.prefix : 0, tile);
     const int used = (tiles.n + a.chunk - 1) / a.chunk;
-    const size_t stride = part_floats(kRowTile, DH);
+    const size_t stride = part_floats(row_block, DH);
     const float *from = a.part + ((size_t)block * a.n_kv_heads + kvh) * a.n_splits * stride;
     for (int i = 0; i < kRowTile; i += RPP) {
-        const int row = i + (int)threadIdx.x / TPR, dim = (int)threadIdx.x % TPR * 4, v = vb + row;
+        const int row = kRowTile * sub + i + (int)threadIdx.x / TPR, dim = (int)threadIdx.x % TPR * 4, v = vb + row;
         if (v >= rows) continue;
-        const float *ml = from + kRowTile * DH + 2 * row, *o = from + row * DH + dim;
+        const float *ml = from + row_block * DH + 2 * row, *o = from + row * DH + dim;
         float top = kNoKey;
         for (int k = 0; k < used; ++k) top = fmaxf(top, ml[k * stride]);
         float sum = 0.f;

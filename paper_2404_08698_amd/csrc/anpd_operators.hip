@@ -103,21 +103,38 @@ int32_t rows_in(const char *who, const CacheShape &c, int32_t layer, const void 
 
 // ---- attention: how the work is divided
 
-// Sets the row blocks of a's sequences, the splits and their size; returns the workspace that the splits need.
-size_t plan_attention(AttnArgs &a, const CacheShape &c, int n_cu)
+struct Plan {
+    bool shared;   // 128 rows share keys through LDS; otherwise blocks of 32 rows
+    int row_block, key_tile;
+    size_t part_bytes;
+};
+
+// Sets the row blocks of a's sequences, the splits and their size.
+Plan plan_attention(AttnArgs &a, const CacheShape &c, int n_cu)
 {
+    Plan p;
+    int64_t blocks32 = 0, blocks128 = 0;
+    for (int s = 0; s < a.n_seq; ++s) {
+        const int64_t v = (int64_t)a.seq[s].n * a.group;
+        blocks32 += (v + kRowTile - 1) / kRowTile;
+        blocks128 += (v + kTileRows - 1) / kTileRows;
+    }
+    p.shared = c.fragments && blocks128 * a.n_kv_heads >= n_cu && blocks128 * 3 <= blocks32;
+    p.row_block = p.shared ? kTileRows : kRowTile;
+    p.key_tile = p.shared ? kTileKeys : kStreamTile;
     a.n_blocks = 0;
     int most = 0;   // tiles of a row block
     for (int s = 0; s < a.n_seq; ++s) {
         SeqView &v = a.seq[s];
         v.block0 = a.n_blocks;
         if (v.n == 0) continue;
-        a.n_blocks += (int32_t)(((int64_t)v.n * a.group + kRowTile - 1) / kRowTile);
-        const int total = v.pos0 + v.n, pre = a.prefix < total ? a.prefix : total, pre_tiles = (pre + kStreamTile - 1) / kStreamTile;
-        const int all = (total - 1) / kStreamTile + 1;
+        const int64_t rows = (int64_t)v.n * a.group;
+        a.n_blocks += (int32_t)((rows + p.row_block - 1) / p.row_block);
+        const int total = v.pos0 + v.n, pre = a.prefix < total ? a.prefix : total, pre_tiles = (pre + p.key_tile - 1) / p.key_tile;
+        const int all = (total - 1) / p.key_tile + 1;
         int64_t tiles = all > pre_tiles ? all : pre_tiles;
         if (a.window > 0) {
-            const int64_t some = pre_tiles + ((int64_t)a.window + kRowTile / a.group + 1) / kStreamTile + 2;
+            const int64_t some = pre_tiles + ((int64_t)a.window + p.row_block / a.group + 1) / p.key_tile + 2;
             if (some < tiles) tiles = some;
         }
         if (tiles > most) most = (int)tiles;
@@ -128,25 +145,33 @@ size_t plan_attention(AttnArgs &a, const CacheShape &c, int n_cu)
     if (splits < 1) splits = 1;
     a.chunk = most > 0 ? (int)((most + splits - 1) / splits) : 1;
     a.n_splits = most > 0 ? (most + a.chunk - 1) / a.chunk : 1;
-    return a.n_splits > 1 ? align_up((size_t)items * a.n_splits * part_floats(kRowTile, c.head_dim) * sizeof(float)) : 0;
+    p.part_bytes = a.n_splits > 1 ? align_up((size_t)items * a.n_splits * part_floats(p.row_block, c.head_dim) * sizeof(float)) : 0;
+    return p;
 }
 
-template <int DH>
-int32_t launch_attention(const AttnArgs &a, const CacheShape &c, hipStream_t st)
+template <int DH, int TERMS, bool RULES>
+void launch_fragments(const AttnArgs &a, const Plan &p, hipStream_t st)
 {
-    const dim3 grid((unsigned)((int64_t)a.n_blocks * a.n_splits * a.n_kv_heads)), block(256);
+    const dim3 grid((unsigned)((int64_t)a.n_blocks * a.n_splits * a.n_kv_heads));
+    if (p.shared) hipLaunchKernelGGL((cache_attn_tile_kernel<DH, TERMS, RULES>), grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((cache_attn_stream_kernel<DH, TERMS, RULES>), grid, dim3(256), 0, st, a);
+}
+template <int DH>
+int32_t launch_attention(const AttnArgs &a, const Plan &p, const CacheShape &c, hipStream_t st)
+{
     const bool rules = ruled(a);
     if (c.fragments) {
-        if (a.q_f32) {
-            if (rules) hipLaunchKernelGGL((cache_attn_stream_kernel<DH, 3, true>), grid, block, 0, st, a);
-            else hipLaunchKernelGGL((cache_attn_stream_kernel<DH, 3, false>), grid, block, 0, st, a);
-        } else if (rules) hipLaunchKernelGGL((cache_attn_stream_kernel<DH, 1, true>), grid, block, 0, st, a);
-        else hipLaunchKernelGGL((cache_attn_stream_kernel<DH, 1, false>), grid, block, 0, st, a);
-    } else if (c.dtype == ANPD_BF16) hipLaunchKernelGGL((cache_attn_plain_kernel<bf16_t, DH>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((cache_attn_plain_kernel<float, DH>), grid, block, 0, st, a);
+        if (a.q_f32) { if (rules) launch_fragments<DH, 3, true>(a, p, st); else launch_fragments<DH, 3, false>(a, p, st); }
+        else { if (rules) launch_fragments<DH, 1, true>(a, p, st); else launch_fragments<DH, 1, false>(a, p, st); }
+    } else {
+        const dim3 grid((unsigned)((int64_t)a.n_blocks * a.n_splits * a.n_kv_heads));
+        if (c.dtype == ANPD_BF16) hipLaunchKernelGGL((cache_attn_plain_kernel<bf16_t, DH>), grid, dim3(256), 0, st, a);
+        else hipLaunchKernelGGL((cache_attn_plain_kernel<float, DH>), grid, dim3(256), 0, st, a);
+    }
     HIP_TRY(hipGetLastError());
     if (a.part) {
-        hipLaunchKernelGGL((cache_attn_join_kernel<DH>), dim3((unsigned)((int64_t)a.n_blocks * a.n_kv_heads)), block, 0, st, a);
+        hipLaunchKernelGGL((cache_attn_join_kernel<DH>), dim3((unsigned)((int64_t)a.n_blocks * a.n_kv_heads * (p.row_block / kRowTile))), dim3(256), 0, st, a,
+                           p.row_block, p.key_tile, rules ? 1 : 0);
         HIP_TRY(hipGetLastError());
     }
     return ANPD_OK;
@@ -255,7 +280,7 @@ size_t anpd_attention_workspace_bytes(const anpd_kv_t *const *kvs, int32_t n_seq
     AttnArgs a;
     int64_t rows;
     if (gather("anpd_attention_workspace_bytes", kvs, n_seq, n_rows, pos0, rules, a, rows) != ANPD_OK) return 0;
-    return plan_attention(a, kvs[0]->shape, kvs[0]->n_cu);
+    return plan_attention(a, kvs[0]->shape, kvs[0]->n_cu).part_bytes;
 }
 
 int32_t anpd_attention(const anpd_kv_t *const *kvs, int32_t n_seq, const int32_t *n_rows, const int32_t *pos0, int32_t layer, const void *q, int64_t ldq,
@@ -276,11 +301,11 @@ int32_t anpd_attention(const anpd_kv_t *const *kvs, int32_t n_seq, const int32_t
     a.ldo = ldo;
     a.lse = lse;
     a.q_wide = a.q_wide && ((uintptr_t)out & 15) == 0 && ldo % (a.q_f32 ? 4 : 8) == 0;
-    const size_t need = plan_attention(a, c, kvs[0]->n_cu);
-    if ((rc = workspace_of(who, a, need, workspace, workspace_bytes)) != ANPD_OK) return rc;
+    const Plan p = plan_attention(a, c, kvs[0]->n_cu);
+    if ((rc = workspace_of(who, a, p.part_bytes, workspace, workspace_bytes)) != ANPD_OK) return rc;
     OnDevice on;
     if ((rc = on.enter(who, kvs[0]->device)) != ANPD_OK) return rc;
-    return c.head_dim == 128 ? launch_attention<128>(a, c, (hipStream_t)stream) : launch_attention<64>(a, c, (hipStream_t)stream);
+    return c.head_dim == 128 ? launch_attention<128>(a, p, c, (hipStream_t)stream) : launch_attention<64>(a, p, c, (hipStream_t)stream);
 }
 
 size_t anpd_key_mass_workspace_bytes(const anpd_kv_t *const *kvs, int32_t n_seq, const int32_t *n_rows, const int32_t *pos0, const anpd_attn_rules *rules)
