@@ -126,6 +126,20 @@ __host__ __device__ __forceinline__ KeyTiles key_tiles(int p_lo, int p_hi, int t
     return k;
 }
 
+__device__ __forceinline__ int wave_min(int v)
+{
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) { const int w = __shfl_xor(v, o, 64); v = w < v ? w : v; }
+    return __builtin_amdgcn_readfirstlane(v);
+}
+// The first of tiles i0 .. i1 - 1 that does not lie wholly below key fk (i1: none); tiles are in the order of their keys.
+__device__ __forceinline__ int first_tile(const KeyTiles &k, int fk, int i0, int i1, int tile)
+{
+    if (fk <= 0) return i0;
+    const int t = fk / tile, i = t <= k.a ? t : (t <= k.b0 ? k.a : k.a + (t - k.b0));
+    return i < i0 ? i0 : (i < i1 ? i : i1);
+}
+
 // tanh, to 2^-23 of its value: a sum of powers where 1 - 2 / (1 + e^2x) would lose them
 __device__ __forceinline__ float tanh_f32(float x)
 {
@@ -410,8 +424,9 @@ __global__ __launch_bounds__(256, TERMS == 1 ? 2 : 1) void cache_attn_stream_ker
     const RowInfo r = row_info<RULES>(a, s, kvh, v0);
     const int pre = RULES && a.prefix > 0 ? (a.prefix < total ? a.prefix : total) : 0;
     const KeyTiles tiles = key_tiles(__builtin_amdgcn_readlane(r.p, 0), __builtin_amdgcn_readlane(r.p, 31), total, RULES ? a.window : 0, RULES ? a.prefix : 0, kStreamTile);
-    const int i0 = split * a.chunk, i1 = i0 + a.chunk < tiles.n ? i0 + a.chunk : tiles.n;
-    if (i0 >= tiles.n) return;   // (the whole block; what joins the splits does not look at this one)
+    const int begin = split * a.chunk, i1 = begin + a.chunk < tiles.n ? begin + a.chunk : tiles.n;
+    if (begin >= tiles.n) return;   // (the whole block; what joins the splits does not look at this one)
+    const int i0 = RULES ? first_tile(tiles, wave_min(r.fk), begin, i1, kStreamTile) : begin;   // (the same for all waves)
 
     u32x4 q[NKS][TERMS];
     {
@@ -451,7 +466,7 @@ __global__ __launch_bounds__(256, TERMS == 1 ? 2 : 1) void cache_attn_stream_ker
                 for (int x = 0; x < 2; ++x) vf[g][d][x] = p[d * 128 + x * 16];
         }
     };
-    {
+    if (i0 < i1) {
         fetch_ids(i0);
         const int pa = __builtin_amdgcn_readlane(ida, 0), pb = __builtin_amdgcn_readlane(idb, 0);
         load_k(pa, pb);
@@ -513,9 +528,9 @@ __global__ __launch_bounds__(256, TERMS == 1 ? 2 : 1) void cache_attn_stream_ker
 #pragma unroll
     for (int w = 0; w < kStreamWaves; ++w) sum = fmaf(wl[w][m], __builtin_amdgcn_exp2f(wm[w][m] - top), sum);
     float *to = a.part ? a.part + (((size_t)block * a.n_kv_heads + kvh) * a.n_splits + split) * part_floats(kRowTile, DH) : nullptr;
-    if (wave == 0 && half == 0) {
+    if (wave == 0 && half == 0 && r.live) {   // (beyond the last row nobody asks)
         if (to) *(float2 *)(to + kRowTile * DH + 2 * m) = make_float2(top, sum);
-        else if (r.live) store_lse(a, r.row, r.head, top, sum);
+        else store_lse(a, r.row, r.head, top, sum);
     }
     const float inv = inverse_sum(sum);
 #pragma unroll
@@ -540,10 +555,11 @@ __global__ __launch_bounds__(256, TERMS == 1 ? 2 : 1) void cache_attn_stream_ker
                 x[i >> 1][2 * (i & 1) + odd] = t;
             }
         const int dim = 64 * d + 16 * wave + 8 * half;
+        if (!r.live) continue;
         if (to) {
             *(f32x4 *)(to + m * DH + dim) = x[0];
             *(f32x4 *)(to + m * DH + dim + 4) = x[1];
-        } else if (r.live) {
+        } else {
             store_out4(a, DH, r.row, r.head, dim, x[0] * inv);
             store_out4(a, DH, r.row, r.head, dim + 4, x[1] * inv);
         }
@@ -573,9 +589,21 @@ __global__ __launch_bounds__(256, TERMS == 1 ? 2 : 1) void cache_attn_tile_kerne
     const int p_lo = s.pos0 + vb / a.group, p_hi = s.pos0 + (vb + kTileRows <= rows ? vb + kTileRows - 1 : rows - 1) / a.group;
     const int pre = RULES && a.prefix > 0 ? (a.prefix < total ? a.prefix : total) : 0;
     const KeyTiles tiles = key_tiles(p_lo, p_hi, total, RULES ? a.window : 0, RULES ? a.prefix : 0, kTileKeys);
-    const int i0 = split * a.chunk, i1 = i0 + a.chunk < tiles.n ? i0 + a.chunk : tiles.n;
-    if (i0 >= tiles.n) return;   // (the whole block; what joins the splits does not look at this one)
+    const int begin = split * a.chunk, i1 = begin + a.chunk < tiles.n ? begin + a.chunk : tiles.n;
+    if (begin >= tiles.n) return;   // (the whole block; what joins the splits does not look at this one)
     const RowInfo r = row_info<RULES>(a, s, kvh, v0);
+    int i0 = begin;
+    if (RULES && a.first_key) {   // (the same for all)
+        int *lowest = (int *)&lk[0][0][0][0];
+        const int low = wave_min(r.fk);
+        if (lane == 0) lowest[wave] = low;
+        __syncthreads();
+        int fk = lowest[0];
+#pragma unroll
+        for (int w = 1; w < 4; ++w) fk = lowest[w] < fk ? lowest[w] : fk;
+        __syncthreads();
+        i0 = first_tile(tiles, __builtin_amdgcn_readfirstlane(fk), begin, i1, kTileKeys);
+    }
 
     u32x4 q[NKS][TERMS];
     {
@@ -611,9 +639,11 @@ __global__ __launch_bounds__(256, TERMS == 1 ? 2 : 1) void cache_attn_tile_kerne
 #pragma unroll
         for (int c = 0; c < NCH; ++c) lv[buf][wave][c][lane] = sv[c];
     };
-    fetch_ids(i0);
-    request(__builtin_amdgcn_readlane(ids, 0));
-    put(0);
+    if (i0 < i1) {
+        fetch_ids(i0);
+        request(__builtin_amdgcn_readlane(ids, 0));
+        put(0);
+    }
     for (int i = i0; i < i1; ++i) {
         const int buf = (i - i0) & 1, nx = (i + 1 - i0) & 63;
         __syncthreads();   // this tile has arrived, and nobody reads the other buffer any more
@@ -665,6 +695,7 @@ __global__ __launch_bounds__(256, TERMS == 1 ? 2 : 1) void cache_attn_tile_kerne
                     add_unbounded<RULES, NDT>(r, pre, base, run, [&](int d, int e) { return 32 * d + 8 * (e >> 2) + 4 * half + (e & 3); },
                                               [&](int j, int dim) { return bf16_to_f32(v_of[(size_t)s.table[j >> 4] * page_elems + vf_elem(j & 15, dim)]); });
     const float l = both_halves_sum(run.l);
+    if (!r.live) return;
     if (a.part) {
         float *to = a.part + (((size_t)block * a.n_kv_heads + kvh) * a.n_splits + split) * part_floats(kTileRows, DH);
         const int row = kRowTile * wave + m;
@@ -674,7 +705,7 @@ __global__ __launch_bounds__(256, TERMS == 1 ? 2 : 1) void cache_attn_tile_kerne
 #pragma unroll
             for (int i = 0; i < 4; ++i)
                 *(f32x4 *)(to + row * DH + 32 * d + 8 * i + 4 * half) = (f32x4){run.o[d][4 * i], run.o[d][4 * i + 1], run.o[d][4 * i + 2], run.o[d][4 * i + 3]};
-    } else if (r.live) {
+    } else {
         const float inv = inverse_sum(l);
         if (half == 0) store_lse(a, r.row, r.head, run.m, l);
 #pragma unroll
@@ -728,8 +759,9 @@ __global__ __launch_bounds__(256, 1) void cache_attn_plain_kernel(const AttnArgs
     const RowInfo r = row_info<true>(a, s, kvh, v0);
     const int pre = a.prefix > 0 ? (a.prefix < total ? a.prefix : total) : 0;
     const KeyTiles tiles = key_tiles(__builtin_amdgcn_readlane(r.p, 0), __builtin_amdgcn_readlane(r.p, 31), total, a.window, a.prefix, kStreamTile);
-    const int i0 = split * a.chunk, i1 = i0 + a.chunk < tiles.n ? i0 + a.chunk : tiles.n;
-    if (i0 >= tiles.n) return;
+    const int begin = split * a.chunk, i1 = begin + a.chunk < tiles.n ? begin + a.chunk : tiles.n;
+    if (begin >= tiles.n) return;
+    const int i0 = first_tile(tiles, wave_min(r.fk), begin, i1, kStreamTile);
     float q[DH / 2];
     {
         const size_t at = (size_t)r.row * a.ldq + (size_t)r.head * DH + half * (DH / 2);
@@ -795,9 +827,9 @@ __global__ __launch_bounds__(256, 1) void cache_attn_plain_kernel(const AttnArgs
 #pragma unroll
     for (int w = 0; w < kStreamWaves; ++w) sum = fmaf(wl[w][m], __builtin_amdgcn_exp2f(wm[w][m] - top), sum);
     float *to = a.part ? a.part + (((size_t)block * a.n_kv_heads + kvh) * a.n_splits + split) * part_floats(kRowTile, DH) : nullptr;
-    if (wave == 0 && half == 0) {
+    if (wave == 0 && half == 0 && r.live) {   // (beyond the last row nobody asks)
         if (to) *(float2 *)(to + kRowTile * DH + 2 * m) = make_float2(top, sum);
-        else if (r.live) store_lse(a, r.row, r.head, top, sum);
+        else store_lse(a, r.row, r.head, top, sum);
     }
     const float inv = inverse_sum(sum);
 #pragma unroll
@@ -814,66 +846,100 @@ __global__ __launch_bounds__(256, 1) void cache_attn_plain_kernel(const AttnArgs
             for (int w = 1; w < kStreamWaves; ++w) x[i] += part[w][4 * wave + i][lane];
         }
         const int dim = 32 * d + 8 * wave + 4 * half;
+        if (!r.live) continue;
         if (to) *(f32x4 *)(to + m * DH + dim) = x;
-        else if (r.live) store_out4(a, DH, r.row, r.head, dim, x * inv);
+        else store_out4(a, DH, r.row, r.head, dim, x * inv);
     }
 }
 
 // ------------------------------------------------------------------ the splits meet
 //
-// Block = (32 virtual rows, kv head): four adjacent dims of a row per thread, the splits in their order.
-// row_block: rows of the blocks that were split; tile: keys of their tiles.   grid: n_kv_heads * n_blocks * (row_block / 32)
+// Block = a row: four adjacent dims per thread, the splits dealt to the block's groups of DH / 4 threads, whose sums meet in LDS in
+// their order.  (With a block for all rows of a key / value head and the splits one after the other a token behind 65535 positions
+// waited 23 us for 128 of them.)   row_block: rows of the blocks that were split; tile: keys of their tiles.
+// grid: n_kv_heads * n_blocks * row_block
 template <int DH>
-__global__ __launch_bounds__(256) void cache_attn_join_kernel(const AttnArgs a, int row_block, int tile, int rules)
+__global__ __launch_bounds__(256) void cache_attn_join_kernel(const AttnArgs a, int row_block, int tile)
 {
-    constexpr int TPR = DH / 4, RPP = 256 / TPR;   // threads of a row, rows at a time
-    const int per = row_block / kRowTile;
-    const int kvh = blockIdx.x % a.n_kv_heads, sub = blockIdx.x / a.n_kv_heads % per, block = blockIdx.x / a.n_kv_heads / per;
+    constexpr int TPR = DH / 4, GROUPS = 256 / TPR;
+    __shared__ float tops[GROUPS], sums[GROUPS];
+    __shared__ f32x4 part[GROUPS][TPR];
+    const int row = blockIdx.x % row_block, rest = blockIdx.x / row_block, kvh = rest % a.n_kv_heads, block = rest / a.n_kv_heads;
     const SeqView s = a.seq[seq_of_block(a, block)];
-    const int vb = (block - s.block0) * row_block, rows = s.n * a.group;
+    const int vb = (block - s.block0) * row_block, rows = s.n * a.group, v = vb + row;
+    if (v >= rows) return;
     const int p_lo = s.pos0 + vb / a.group, p_hi = s.pos0 + (vb + row_block <= rows ? vb + row_block - 1 : rows - 1) / a.group;
-    const KeyTiles tiles = key_tiles(p_lo, p_hi, s.pos0 + s.n, rules ? a.window : 0, rules ? a.prefix : 0, tile);
+    const KeyTiles tiles = key_tiles(p_lo, p_hi, s.pos0 + s.n, a.window, a.prefix, tile);
     const int used = (tiles.n + a.chunk - 1) / a.chunk;
     const size_t stride = part_floats(row_block, DH);
     const float *from = a.part + ((size_t)block * a.n_kv_heads + kvh) * a.n_splits * stride;
-    for (int i = 0; i < kRowTile; i += RPP) {
-        const int row = kRowTile * sub + i + (int)threadIdx.x / TPR, dim = (int)threadIdx.x % TPR * 4, v = vb + row;
-        if (v >= rows) continue;
-        const float *ml = from + row_block * DH + 2 * row, *o = from + row * DH + dim;
-        float top = kNoKey;
-        for (int k = 0; k < used; ++k) top = fmaxf(top, ml[k * stride]);
-        float sum = 0.f;
-        f32x4 x = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-        for (int k = 0; k < used; ++k) {
-            const float2 t = *(const float2 *)(ml + k * stride);
-            const float f = __builtin_amdgcn_exp2f(t.x - top);
-            sum = fmaf(t.y, f, sum);
-            x += *(const f32x4 *)(o + k * stride) * f;
+    const int group = threadIdx.x / TPR, d = threadIdx.x % TPR;
+    const float *ml = from + row_block * DH + 2 * row, *o = from + row * DH + 4 * d;
+    float top = kNoKey, sum = 0.f;
+    f32x4 x = {0.f, 0.f, 0.f, 0.f};
+    // (requested side by side, four splits at a time; one that does not exist weighs nothing)
+    for (int k0 = group; k0 < used; k0 += 4 * GROUPS) {
+        float2 t[4];
+        f32x4 y[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int k = k0 + u * GROUPS < used ? k0 + u * GROUPS : k0;
+            t[u] = *(const float2 *)(ml + k * stride);
+            y[u] = *(const f32x4 *)(o + k * stride);
         }
-        const int r = v / a.group, out_row = s.row0 + r, head = kvh * a.group + (v - r * a.group);
-        if (dim == 0) store_lse(a, out_row, head, top, sum);
-        store_out4(a, DH, out_row, head, dim, x * inverse_sum(sum));
+        float t0 = top;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) t0 = fmaxf(t0, t[u].x);
+        const float f0 = __builtin_amdgcn_exp2f(top - t0);
+        top = t0;
+        sum *= f0;
+        x = x * f0;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            if (k0 + u * GROUPS >= used) continue;
+            const float f = __builtin_amdgcn_exp2f(t[u].x - t0);
+            sum = fmaf(t[u].y, f, sum);
+            x += y[u] * f;
+        }
     }
+    if (d == 0) { tops[group] = top; sums[group] = sum; }
+    part[group][d] = x;
+    __syncthreads();
+    if (group > 0) return;
+    float all = tops[0];
+#pragma unroll
+    for (int g = 1; g < GROUPS; ++g) all = fmaxf(all, tops[g]);
+    sum = 0.f;
+    x = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int g = 0; g < GROUPS; ++g) {
+        const float f = __builtin_amdgcn_exp2f(tops[g] - all);
+        sum = fmaf(sums[g], f, sum);
+        x += part[g][d] * f;
+    }
+    const int r = v / a.group, out_row = s.row0 + r, head = kvh * a.group + (v - r * a.group);
+    if (d == 0) store_lse(a, out_row, head, all, sum);
+    store_out4(a, DH, out_row, head, 4 * d, x * inverse_sum(sum));
 }
 
 // ------------------------------------------------------------------ the weight of every key
 //
-// Block = (128 keys, kv head, part of the rows), four waves of 32 keys, whose operands a wave holds in registers while the rows go by
-// in tiles of 32 through LDS (fp32 rows are split into their terms there, once for the four waves).  A lane adds the weights of its
-// row's 16 keys to 16 sums over all tiles; the lanes meet at the end.  One block owns a key's sum, so there are no atomics and
+// Block = (128 SETS keys, kv head, part of the rows), four waves of SETS x 32 keys, whose operands a wave holds in registers while the
+// rows go by in tiles of 32 through LDS (fp32 rows are split into their terms there, once for the four waves).  A lane adds the weights
+// of its row's 16 keys per set to as many sums over all tiles; the lanes meet at the end.  Two sets use a row operand twice for
+// one read of it: with one, LDS was as busy as the matrix cores (1800 fp32 rows of 40 heads: 127 us).  One block owns a key's sum, so there are no atomics and
 // the order is always the same; where keys are too few for all compute units, the rows are dealt to several blocks whose sums are
 // added in order by a second kernel.  exp(t - lse) is formed from the difference, not from two numbers scaled to base 2 first,
 // whose roundings would stay in it.
 // a.block0 / n_blocks / n_splits / chunk: blocks of keys; parts of the rows, row tiles in each.
 // grid: n_blocks * n_splits * n_kv_heads
-constexpr int kMassKeys = 128;
+constexpr int kMassKeys = 128;   // of a block, per set
 
-// The row tiles that can see keys kb .. kb + 127: first one and one behind the last.
+// The row tiles that can see keys kb .. kb + keys - 1: first one and one behind the last.
 struct RowTiles {
     int t0, t1;
 };
-__host__ __device__ __forceinline__ RowTiles row_tiles(int kb, int pos0, int n, int group, int window, int prefix)
+__host__ __device__ __forceinline__ RowTiles row_tiles(int kb, int keys, int pos0, int n, int group, int window, int prefix)
 {
     const long long rows = (long long)n * group;
     long long v0 = 0, v1 = rows;
@@ -881,7 +947,7 @@ __host__ __device__ __forceinline__ RowTiles row_tiles(int kb, int pos0, int n, 
         v0 = (long long)(kb - pos0) * group;
         if (v0 < 0) v0 = 0;
         if (window > 0) {
-            v1 = ((long long)kb + kMassKeys - 1 + window - pos0) * group;
+            v1 = ((long long)kb + keys - 1 + window - pos0) * group;
             if (v1 > rows) v1 = rows;
         }
     }
@@ -922,14 +988,15 @@ __device__ __forceinline__ float meet_lanes(const f32x16 &acc, float (&red)[16][
     for (int x = 0; x < 32; ++x) sum += red[from][half * 32 + ((x + k) & 31)];   // (turned by k: every lane its own bank)
     return sum;
 }
-__device__ __forceinline__ void store_mass(const AttnArgs &a, const MassOut &to, int seq, int total, int kvh, int block, int split, int key, float sum)
+// k: key of the block, key: of the sequence
+__device__ __forceinline__ void store_mass(const AttnArgs &a, const MassOut &to, int seq, int total, int kvh, int block, int split, int keys, int k, int key, float sum)
 {
-    if (a.part) a.part[(((size_t)block * a.n_kv_heads + kvh) * a.n_splits + split) * kMassKeys + key % kMassKeys] = sum;
+    if (a.part) a.part[(((size_t)block * a.n_kv_heads + kvh) * a.n_splits + split) * keys + k] = sum;
     else if (key < total) to.mass[seq][(size_t)kvh * to.ld + key] += sum;
 }
 
-template <int DH, int TERMS, bool RULES>
-__global__ __launch_bounds__(256, TERMS == 1 ? 2 : 1) void cache_mass_kernel(const AttnArgs a, const MassOut to)
+template <int DH, int TERMS, bool RULES, int SETS>
+__global__ __launch_bounds__(256, 2) void cache_mass_kernel(const AttnArgs a, const MassOut to)
 {
     constexpr int NKS = DH / 16, UNITS = NKS * 64 / 256;   // pieces of eight dims of a row tile per thread
     __shared__ union {
@@ -940,20 +1007,21 @@ __global__ __launch_bounds__(256, TERMS == 1 ? 2 : 1) void cache_mass_kernel(con
     const int kvh = blockIdx.x % a.n_kv_heads, rest = blockIdx.x / a.n_kv_heads;
     const int split = rest % a.n_splits, block = rest / a.n_splits, seq = seq_of_block(a, block);
     const SeqView s = a.seq[seq];
-    const int kb = (block - s.block0) * kMassKeys, base = kb + 32 * wave, total = s.pos0 + s.n;
+    const int kb = (block - s.block0) * (kMassKeys * SETS), base = kb + 32 * SETS * wave, total = s.pos0 + s.n;
     const int pre = RULES && a.prefix > 0 ? (a.prefix < total ? a.prefix : total) : 0;
-    const RowTiles tiles = row_tiles(kb, s.pos0, s.n, a.group, RULES ? a.window : 0, pre);
+    const RowTiles tiles = row_tiles(kb, kMassKeys * SETS, s.pos0, s.n, a.group, RULES ? a.window : 0, pre);
     const int t0 = tiles.t0 + split * a.chunk, t1 = t0 + a.chunk < tiles.t1 ? t0 + a.chunk : tiles.t1;
     if (t0 >= tiles.t1) return;   // (the whole block)
 
-    u32x4 kf[NKS];
-    {
-        const int last_page = (total - 1) >> 4, page = (base >> 4) + ((lane >> 4) & 1);
+    u32x4 kf[SETS][NKS];
+#pragma unroll
+    for (int x = 0; x < SETS; ++x) {
+        const int last_page = (total - 1) >> 4, page = ((base + 32 * x) >> 4) + ((lane >> 4) & 1);
         const int id = s.table[page < last_page ? page : last_page];
         const bf16_t *pool = (const bf16_t *)s.pool + kvf_base(id, a.layer, a.n_layers, 0, kvh, a.n_kv_heads, DH);
         const u32x4 *p = (const u32x4 *)pool + half * 16 + (lane & 15);
 #pragma unroll
-        for (int ks = 0; ks < NKS; ++ks) kf[ks] = p[(ks >> 1) * 64 + (ks & 1) * 32];
+        for (int ks = 0; ks < NKS; ++ks) kf[x][ks] = p[(ks >> 1) * 64 + (ks & 1) * 32];
     }
     // what the next tile is made of: its rows' pieces, and every lane's row
     u32x4 piece[UNITS][TERMS];
@@ -973,7 +1041,7 @@ __global__ __launch_bounds__(256, TERMS == 1 ? 2 : 1) void cache_mass_kernel(con
 #pragma unroll
             for (int k = 0; k < TERMS; ++k) lds.q[buf][k][wave + 4 * u][lane] = piece[u][k];
     };
-    f32x16 acc = {};
+    f32x16 acc[SETS] = {};
     request(t0);
     put(0);
     for (int t = t0; t < t1; ++t) {
@@ -982,19 +1050,31 @@ __global__ __launch_bounds__(256, TERMS == 1 ? 2 : 1) void cache_mass_kernel(con
         const float lse = lse_next;
         __syncthreads();
         if (t + 1 < t1) request(t + 1);
-        if (base < total && any_seen<RULES>(r, pre, base)) {
-            f32x16 sc = {};
+        bool seen = false;
+#pragma unroll
+        for (int x = 0; x < SETS; ++x) seen = seen || (base + 32 * x < total && any_seen<RULES>(r, pre, base + 32 * x));
+        if (seen) {
+            f32x16 sc[SETS] = {};
 #pragma unroll
             for (int k = TERMS - 1; k >= 0; --k)
 #pragma unroll
-                for (int ks = 0; ks < NKS; ++ks) sc = mfma32(as_bf16(kf[ks]), as_bf16(lds.q[buf][k][ks][lane]), sc);
-            add_weights<RULES>(a, r, lse, pre, base, sc, acc);
+                for (int ks = 0; ks < NKS; ++ks) {
+                    const bf16x8 q = as_bf16(lds.q[buf][k][ks][lane]);
+#pragma unroll
+                    for (int x = 0; x < SETS; ++x) sc[x] = mfma32(as_bf16(kf[x][ks]), q, sc[x]);
+                }
+#pragma unroll
+            for (int x = 0; x < SETS; ++x) add_weights<RULES>(a, r, lse, pre, base + 32 * x, sc[x], acc[x]);
         }
         if (t + 1 < t1) put(buf ^ 1);
     }
-    __syncthreads();
-    const float sum = meet_lanes(acc, lds.red[wave]);
-    if (half == 0) store_mass(a, to, seq, total, kvh, block, split, base + m, sum);
+#pragma unroll
+    for (int x = 0; x < SETS; ++x) {
+        __syncthreads();
+        const float sum = meet_lanes(acc[x], lds.red[wave]);
+        const int k = 32 * (SETS * wave + x) + m;
+        if (half == 0) store_mass(a, to, seq, total, kvh, block, split, kMassKeys * SETS, k, kb + k, sum);
+    }
 }
 
 // The same for caches in plain order (exact fp32 products).
@@ -1012,7 +1092,7 @@ __global__ __launch_bounds__(256, 1) void cache_mass_plain_kernel(const AttnArgs
     const SeqView s = a.seq[seq];
     const int kb = (block - s.block0) * kMassKeys, base = kb + 32 * wave, total = s.pos0 + s.n, pt = a.page_tokens;
     const int pre = a.prefix > 0 ? (a.prefix < total ? a.prefix : total) : 0;
-    const RowTiles tiles = row_tiles(kb, s.pos0, s.n, a.group, a.window, pre);
+    const RowTiles tiles = row_tiles(kb, kMassKeys, s.pos0, s.n, a.group, a.window, pre);
     const int t0 = tiles.t0 + split * a.chunk, t1 = t0 + a.chunk < tiles.t1 ? t0 + a.chunk : tiles.t1;
     if (t0 >= tiles.t1) return;   // (the whole block)
     float k[DH / 2];
@@ -1061,22 +1141,22 @@ __global__ __launch_bounds__(256, 1) void cache_mass_plain_kernel(const AttnArgs
     }
     __syncthreads();
     const float sum = meet_lanes(acc, lds.red[wave]);
-    if (half == 0) store_mass(a, to, seq, total, kvh, block, split, base + m, sum);
+    if (half == 0) store_mass(a, to, seq, total, kvh, block, split, kMassKeys, 32 * wave + m, base + m, sum);
 }
 
-// The parts of the rows meet, in their order.   grid: n_blocks * n_kv_heads
-__global__ __launch_bounds__(kMassKeys) void cache_mass_join_kernel(const AttnArgs a, const MassOut to)
+// The parts of the rows meet, in their order.   grid: n_blocks * n_kv_heads, a thread per key of the block
+__global__ void cache_mass_join_kernel(const AttnArgs a, const MassOut to)
 {
-    const int kvh = blockIdx.x % a.n_kv_heads, block = blockIdx.x / a.n_kv_heads, seq = seq_of_block(a, block);
+    const int kvh = blockIdx.x % a.n_kv_heads, block = blockIdx.x / a.n_kv_heads, seq = seq_of_block(a, block), keys = blockDim.x;
     const SeqView s = a.seq[seq];
-    const int kb = (block - s.block0) * kMassKeys, total = s.pos0 + s.n, key = kb + (int)threadIdx.x;
+    const int kb = (block - s.block0) * keys, total = s.pos0 + s.n, key = kb + (int)threadIdx.x;
     const int pre = a.prefix < total ? a.prefix : total;
-    const RowTiles tiles = row_tiles(kb, s.pos0, s.n, a.group, a.window, pre);
+    const RowTiles tiles = row_tiles(kb, keys, s.pos0, s.n, a.group, a.window, pre);
     const int used = (tiles.t1 - tiles.t0 + a.chunk - 1) / a.chunk;
-    const float *from = a.part + ((size_t)block * a.n_kv_heads + kvh) * a.n_splits * kMassKeys + threadIdx.x;
+    const float *from = a.part + ((size_t)block * a.n_kv_heads + kvh) * a.n_splits * keys + threadIdx.x;
     float sum = 0.f;
 #pragma unroll 4
-    for (int k = 0; k < used; ++k) sum += from[(size_t)k * kMassKeys];
+    for (int k = 0; k < used; ++k) sum += from[(size_t)k * keys];
     if (key < total && used > 0) to.mass[seq][(size_t)kvh * to.ld + key] += sum;
 }
 

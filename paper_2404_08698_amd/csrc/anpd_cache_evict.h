@@ -27,38 +27,104 @@ struct SelectArgs {
     int32_t len, keep, first, last;
 };
 
-// Block = (layer, head).  The smallest rank that stays is found a byte at a time from the top (a histogram of the candidates'
-// next byte in LDS, whole numbers, so the order of the counts does not matter); then every wave counts what stays of its stretch of
-// positions, the counts are summed over the waves, and each wave writes its own.
+// Block = (layer, head); a wave has a stretch of whole 64s of positions.  What stays in any case has the highest rank of all, so that
+// one search finds the smallest rank that stays; then every wave counts what stays of its stretch, the counts are summed over the
+// waves, and each wave writes its own.
+// HELD: positions per lane, whose ranks stay in registers: the search goes bit by bit, a comparison and a count of the lanes per 64 positions,
+// and ends as soon as a rank separates as many as are wanted.  HELD = 0 (beyond 65536 positions): byte by byte, each time with a
+// histogram of the candidates' next byte in LDS (whole numbers: the order of the counts does not matter), for which all is
+// read again.  8 heads of 65536 positions took 132 us so, 60 of them in instructions around the histogram's.
 // grid: n_layers * n_kv_heads
+template <int HELD>
 __global__ __launch_bounds__(kSelectThreads) void cache_select_kernel(const SelectArgs a)
 {
     __shared__ uint32_t bins[256], above[kSelectWaves], equal[kSelectWaves], choice[2];
+    __shared__ uint4 counts[2][kSelectWaves / 4];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const float *mass = a.mass + (size_t)blockIdx.x * a.ld;
     int32_t *kept = a.kept + (size_t)blockIdx.x * a.keep;
     float *out = a.out_mass ? a.out_mass + (size_t)blockIdx.x * a.ld_out : nullptr;
-    const int lo = a.first, hi = a.len - a.last;
-    const uint32_t want = (uint32_t)(a.keep - a.first - a.last);   // of the positions lo .. hi - 1
+    const uint32_t want = (uint32_t)a.keep;
+    const int steps = (a.len + kSelectThreads - 1) / kSelectThreads, p0 = wave * steps * 64;   // positions p0 + 64 k + lane, k < steps
+    // (a position behind the last one has the lowest rank and comes last among those: it never stays)
+    const int p1 = p0 + 64 * steps < a.len ? p0 + 64 * steps : a.len;
+    auto load = [&](int k) __attribute__((always_inline)) {
+        const int i = p0 + 64 * k + lane;
+        return mass[i < a.len ? i : a.len - 1];
+    };
+    auto rank_of = [&](int k, float x) __attribute__((always_inline)) {
+        const int i = p0 + 64 * k + lane;
+        return i >= p1 ? 0u : (i < a.first || i >= a.len - a.last ? ~0u : mass_rank(x));
+    };
+    uint32_t held[HELD > 0 ? HELD : 1];
+#pragma unroll
+    for (int k = 0; k < HELD; ++k) held[k] = __float_as_uint(load(k));
+#pragma unroll
+    for (int k = 0; k < HELD; ++k) {
+        held[k] = rank_of(k, __uint_as_float(held[k]));
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    // fn(position, rank) for the wave's stretch, 64 positions at a time
+    auto each = [&](auto fn) __attribute__((always_inline)) {
+        if constexpr (HELD > 0) {
+#pragma unroll
+            for (int k = 0; k < HELD; ++k) {
+                if (k < steps) fn(p0 + 64 * k + lane, held[k]);   // (the same for the whole wave)
+                __builtin_amdgcn_sched_barrier(0);   // (one after the other: the ranks fill the registers)
+            }
+        } else {
+            for (int k0 = 0; k0 < steps; k0 += 8) {
+                uint32_t y[8];
+#pragma unroll
+                for (int u = 0; u < 8; ++u) y[u] = __float_as_uint(load(k0 + u));
+#pragma unroll
+                for (int u = 0; u < 8; ++u) y[u] = rank_of(k0 + u, __uint_as_float(y[u]));
+#pragma unroll
+                for (int u = 0; u < 8; ++u)
+                    if (k0 + u < steps) fn(p0 + 64 * (k0 + u) + lane, y[u]);
+            }
+        }
+    };
     uint32_t limit = 0, left = want;   // ranks above `limit` stay, and `left` of those equal to it
-    if (want > 0) {
+    if constexpr (HELD > 0) {
+        for (int bit = 31; bit >= 0; --bit) {
+            const uint32_t t = limit | (1u << bit);
+            uint32_t n = 0;
+#pragma unroll
+            for (int k = 0; k < HELD; ++k) {
+                n += (uint32_t)__builtin_popcountll(__builtin_amdgcn_ballot_w64(held[k] >= t));
+                if (k % 4 == 3) asm volatile("" : "+s"(n));   // (all comparisons first would be more than the scalar registers hold)
+            }
+            if (lane == 0) ((uint32_t *)counts[bit & 1])[wave] = n;
+            __syncthreads();   // (the other half of the counts is read until the next one)
+            uint32_t total = 0;
+#pragma unroll
+            for (int w = 0; w < kSelectWaves / 4; ++w) { const uint4 c = counts[bit & 1][w]; total += (c.x + c.y) + (c.z + c.w); }
+            total = (uint32_t)__builtin_amdgcn_readfirstlane((int)total);
+            if (total == want) {   // (the same for all)
+                limit = t - 1;
+                left = 0;
+                break;
+            }
+            if (total > want) limit = t;
+            else left = want - total;   // (of the ranks above the limit that is found in the end, this many are missing)
+        }
+    } else {
         for (int shift = 24; shift >= 0; shift -= 8) {
-            for (int i = tid; i < 256; i += kSelectThreads) bins[i] = 0;
+            if (tid < 256) bins[tid] = 0;
             __syncthreads();
             const uint32_t mask = shift == 24 ? 0u : ~0u << (shift + 8);
-            for (int i0 = lo + wave * 64; i0 < hi; i0 += kSelectThreads) {
-                const int i = i0 + lane;
-                const uint32_t rank = i < hi ? mass_rank(mass[i]) : 0;
-                const bool in = i < hi && (rank & mask) == limit;
+            each([&](int i, uint32_t rank) __attribute__((always_inline)) {
+                const bool in = (rank & mask) == limit && i < a.len;
                 const uint32_t bin = (rank >> shift) & 255u;
                 // (the first candidate's bin at once for all lanes that share it: positions that nothing looked at are all 0)
                 const unsigned long long some = __builtin_amdgcn_ballot_w64(in);
-                if (some == 0) continue;
+                if (some == 0) return;
                 const uint32_t one = (uint32_t)__builtin_amdgcn_readlane((int)bin, __builtin_ctzll(some));
                 const unsigned long long same = __builtin_amdgcn_ballot_w64(in && bin == one);
                 if (lane == 0) atomicAdd(&bins[one], (uint32_t)__builtin_popcountll(same));
                 if (in && bin != one) atomicAdd(&bins[bin], 1u);
-            }
+            });
             __syncthreads();
             if (wave == 0) {
                 // from the top bin down: the one in which the `left`th candidate lies.  Lane: four bins, the highest first.
@@ -80,44 +146,66 @@ __global__ __launch_bounds__(kSelectThreads) void cache_select_kernel(const Sele
             left = choice[1];
         }
     }
-    // stretches of whole 64s
-    const int each = ((a.len + kSelectWaves - 1) / kSelectWaves + 63) / 64 * 64, p0 = wave * each, p1 = p0 + each < a.len ? p0 + each : a.len;
-    auto look = [&](int i, bool &gt, bool &eq, float &x) __attribute__((always_inline)) {
-        const bool in = i < p1;
-        x = in ? mass[i] : 0.f;
-        const bool middle = in && i >= lo && i < hi;
-        const uint32_t rank = mass_rank(x);
-        gt = (in && !middle) || (middle && want > 0 && rank > limit);
-        eq = middle && want > 0 && rank == limit;
-    };
     uint32_t n_gt = 0, n_eq = 0;
-    for (int i0 = p0; i0 < p1; i0 += 64) {
-        bool gt, eq;
-        float x;
-        look(i0 + lane, gt, eq, x);
-        n_gt += (uint32_t)__builtin_popcountll(__builtin_amdgcn_ballot_w64(gt));
-        n_eq += (uint32_t)__builtin_popcountll(__builtin_amdgcn_ballot_w64(eq));
-    }
+    each([&](int, uint32_t rank) __attribute__((always_inline)) {
+        n_gt += (uint32_t)__builtin_popcountll(__builtin_amdgcn_ballot_w64(rank > limit));
+        n_eq += (uint32_t)__builtin_popcountll(__builtin_amdgcn_ballot_w64(rank == limit));
+        asm volatile("" : "+s"(n_gt), "+s"(n_eq));
+    });
     if (lane == 0) { above[wave] = n_gt; equal[wave] = n_eq; }
     __syncthreads();
     uint32_t at = 0, ties = 0;
     for (int w = 0; w < wave; ++w) { at += above[w]; ties += equal[w]; }
     at += ties < left ? ties : left;
+    limit = (uint32_t)__builtin_amdgcn_readfirstlane((int)limit);
+    int from = lane;
+    asm volatile("" : "+s"(limit), "+v"(from));   // (comparisons and addresses are made again: those of above would fill the registers)
     const unsigned long long below = (1ull << lane) - 1;
-    for (int i0 = p0; i0 < p1; i0 += 64) {
-        bool gt, eq;
-        float x;
-        look(i0 + lane, gt, eq, x);
-        const unsigned long long e = __builtin_amdgcn_ballot_w64(eq);
-        const bool stays = gt || (eq && ties + (uint32_t)__builtin_popcountll(e & below) < left);
-        const unsigned long long g = __builtin_amdgcn_ballot_w64(stays);
-        if (stays) {
-            const uint32_t to = at + (uint32_t)__builtin_popcountll(g & below);
-            kept[to] = i0 + lane;
-            if (out) out[to] = x;
+    // (eight times 64 positions side by side: the masses that go along are loads)
+    constexpr int BATCH = HELD > 0 && HELD < 8 ? HELD : 8;
+    auto write = [&](int k0, const uint32_t (&rank)[BATCH]) __attribute__((always_inline)) {
+        uint32_t to[BATCH];
+        float x[BATCH];
+#pragma unroll
+        for (int u = 0; u < BATCH; ++u) {
+            const bool tie = rank[u] == limit && k0 + u < steps;
+            const unsigned long long e = __builtin_amdgcn_ballot_w64(tie);
+            const bool stays = (rank[u] > limit && k0 + u < steps) || (tie && ties + (uint32_t)__builtin_popcountll(e & below) < left);
+            const unsigned long long g = __builtin_amdgcn_ballot_w64(stays);
+            to[u] = stays ? at + (uint32_t)__builtin_popcountll(g & below) : ~0u;
+            at += (uint32_t)__builtin_popcountll(g);
+            ties += (uint32_t)__builtin_popcountll(e);
         }
-        at += (uint32_t)__builtin_popcountll(g);
-        ties += (uint32_t)__builtin_popcountll(e);
+        if (out) {
+#pragma unroll
+            for (int u = 0; u < BATCH; ++u) x[u] = to[u] != ~0u ? mass[p0 + 64 * (k0 + u) + from] : 0.f;
+        }
+#pragma unroll
+        for (int u = 0; u < BATCH; ++u) {
+            if (to[u] == ~0u) continue;
+            kept[to[u]] = p0 + 64 * (k0 + u) + from;
+            if (out) out[to[u]] = x[u];
+        }
+    };
+    if constexpr (HELD > 0) {
+#pragma unroll
+        for (int k0 = 0; k0 < HELD; k0 += BATCH) {
+            if (k0 >= steps) break;   // (the same for the whole wave)
+            uint32_t rank[BATCH];
+#pragma unroll
+            for (int u = 0; u < BATCH; ++u) rank[u] = held[k0 + u];
+            write(k0, rank);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    } else {
+        for (int k0 = 0; k0 < steps; k0 += BATCH) {
+            uint32_t rank[BATCH];
+#pragma unroll
+            for (int u = 0; u < BATCH; ++u) rank[u] = __float_as_uint(load(k0 + u));
+#pragma unroll
+            for (int u = 0; u < BATCH; ++u) rank[u] = rank_of(k0 + u, __uint_as_float(rank[u]));
+            write(k0, rank);
+        }
     }
 }
 
@@ -131,11 +219,17 @@ struct MoveArgs {
 
 constexpr int kMoveThreads = 512, kMovePages = 8;   // pages of 16 tokens at a time
 
-// cos and sin of the turn by `moved` positions, the angle reduced in 64 bits
-__device__ __forceinline__ void turn_of(const MoveArgs &a, int moved, int pair, float &c, float &s)
+// cos and sin of the turn by `moved` positions, the angle reduced in 64 bits.  ROUGH: by the hardware's functions of a turn, to about
+// 2^-20, for keys that are rounded to bf16 behind it.
+template <bool ROUGH>
+__device__ __forceinline__ void turn_of(double turn, int moved, float &c, float &s)
 {
-    const double t = (double)moved * a.turn[pair];
-    sincospif((float)(2.0 * (t - rint(t))), &s, &c);
+    const double t = (double)moved * turn;
+    const float f = (float)(t - rint(t));
+    if (ROUGH) {
+        c = __builtin_amdgcn_cosf(f);
+        s = __builtin_amdgcn_sinf(f);
+    } else sincospif(2.f * f, &s, &c);
 }
 
 // The cache in matrix-core order.  Block = (layer, head; keys or values; every gridDim.z-th group of eight pages): all that goes into the
@@ -187,7 +281,7 @@ __global__ __launch_bounds__(kMoveThreads) void cache_move_kernel(const MoveArgs
                             const float x0 = e ? __uint_as_float(l[w] & 0xffff0000u) : __uint_as_float(l[w] << 16);
                             const float x1 = e ? __uint_as_float(h[w] & 0xffff0000u) : __uint_as_float(h[w] << 16);
                             float cs, sn;
-                            turn_of(a, to - p, 8 * c + 2 * w + e, cs, sn);
+                            turn_of<true>(a.turn[8 * c + 2 * w + e], to - p, cs, sn);
                             r[0][e] = x0 * cs - x1 * sn;   // (the cache's own type is what there is room for)
                             r[1][e] = x1 * cs + x0 * sn;
                         }
@@ -258,7 +352,7 @@ __global__ __launch_bounds__(kMoveThreads) void cache_move_plain_kernel(const Mo
             KT *put = dst + kv_offset(a.dst_table[to / pt], layer, a.n_layers, kind, head, a.n_kv_heads, to % pt, pt, DH);
             if (kind == 0 && a.rotate && p != to) {
                 float cs, sn;
-                turn_of(a, to - p, i, cs, sn);
+                turn_of<sizeof(KT) == 2>(a.turn[i], to - p, cs, sn);
                 const float x0 = load_f32(&lo[u], 0), x1 = load_f32(&hi[u], 0);
                 store_kv(put, i, x0 * cs - x1 * sn);
                 store_kv(put, i + PAIRS, x1 * cs + x0 * sn);

@@ -170,8 +170,8 @@ int32_t launch_attention(const AttnArgs &a, const Plan &p, const CacheShape &c, 
     }
     HIP_TRY(hipGetLastError());
     if (a.part) {
-        hipLaunchKernelGGL((cache_attn_join_kernel<DH>), dim3((unsigned)((int64_t)a.n_blocks * a.n_kv_heads * (p.row_block / kRowTile))), dim3(256), 0, st, a,
-                           p.row_block, p.key_tile, rules ? 1 : 0);
+        hipLaunchKernelGGL((cache_attn_join_kernel<DH>), dim3((unsigned)((int64_t)a.n_blocks * a.n_kv_heads * p.row_block)), dim3(256), 0, st, a, p.row_block,
+                           p.key_tile);
         HIP_TRY(hipGetLastError());
     }
     return ANPD_OK;
@@ -179,46 +179,63 @@ int32_t launch_attention(const AttnArgs &a, const Plan &p, const CacheShape &c, 
 
 // ---- key mass: how the work is divided
 
-size_t plan_mass(AttnArgs &a, int n_cu)
+// Sets the key blocks of a's sequences and the parts of their rows.  sets: 32-key sets per wave.
+size_t plan_mass(AttnArgs &a, const CacheShape &c, int n_cu, int &sets)
 {
-    a.n_blocks = 0;
-    int most = 0;   // row tiles of a block of keys
-    for (int s = 0; s < a.n_seq; ++s) {
-        SeqView &v = a.seq[s];
-        v.block0 = a.n_blocks;
-        if (v.n == 0) continue;
-        const int total = v.pos0 + v.n, pre = a.prefix < total ? a.prefix : total, blocks = (total + kMassKeys - 1) / kMassKeys;
-        a.n_blocks += blocks;
-        for (int b = 0; b < blocks; ++b) {
-            const RowTiles t = row_tiles(b * kMassKeys, v.pos0, v.n, a.group, a.window, pre);
-            if (t.t1 - t.t0 > most) most = t.t1 - t.t0;
+    // most row tiles of a block of keys, and all of them together
+    int most;
+    int64_t all;
+    auto count = [&](int keys) {
+        a.n_blocks = most = 0;
+        all = 0;
+        for (int s = 0; s < a.n_seq; ++s) {
+            SeqView &v = a.seq[s];
+            v.block0 = a.n_blocks;
+            if (v.n == 0) continue;
+            const int total = v.pos0 + v.n, pre = a.prefix < total ? a.prefix : total, blocks = (total + keys - 1) / keys;
+            a.n_blocks += blocks;
+            for (int b = 0; b < blocks; ++b) {
+                const RowTiles t = row_tiles(b * keys, keys, v.pos0, v.n, a.group, a.window, pre);
+                all += t.t1 - t.t0;
+                if (t.t1 - t.t0 > most) most = t.t1 - t.t0;
+            }
         }
+    };
+    sets = 1;
+    count(kMassKeys);
+    // two sets where the rows are many: the operand of a tile is then shared by twice the keys
+    if (c.fragments && most >= 16) {
+        sets = 2;
+        count(2 * kMassKeys);
     }
-    const int64_t items = (int64_t)a.n_blocks * a.n_kv_heads;
-    int64_t splits = items > 0 ? (2 * n_cu + items - 1) / items : 1;
-    if (splits > most / 4) splits = most / 4;
-    if (splits < 1) splits = 1;
-    a.chunk = most > 0 ? (int)((most + splits - 1) / splits) : 1;
+    // parts of at least eight tiles, six for each compute unit: later blocks have fewer rows than earlier ones
+    int64_t chunk = (all * a.n_kv_heads + 6 * n_cu - 1) / (6 * n_cu);
+    if (chunk < 8) chunk = 8;
+    a.chunk = chunk < most ? (int)chunk : (most > 0 ? most : 1);
     a.n_splits = most > 0 ? (most + a.chunk - 1) / a.chunk : 1;
-    return a.n_splits > 1 ? align_up((size_t)items * a.n_splits * kMassKeys * sizeof(float)) : 0;
+    return a.n_splits > 1 ? align_up((size_t)a.n_blocks * a.n_kv_heads * a.n_splits * kMassKeys * sets * sizeof(float)) : 0;
 }
 
+template <int DH, int SETS>
+void launch_mass_fragments(const AttnArgs &a, const MassOut &to, dim3 grid, hipStream_t st)
+{
+    const bool rules = ruled(a);
+    if (a.q_f32) {
+        if (rules) hipLaunchKernelGGL((cache_mass_kernel<DH, 3, true, SETS>), grid, dim3(256), 0, st, a, to);
+        else hipLaunchKernelGGL((cache_mass_kernel<DH, 3, false, SETS>), grid, dim3(256), 0, st, a, to);
+    } else if (rules) hipLaunchKernelGGL((cache_mass_kernel<DH, 1, true, SETS>), grid, dim3(256), 0, st, a, to);
+    else hipLaunchKernelGGL((cache_mass_kernel<DH, 1, false, SETS>), grid, dim3(256), 0, st, a, to);
+}
 template <int DH>
-int32_t launch_mass(const AttnArgs &a, const MassOut &to, const CacheShape &c, hipStream_t st)
+int32_t launch_mass(const AttnArgs &a, const MassOut &to, const CacheShape &c, int sets, hipStream_t st)
 {
     const dim3 grid((unsigned)((int64_t)a.n_blocks * a.n_splits * a.n_kv_heads));
-    const bool rules = ruled(a);
-    if (c.fragments) {
-        if (a.q_f32) {
-            if (rules) hipLaunchKernelGGL((cache_mass_kernel<DH, 3, true>), grid, dim3(256), 0, st, a, to);
-            else hipLaunchKernelGGL((cache_mass_kernel<DH, 3, false>), grid, dim3(256), 0, st, a, to);
-        } else if (rules) hipLaunchKernelGGL((cache_mass_kernel<DH, 1, true>), grid, dim3(256), 0, st, a, to);
-        else hipLaunchKernelGGL((cache_mass_kernel<DH, 1, false>), grid, dim3(256), 0, st, a, to);
-    } else if (c.dtype == ANPD_BF16) hipLaunchKernelGGL((cache_mass_plain_kernel<bf16_t, DH>), grid, dim3(256), 0, st, a, to);
+    if (c.fragments) { if (sets == 2) launch_mass_fragments<DH, 2>(a, to, grid, st); else launch_mass_fragments<DH, 1>(a, to, grid, st); }
+    else if (c.dtype == ANPD_BF16) hipLaunchKernelGGL((cache_mass_plain_kernel<bf16_t, DH>), grid, dim3(256), 0, st, a, to);
     else hipLaunchKernelGGL((cache_mass_plain_kernel<float, DH>), grid, dim3(256), 0, st, a, to);
     HIP_TRY(hipGetLastError());
     if (a.part) {
-        hipLaunchKernelGGL(cache_mass_join_kernel, dim3((unsigned)((int64_t)a.n_blocks * a.n_kv_heads)), dim3(kMassKeys), 0, st, a, to);
+        hipLaunchKernelGGL(cache_mass_join_kernel, dim3((unsigned)((int64_t)a.n_blocks * a.n_kv_heads)), dim3(kMassKeys * sets), 0, st, a, to);
         HIP_TRY(hipGetLastError());
     }
     return ANPD_OK;
@@ -313,7 +330,8 @@ size_t anpd_key_mass_workspace_bytes(const anpd_kv_t *const *kvs, int32_t n_seq,
     AttnArgs a;
     int64_t rows;
     if (gather("anpd_key_mass_workspace_bytes", kvs, n_seq, n_rows, pos0, rules, a, rows) != ANPD_OK) return 0;
-    return plan_mass(a, kvs[0]->n_cu);
+    int sets;
+    return plan_mass(a, kvs[0]->shape, kvs[0]->n_cu, sets);
 }
 
 int32_t anpd_key_mass(const anpd_kv_t *const *kvs, int32_t n_seq, const int32_t *n_rows, const int32_t *pos0, int32_t layer, const void *q, int64_t ldq,
@@ -346,11 +364,12 @@ int32_t anpd_key_mass(const anpd_kv_t *const *kvs, int32_t n_seq, const int32_t 
         to.mass[s] = mass[s];
     }
     a.lse = const_cast<float *>(lse);   // (read only)
-    const size_t need = plan_mass(a, kvs[0]->n_cu);
+    int sets;
+    const size_t need = plan_mass(a, c, kvs[0]->n_cu, sets);
     if ((rc = workspace_of(who, a, need, workspace, workspace_bytes)) != ANPD_OK) return rc;
     OnDevice on;
     if ((rc = on.enter(who, kvs[0]->device)) != ANPD_OK) return rc;
-    return c.head_dim == 128 ? launch_mass<128>(a, to, c, (hipStream_t)stream) : launch_mass<64>(a, to, c, (hipStream_t)stream);
+    return c.head_dim == 128 ? launch_mass<128>(a, to, c, sets, (hipStream_t)stream) : launch_mass<64>(a, to, c, sets, (hipStream_t)stream);
 }
 
 int32_t anpd_kv_evict(const anpd_kv_t *src, anpd_kv_t *dst, const float *mass, int64_t ld_mass, int32_t keep, int32_t first, int32_t last, float rope_base,
@@ -378,7 +397,12 @@ int32_t anpd_kv_evict(const anpd_kv_t *src, anpd_kv_t *dst, const float *mass, i
     if (keep > 0) {
         if ((rc = ensure_pages(dst, keep, st)) != ANPD_OK) return rc;
         SelectArgs a = {mass, out_kept, out_mass, ld_mass, ld_out, len, keep, first, last};
-        hipLaunchKernelGGL(cache_select_kernel, dim3((unsigned)heads), dim3(kSelectThreads), 0, st, a);
+        const dim3 rows((unsigned)heads), threads(kSelectThreads);
+        // positions per lane: as few registers as hold them
+        if (len <= 4 * kSelectThreads) hipLaunchKernelGGL(cache_select_kernel<4>, rows, threads, 0, st, a);
+        else if (len <= 16 * kSelectThreads) hipLaunchKernelGGL(cache_select_kernel<16>, rows, threads, 0, st, a);
+        else if (len <= 64 * kSelectThreads) hipLaunchKernelGGL(cache_select_kernel<64>, rows, threads, 0, st, a);
+        else hipLaunchKernelGGL(cache_select_kernel<0>, rows, threads, 0, st, a);
         HIP_TRY(hipGetLastError());
         MoveArgs m;
         std::memset(&m, 0, sizeof(m));
