@@ -1738,12 +1738,13 @@ static int32_t kv_copy(anpd_kv *kv, int32_t layer, int32_t pos0, int32_t n, floa
     hipLaunchKernelGGL((kv_copy_kernel<KT, TO>), dim3(n), dim3(256), 0, st, (KT *)kv->pool, kv->d_table, k, v, pos0, \
                        layer, c.n_layers, c.n_kv_heads, c.head_dim, c.page_tokens)
     if (c.fragments) {
-        if (to_cache)
-            hipLaunchKernelGGL((kvf_copy_kernel<true>), dim3(n), dim3(256), 0, st, (bf16_t *)kv->pool, kv->d_table, k, v, pos0,
-                               layer, c.n_layers, c.n_kv_heads, c.head_dim);
-        else
-            hipLaunchKernelGGL((kvf_copy_kernel<false>), dim3(n), dim3(256), 0, st, (bf16_t *)kv->pool, kv->d_table, k, v, pos0,
-                               layer, c.n_layers, c.n_kv_heads, c.head_dim);
+        const dim3 grid((unsigned)((pos0 + n - 1) / 16 - pos0 / 16 + 1), (unsigned)((c.n_kv_heads * 2 * c.head_dim + 255) / 256));
+#define KVF_COPY(DH_, TO)                                                                                          \
+    hipLaunchKernelGGL((kvf_copy_kernel<DH_, TO>), grid, dim3(256), 0, st, (bf16_t *)kv->pool, kv->d_table, k, v, pos0, n, layer, c.n_layers, c.n_kv_heads)
+        if (c.head_dim == 128) { if (to_cache) KVF_COPY(128, true); else KVF_COPY(128, false); }
+        else if (to_cache) KVF_COPY(64, true);
+        else KVF_COPY(64, false);
+#undef KVF_COPY
     } else if (c.dtype == ANPD_BF16) { if (to_cache) KV_COPY(bf16_t, true); else KV_COPY(bf16_t, false); }
     else { if (to_cache) KV_COPY(float, true); else KV_COPY(float, false); }
 #undef KV_COPY
