@@ -17,6 +17,8 @@
 // rounded to bf16 for the second product (2^-9 of a weight, as much as the output's own rounding).  fp32 rows are three bf16
 // terms, 24 bits, and so are their weights: two terms keep 2^-18 of every weight, which was ten times the error of fp32 sums.
 #pragma once
+#include <type_traits>
+
 #include "anpd_layout.h"
 
 namespace anpd {
@@ -168,24 +170,30 @@ __device__ __forceinline__ float ruled_score(const AttnArgs &a, float product, f
 __device__ __forceinline__ bf16x8 as_bf16(u32x4 v) { return __builtin_bit_cast(bf16x8, v); }
 __device__ __forceinline__ f32x16 mfma32(bf16x8 x, bf16x8 y, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, y, c, 0, 0, 0); }
 
+// Two numbers as words of TERMS bf16 operands.
+template <int TERMS>
+__device__ __forceinline__ void split_pair(float x, float y, uint32_t (&t)[TERMS])
+{
+#pragma unroll
+    for (int k = 0; k < TERMS; ++k) {
+        t[k] = pack_bf16(x, y);
+        if (k + 1 < TERMS) {
+            x -= __uint_as_float(t[k] << 16);
+            y -= __uint_as_float(t[k] & 0xffff0000u);
+        }
+    }
+}
 // Eight numbers as TERMS bf16 operands that add up to them (1: rounded; 3: exact but for the smallest of numbers).
 template <int TERMS>
 __device__ __forceinline__ void split_terms(const float (&x)[8], u32x4 (&t)[TERMS])
 {
-    float r[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) r[i] = x[i];
+    for (int i = 0; i < 4; ++i) {
+        uint32_t w[TERMS];
+        split_pair<TERMS>(x[2 * i], x[2 * i + 1], w);
 #pragma unroll
-    for (int k = 0; k < TERMS; ++k)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint32_t w = pack_bf16(r[2 * i], r[2 * i + 1]);
-            t[k][i] = w;
-            if (k + 1 < TERMS) {
-                r[2 * i] -= __uint_as_float(w << 16);
-                r[2 * i + 1] -= __uint_as_float(w & 0xffff0000u);
-            }
-        }
+        for (int k = 0; k < TERMS; ++k) t[k][i] = w[k];
+    }
 }
 
 // Eight dims of a row, whatever its type and alignment.
@@ -258,16 +266,18 @@ __device__ __forceinline__ float both_halves_sum(float v)
     return __uint_as_float(x[0]) + __uint_as_float(x[1]);
 }
 
-// Products of NB x 32 keys -> weights, in place; the row's reference, sum and output move along.  Keys that the row does not
-// see have weight 0.  The reference follows the row's maximum only when that is more than 2^8 above it: weights are at most 2^8
-// then, which costs no precision, and the output is rescaled a few times instead of at every other tile.
-template <bool RULES, int NB, int NDT>
-__device__ __forceinline__ void weigh(const AttnArgs &a, const RowInfo &r, int pre, int base, f32x16 (&s)[NB], Running<NDT> &run)
+// What is multiplied with a score to have its exponent in base 2.
+template <bool RULES>
+__device__ __forceinline__ float score_factor(const AttnArgs &a)
+{
+    return RULES && (a.cap > 0.f || a.slopes) ? kLog2e : a.scale * kLog2e;
+}
+// Products of NB x 32 keys -> scores: the rules, and minus infinity for the keys that the row does not see.
+template <bool RULES, int NB>
+__device__ __forceinline__ void finish_scores(const AttnArgs &a, const RowInfo &r, int pre, int base, f32x16 (&s)[NB])
 {
     const int half = (threadIdx.x >> 5) & 1;
-    float factor = a.scale * kLog2e;
     if (RULES && (a.cap > 0.f || a.slopes)) {   // (the same for all)
-        factor = kLog2e;
 #pragma unroll
         for (int b = 0; b < NB; ++b)
 #pragma unroll
@@ -280,44 +290,78 @@ __device__ __forceinline__ void weigh(const AttnArgs &a, const RowInfo &r, int p
         for (int i = 0; i < 16; ++i)
             if (!sees<RULES>(r, pre, base + 32 * b + 8 * (i >> 2) + 4 * half + (i & 3))) s[b][i] = -INFINITY;
     }
+}
+// The row's reference with these scores: it follows the row's maximum only when that is more than 2^8 above it.  Weights are at most 2^8
+// then, which costs no precision, and the output is rescaled a few times instead of at every other tile.
+template <int NB>
+__device__ __forceinline__ float new_reference(const f32x16 (&s)[NB], float factor, float m)
+{
     float mx = -INFINITY;
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
         for (int i = 0; i < 16; i += 2) mx = fmaxf(fmaxf(mx, s[b][i]), s[b][i + 1]);
     mx = both_halves_max(mx) * factor;
-    const float m_new = mx > run.m + 8.f ? mx : run.m, alpha = __builtin_amdgcn_exp2f(run.m - m_new);
+    return mx > m + 8.f ? mx : m;
+}
+// Sum and output, which hold all weights formed so far, are moved to the new reference.
+template <int NDT>
+__device__ __forceinline__ void move_reference(Running<NDT> &run, float m_new)
+{
+    const float alpha = __builtin_amdgcn_exp2f(run.m - m_new);
     run.m = m_new;
-    // (where the reference is huge, the fused product is not the product that it was rounded from, and the difference, up to 2^-24
-    // of it, would be the largest key's exponent)
-    if (__builtin_amdgcn_ballot_w64(fabsf(m_new) > 0x1p28f) != 0) {
+    if (__builtin_amdgcn_ballot_w64(alpha != 1.f) == 0) return;   // (a factor of 1 changes nothing)
+    run.l *= alpha;
 #pragma unroll
-        for (int b = 0; b < NB; ++b)
+    for (int d = 0; d < NDT; ++d) run.o[d] = run.o[d] * alpha;
+}
+// Where a reference is huge, the fused product is not the product that it was rounded from, and the difference, up to 2^-24 of it, would
+// be the largest key's exponent: careful_weights then.  (The same for the whole wave.)
+__device__ __forceinline__ bool huge_reference(float m) { return __builtin_amdgcn_ballot_w64(fabsf(m) > 0x1p28f) != 0; }
+__device__ __forceinline__ float sum16(const f32x16 &s)
+{
+    float t[4];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                float t = s[b][i] * factor;
-                asm volatile("" : "+v"(t));
-                s[b][i] = __builtin_amdgcn_exp2f(t - m_new);
-            }
-    } else {
+    for (int i = 0; i < 4; ++i) t[i] = (s[4 * i] + s[4 * i + 1]) + (s[4 * i + 2] + s[4 * i + 3]);
+    return (t[0] + t[1]) + (t[2] + t[3]);
+}
+// Scores -> weights, in place, and their sum.
+template <int NB>
+__device__ __forceinline__ float weights(f32x16 (&s)[NB], float factor, float m)
+{
 #pragma unroll
-        for (int b = 0; b < NB; ++b)
+    for (int b = 0; b < NB; ++b)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) s[b][i] = __builtin_amdgcn_exp2f(fmaf(s[b][i], factor, -m_new));
-    }
-    float sum = 0.f;
+        for (int i = 0; i < 16; ++i) s[b][i] = __builtin_amdgcn_exp2f(fmaf(s[b][i], factor, -m));
+    float sum = sum16(s[0]);
 #pragma unroll
-    for (int b = 0; b < NB; ++b) {
-        float t[4];
+    for (int b = 1; b < NB; ++b) sum += sum16(s[b]);
+    return sum;
+}
+template <int NB>
+__device__ __forceinline__ float careful_weights(f32x16 (&s)[NB], float factor, float m)
+{
 #pragma unroll
-        for (int i = 0; i < 4; ++i) t[i] = (s[b][4 * i] + s[b][4 * i + 1]) + (s[b][4 * i + 2] + s[b][4 * i + 3]);
-        sum += (t[0] + t[1]) + (t[2] + t[3]);
-    }
-    run.l = fmaf(run.l, alpha, sum);
-    if (__builtin_amdgcn_ballot_w64(alpha != 1.f) != 0) {   // (a factor of 1 changes nothing)
+    for (int b = 0; b < NB; ++b)
 #pragma unroll
-        for (int d = 0; d < NDT; ++d) run.o[d] = run.o[d] * alpha;
-    }
+        for (int i = 0; i < 16; ++i) {
+            float t = s[b][i] * factor;
+            asm volatile("" : "+v"(t));   // (rounded here)
+            s[b][i] = __builtin_amdgcn_exp2f(t - m);
+        }
+    float sum = sum16(s[0]);
+#pragma unroll
+    for (int b = 1; b < NB; ++b) sum += sum16(s[b]);
+    return sum;
+}
+// All of it, one step after the other.
+template <bool RULES, int NB, int NDT>
+__device__ __forceinline__ void weigh(const AttnArgs &a, const RowInfo &r, int pre, int base, f32x16 (&s)[NB], Running<NDT> &run)
+{
+    const float factor = score_factor<RULES>(a);
+    finish_scores<RULES, NB>(a, r, pre, base, s);
+    move_reference(run, new_reference<NB>(s, factor, run.m));
+    run.l += huge_reference(run.m) ? careful_weights<NB>(s, factor, run.m) : weights<NB>(s, factor, run.m);
 }
 
 // Where some key of a tile is hidden from some row, its values must not meet a weight of 0 if they are infinite or NaN: that product
@@ -527,7 +571,7 @@ __global__ __launch_bounds__(256, TERMS == 1 ? 2 : 1) void cache_attn_stream_ker
     float sum = 0.f;
 #pragma unroll
     for (int w = 0; w < kStreamWaves; ++w) sum = fmaf(wl[w][m], __builtin_amdgcn_exp2f(wm[w][m] - top), sum);
-    float *to = a.part ? a.part + (((size_t)block * a.n_kv_heads + kvh) * a.n_splits + split) * part_floats(kRowTile, DH) : nullptr;
+    float *to = a.part && tiles.n > a.chunk ? a.part + (((size_t)block * a.n_kv_heads + kvh) * a.n_splits + split) * part_floats(kRowTile, DH) : nullptr;
     if (wave == 0 && half == 0 && r.live) {   // (beyond the last row nobody asks)
         if (to) *(float2 *)(to + kRowTile * DH + 2 * m) = make_float2(top, sum);
         else store_lse(a, r.row, r.head, top, sum);
@@ -568,41 +612,86 @@ __global__ __launch_bounds__(256, TERMS == 1 ? 2 : 1) void cache_attn_stream_ker
 
 // ------------------------------------------------------------------ many rows: keys and values shared through LDS
 //
-// Block = (128 virtual rows, kv head, split of the keys), four waves of 32 rows each against the same 64 keys, which go from the
+// Block = (128 virtual rows, kv head, split of the keys), four waves of 32 rows each against the same 32 keys, which go from the
 // cache through registers into one of two LDS buffers while the other one is multiplied: a key is read from L2 once for 128 rows
-// where the form above reads it for 32, and a wave has the other block of its compute unit to cover its exponentials.
-// 32 heads, bf16, 3584 rows: 300 us in blocks of 32 rows, 143 us so (735 TFLOP/s).
+// where the form above reads it for 32.
+// 64 keys take a wave about 1000 cycles of matrix instructions, as many of vector instructions (a score: a fused product, an exponential,
+// a sum, its share of a maximum and of a rounding) and LDS as many for the four waves; two waves share a SIMD, which is what the registers
+// hold.  One step after the other, the three took turns (each 37 % busy, 143 us for 3584 rows of 32 heads).  So the keys of tile i + 1
+// are multiplied while the weights of tile i are formed, and the maximum of tile i + 1 is found while the weights of
+// tile i meet its values: both halves of the loop have matrix and vector instructions that do not wait for each other, dealt out in
+// turn.  Keys are a tile ahead of values for that.
 // grid: n_blocks * n_splits * n_kv_heads, blocks with the most keys first
-constexpr int kTileRows = 128, kTileKeys = 64;
+constexpr int kTileKeys = 32;
+constexpr int kTileSlots = 8;   // tiles that LDS holds
+__host__ __device__ constexpr int tile_waves(int terms) { return terms == 1 ? 8 : 4; }   // what the registers of a SIMD hold
+__host__ __device__ constexpr int tile_rows(int terms) { return tile_waves(terms) * kRowTile; }
+__host__ __device__ constexpr size_t tile_lds_bytes(int head_dim) { return (size_t)kTileSlots * kTileKeys * head_dim * 4; }
+
+// 16 bytes per lane from p + offset to 1 KB of LDS at byte `at`, past the registers.  In assembly, since behind the builtin the compiler
+// lets every read of LDS wait for all loads in flight; what is read is waited for at loads_meet.
+__device__ __forceinline__ void load_to_lds(const void *p, uint32_t offset, uint32_t at)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(at), "v"(offset), "s"(p) : "m0", "memory");
+}
+// All but the wave's last LEFT loads have arrived, and so have the other waves'; everybody's reads of LDS are done.
+template <int LEFT>
+__device__ __forceinline__ void loads_meet()
+{
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LEFT) : "memory");
+}
 
 template <int DH, int TERMS, bool RULES>
-__global__ __launch_bounds__(256, TERMS == 1 ? 2 : 1) void cache_attn_tile_kernel(const AttnArgs a)
+__global__ __launch_bounds__(tile_waves(TERMS) * 64, tile_waves(TERMS) / 4) void cache_attn_tile_kernel(const AttnArgs a)
 {
-    constexpr int NKS = DH / 16, NDT = DH / 32, NCH = DH / 32;
-    __shared__ u32x4 lk[2][4][NCH][64], lv[2][4][NCH][64];   // [buffer][page][1 KB pieces][lane]
+    constexpr int NKS = DH / 16, NDT = DH / 32, NCH = DH / 32;   // (NCH: 1 KB pieces of a page's keys or values)
+    constexpr int WAVES = tile_waves(TERMS), ROWS = WAVES * kRowTile;
+    constexpr int LOADS = 4 * NCH / WAVES;   // of a wave for a tile
+    extern __shared__ u32x4 lds_tiles[];     // [slot][keys | values][page][piece][lane]
+    auto lk = [&](int slot, int page) __attribute__((always_inline)) { return lds_tiles + ((slot * 2 + 0) * 2 + page) * NCH * 64; };
+    auto lv = [&](int slot, int page) __attribute__((always_inline)) { return lds_tiles + ((slot * 2 + 1) * 2 + page) * NCH * 64; };
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, m = lane & 31;
     const int kvh = blockIdx.x % a.n_kv_heads, rest = blockIdx.x / a.n_kv_heads;
     const int split = rest % a.n_splits, block = a.n_blocks - 1 - rest / a.n_splits;
     const SeqView s = a.seq[seq_of_block(a, block)];
-    const int vb = (block - s.block0) * kTileRows, rows = s.n * a.group, total = s.pos0 + s.n;
+    const int vb = (block - s.block0) * ROWS, rows = s.n * a.group, total = s.pos0 + s.n;
     const int v0 = vb + kRowTile * wave;
-    const int p_lo = s.pos0 + vb / a.group, p_hi = s.pos0 + (vb + kTileRows <= rows ? vb + kTileRows - 1 : rows - 1) / a.group;
+    const int p_lo = s.pos0 + vb / a.group, p_hi = s.pos0 + (vb + ROWS <= rows ? vb + ROWS - 1 : rows - 1) / a.group;
     const int pre = RULES && a.prefix > 0 ? (a.prefix < total ? a.prefix : total) : 0;
     const KeyTiles tiles = key_tiles(p_lo, p_hi, total, RULES ? a.window : 0, RULES ? a.prefix : 0, kTileKeys);
     const int begin = split * a.chunk, i1 = begin + a.chunk < tiles.n ? begin + a.chunk : tiles.n;
     if (begin >= tiles.n) return;   // (the whole block; what joins the splits does not look at this one)
     const RowInfo r = row_info<RULES>(a, s, kvh, v0);
-    int i0 = begin;
+    // Tiles f0 .. f1 - 1 are those that every row of the block sees all of.
+    int i0 = begin, fk_max = 0;
     if (RULES && a.first_key) {   // (the same for all)
-        int *lowest = (int *)&lk[0][0][0][0];
-        const int low = wave_min(r.fk);
-        if (lane == 0) lowest[wave] = low;
+        int *lowest = (int *)lds_tiles, *highest = lowest + WAVES;
+        const int low = wave_min(r.fk), high = ~wave_min(~r.fk);
+        if (lane == 0) { lowest[wave] = low; highest[wave] = high; }
         __syncthreads();
         int fk = lowest[0];
+        fk_max = highest[0];
 #pragma unroll
-        for (int w = 1; w < 4; ++w) fk = lowest[w] < fk ? lowest[w] : fk;
+        for (int w = 1; w < WAVES; ++w) {
+            fk = lowest[w] < fk ? lowest[w] : fk;
+            fk_max = highest[w] > fk_max ? highest[w] : fk_max;
+        }
         __syncthreads();
+        fk_max = __builtin_amdgcn_readfirstlane(fk_max);
         i0 = first_tile(tiles, __builtin_amdgcn_readfirstlane(fk), begin, i1, kTileKeys);
+    }
+    int f0, f1;
+    {
+        const bool window = RULES && a.window > 0;
+        const int from = window && p_hi - a.window + 1 > fk_max ? p_hi - a.window + 1 : fk_max, to = window || p_lo >= pre ? p_lo : pre - 1;
+        auto place = [&](int t) { return !window ? t : (t <= tiles.b0 ? tiles.a : tiles.a + (t - tiles.b0)); };   // of tile t among those that are visited
+        f0 = place(from > 0 ? (from - 1) / kTileKeys + 1 : 0);
+        f1 = place((to + 1) / kTileKeys);
+        if (RULES && (a.cap > 0.f || a.slopes)) f1 = f0;
+        f0 = f0 < i0 ? i0 : f0;
+        f0 += (f0 - i0) & 1;   // (tiles are met in twos)
+        f0 = f0 < i1 ? f0 : i1;
+        f1 = f1 < f0 ? f0 : (f1 < i1 ? f1 : i1);
     }
 
     u32x4 q[NKS][TERMS];
@@ -614,92 +703,215 @@ __global__ __launch_bounds__(256, TERMS == 1 ? 2 : 1) void cache_attn_tile_kerne
     Running<NDT> run;
     run.start();
     bool unbounded = false;
+    const float factor = score_factor<RULES>(a);
 
     const int last_page = (total - 1) >> 4;
     const bf16_t *pool = (const bf16_t *)s.pool;
     const size_t page_elems = (size_t)a.n_layers * 2 * a.n_kv_heads * 16 * DH;
     const bf16_t *k_of = pool + ((size_t)a.layer * 2 * a.n_kv_heads + kvh) * (16 * DH), *v_of = k_of + (size_t)a.n_kv_heads * (16 * DH);
-    int ids = 0;
+    // The wave brings pieces wave, wave + WAVES, ... of a tile: keys of both pages, then values; of one page, or of both in turn.
+    // A lane has where that page's keys lie for one of the next 64 tiles from `ids0` on.
+    constexpr int PAGES = WAVES < 2 * NCH ? 2 : 1;
+    const ptrdiff_t to_values = (ptrdiff_t)a.n_kv_heads * (16 * DH) * sizeof(bf16_t);
+    uint32_t at_lo[PAGES], at_hi[PAGES];
+    int ids0 = i0;
     auto fetch_ids = [&](int i) __attribute__((always_inline)) {
         const int t = i + lane < i1 ? i + lane : i1 - 1;
-        const int page = tiles.at(t) * (kTileKeys / 16) + wave;
-        ids = s.table[page < last_page ? page : last_page];
+#pragma unroll
+        for (int x = 0; x < PAGES; ++x) {
+            const int page = tiles.at(t) * 2 + (PAGES == 2 ? x : wave / NCH % 2);
+            const unsigned long long at = (unsigned long long)(k_of + (size_t)s.table[page < last_page ? page : last_page] * page_elems);
+            at_lo[x] = (uint32_t)at;
+            at_hi[x] = (uint32_t)(at >> 32);
+            asm volatile("" : "+v"(at_lo[x]), "+v"(at_hi[x]));   // (waited for here, not in front of every use)
+        }
+        ids0 = i;
     };
-    u32x4 sk[NCH], sv[NCH];
-    auto request = [&](int page) __attribute__((always_inline)) {
-        const u32x4 *pk = (const u32x4 *)(k_of + (size_t)page * page_elems) + lane, *pv = (const u32x4 *)(v_of + (size_t)page * page_elems) + lane;
+    const uint32_t lds0 = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(uintptr_t)(__attribute__((address_space(3))) u32x4 *)lds_tiles) + wave * 1024;
+    const uint32_t offset = wave % NCH * 1024 + lane * 16;
+    // (beyond the last tile: the last one, for nothing, so that the loads in flight can be counted)
+    auto request = [&](int i) __attribute__((always_inline)) {
+        const int x = (i < i1 ? i : i1 - 1) - ids0;
+        const uint32_t at = lds0 + (uint32_t)((i - i0) & (kTileSlots - 1)) * (4 * NCH * 1024);
 #pragma unroll
-        for (int c = 0; c < NCH; ++c) sk[c] = pk[c * 64];
-#pragma unroll
-        for (int c = 0; c < NCH; ++c) sv[c] = pv[c * 64];
+        for (int c = 0; c < LOADS; ++c) {
+            const int y = PAGES == 2 ? c % 2 : 0;
+            const char *p = (const char *)(((unsigned long long)(uint32_t)__builtin_amdgcn_readlane((int)at_hi[y], x) << 32) |
+                                           (uint32_t)__builtin_amdgcn_readlane((int)at_lo[y], x));
+            // (values: the second half of the pieces, known here but for eight waves of one piece)
+            const bool values = LOADS == 1 ? wave >= 2 * NCH : c >= LOADS / 2;
+            load_to_lds(values ? p + to_values : p, offset, at + c * WAVES * 1024);
+        }
     };
-    auto put = [&](int buf) __attribute__((always_inline)) {
+    auto key = [&](int buf, int ks) __attribute__((always_inline)) {
+        return as_bf16((lk(buf, (lane >> 4) & 1) + half * 16 + (lane & 15))[(ks >> 1) * 64 + (ks & 1) * 32]);
+    };
+    auto value = [&](int buf, int g, int d) __attribute__((always_inline)) {
+        const uint2 *p = (const uint2 *)lv(buf, g) + (m >> 4) * 64 + half * 16 + (m & 15);
+        const uint2 x0 = p[d * 128], x1 = p[d * 128 + 32];
+        return (u32x4){x0.x, x0.y, x1.x, x1.y};
+    };
+    auto products = [&](int buf, f32x16 (&sc)[1]) __attribute__((always_inline)) {
 #pragma unroll
-        for (int c = 0; c < NCH; ++c) lk[buf][wave][c][lane] = sk[c];
+        for (int e = 0; e < 16; ++e) sc[0][e] = 0.f;
 #pragma unroll
-        for (int c = 0; c < NCH; ++c) lv[buf][wave][c][lane] = sv[c];
+        for (int ks = 0; ks < NKS; ++ks) {
+            const bf16x8 k = key(buf, ks);
+#pragma unroll
+            for (int t = TERMS - 1; t >= 0; --t) sc[0] = mfma32(k, as_bf16(q[ks][t]), sc[0]);
+        }
+    };
+    // the weights of 32 keys as operands
+    auto pack = [&](const f32x16 (&sc)[1], u32x4 (&w)[2][TERMS]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+            float x[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = sc[0][8 * g + e];
+            split_terms<TERMS>(x, w[g]);
+        }
+    };
+    auto any = [&](int i) __attribute__((always_inline)) { return v0 < rows && any_seen<RULES>(r, pre, tiles.at(i) * kTileKeys); };
+    auto all = [&](int i) __attribute__((always_inline)) { return all_seen<RULES>(r, pre, tiles.at(i) * kTileKeys); };
+    auto slot = [&](int i) __attribute__((always_inline)) { return (i - i0) & (kTileSlots - 1); };
+    // Every other tile: tiles i .. i + 2 have arrived, nobody reads those before them any more, and two more are requested (i + 5 was
+    // the last one).  Waves that share a SIMD get out of step in between; met at every tile they took turns.
+    auto turn = [&](int i) __attribute__((always_inline)) {
+        loads_meet<3 * LOADS>();
+        if (i + 7 - ids0 >= 64) fetch_ids(i + 6);
+        request(i + 6);
+        request(i + 7);
+    };
+    // A tile, one step after the other.
+    auto tile = [&](int i) __attribute__((always_inline)) {
+        if (((i - i0) & 1) == 0) turn(i);
+        if (!any(i)) return;
+        f32x16 sc[1];
+        u32x4 w[2][TERMS];
+        products(slot(i), sc);
+        weigh<RULES, 1, NDT>(a, r, pre, tiles.at(i) * kTileKeys, sc, run);
+        pack(sc, w);
+        const bool hidden = !all(i);
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+            u32x4 v[NDT];
+#pragma unroll
+            for (int d = 0; d < NDT; ++d) v[d] = value(slot(i), g, d);
+            if (hidden) unbounded |= take_out_unbounded<NDT>(v);
+#pragma unroll
+            for (int d = 0; d < NDT; ++d)
+#pragma unroll
+                for (int t = TERMS - 1; t >= 0; --t) run.o[d] = mfma32(as_bf16(v[d]), as_bf16(w[g][t]), run.o[d]);
+        }
+    };
+    bool huge = false;
+    // A tile that all rows see, its products made before, beside the products and the maximum of the next one (`more`).
+    auto fused = [&](int i, f32x16 (&sc)[1], f32x16 (&sn)[1], auto more) __attribute__((always_inline)) {
+        constexpr bool MORE = decltype(more)::value;
+        float f = factor;
+        if (huge) {   // (the products rounded here; see huge_reference)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) sc[0][e] *= factor;
+            f = 1.f;
+        }
+        // Written in the order in which it is to run, and held to it: operands from LDS are requested four steps ahead, a step is a
+        // matrix instruction (or its terms) and the vector instructions that go beside it.
+        constexpr int RING = 4, PV = 2 * NDT, EACH = 16 / NKS;
+        const int here = slot(i), there = slot(i + 1);
+        __builtin_amdgcn_s_setprio(1);   // (of two waves on a SIMD the one with exponentials to do goes first: 128 -> 124 us)
+        u32x4 w[2][TERMS], ring[NKS + PV];
+        auto fetch = [&](int x) __attribute__((always_inline)) {
+            if (x < NKS) {
+                if (MORE) ring[x] = __builtin_bit_cast(u32x4, key(there, x));
+            } else if (x < NKS + PV) ring[x] = value(here, (x - NKS) / NDT, (x - NKS) % NDT);
+        };
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int x = MORE ? 0 : NKS; x < (MORE ? 0 : NKS) + RING; ++x) fetch(x);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sn[0][e] = 0.f;
+        float sum[2] = {0.f, 0.f};
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int x = 0; x < NKS; ++x) {
+            if (MORE) {
+                fetch(x + RING);
+#pragma unroll
+                for (int t = TERMS - 1; t >= 0; --t) sn[0] = mfma32(as_bf16(ring[x]), as_bf16(q[x][t]), sn[0]);
+            }
+#pragma unroll
+            for (int e = EACH * x; e < EACH * (x + 1); e += 2) {
+                const float p0 = __builtin_amdgcn_exp2f(fmaf(sc[0][e], f, -run.m)), p1 = __builtin_amdgcn_exp2f(fmaf(sc[0][e + 1], f, -run.m));
+                sum[0] += p0;
+                sum[1] += p1;
+                uint32_t t[TERMS];
+                split_pair<TERMS>(p0, p1, t);
+#pragma unroll
+                for (int k = 0; k < TERMS; ++k) w[e >> 3][k][(e & 7) >> 1] = t[k];
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        run.l += sum[0] + sum[1];
+        __builtin_amdgcn_s_setprio(0);
+        float mx = -INFINITY;
+#pragma unroll
+        for (int y = 0; y < PV; ++y) {
+            fetch(NKS + y + RING);
+#pragma unroll
+            for (int t = TERMS - 1; t >= 0; --t) run.o[y % NDT] = mfma32(as_bf16(ring[NKS + y]), as_bf16(w[y / NDT][t]), run.o[y % NDT]);
+            if (MORE) {   // (the products need a step or two before they are there)
+                constexpr int LATE = PV / 4;
+#pragma unroll
+                for (int e = y < LATE ? 0 : 16 * (y - LATE) / (PV - LATE); e < (y < LATE ? 0 : 16 * (y - LATE + 1) / (PV - LATE)); ++e) mx = fmaxf(mx, sn[0][e]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if (MORE) {
+            mx = both_halves_max(mx) * factor;
+            if (__builtin_amdgcn_ballot_w64(mx > run.m + 8.f) != 0) {
+                move_reference(run, mx > run.m + 8.f ? mx : run.m);
+                huge = huge_reference(run.m);
+            }
+        }
     };
     if (i0 < i1) {
         fetch_ids(i0);
-        request(__builtin_amdgcn_readlane(ids, 0));
-        put(0);
-    }
-    for (int i = i0; i < i1; ++i) {
-        const int buf = (i - i0) & 1, nx = (i + 1 - i0) & 63;
-        __syncthreads();   // this tile has arrived, and nobody reads the other buffer any more
-        if (nx == 0) fetch_ids(i + 1);
-        request(__builtin_amdgcn_readlane(ids, nx));   // (behind the last one: for nothing)
-        const int base = tiles.at(i) * kTileKeys;
-        if (v0 < rows && (any_seen<RULES>(r, pre, base) || any_seen<RULES>(r, pre, base + 32))) {
-            f32x16 sc[2];
+        __syncthreads();
 #pragma unroll
-            for (int b = 0; b < 2; ++b) {
-#pragma unroll
-                for (int e = 0; e < 16; ++e) sc[b][e] = 0.f;
-                const u32x4 *kp = &lk[buf][2 * b + ((lane >> 4) & 1)][0][half * 16 + (lane & 15)];
-#pragma unroll
-                for (int ks = 0; ks < NKS; ++ks) {
-                    const u32x4 k = kp[(ks >> 1) * 64 + (ks & 1) * 32];
-#pragma unroll
-                    for (int t = TERMS - 1; t >= 0; --t) sc[b] = mfma32(as_bf16(k), as_bf16(q[ks][t]), sc[b]);
-                }
+        for (int t = 0; t < 6; ++t) request(i0 + t);
+        for (int i = i0; i < f0; ++i) tile(i);
+        if (f0 < f1) {
+            f32x16 s0[1], s1[1];
+            if (f0 == i0) loads_meet<5 * LOADS>();   // (later tiles have arrived with the turn before)
+            products(slot(f0), s0);
+            move_reference(run, new_reference<1>(s0, factor, run.m));
+            huge = huge_reference(run.m);
+            int i = f0;
+            for (; i + 2 < f1; i += 2) {
+                turn(i);
+                fused(i, s0, s1, std::true_type());
+                fused(i + 1, s1, s0, std::true_type());
             }
-            weigh<RULES, 2, NDT>(a, r, pre, base, sc, run);
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                float x[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] = sc[g >> 1][8 * (g & 1) + e];
-                u32x4 w[TERMS];
-                split_terms<TERMS>(x, w);
-                const uint2 *vp = (const uint2 *)&lv[buf][g][0][0] + (m >> 4) * 64 + half * 16 + (m & 15);
-                u32x4 v[NDT];
-#pragma unroll
-                for (int d = 0; d < NDT; ++d) {
-                    const uint2 x0 = vp[d * 128], x1 = vp[d * 128 + 32];
-                    v[d] = (u32x4){x0.x, x0.y, x1.x, x1.y};
-                }
-                if (!all_seen<RULES>(r, pre, base + 32 * (g >> 1))) unbounded |= take_out_unbounded<NDT>(v);
-#pragma unroll
-                for (int d = 0; d < NDT; ++d)
-#pragma unroll
-                    for (int t = TERMS - 1; t >= 0; --t) run.o[d] = mfma32(as_bf16(v[d]), as_bf16(w[t]), run.o[d]);
-            }
+            turn(i);
+            if (i + 1 < f1) {
+                fused(i, s0, s1, std::true_type());
+                fused(i + 1, s1, s0, std::false_type());
+            } else fused(i, s0, s1, std::false_type());
         }
-        put(buf ^ 1);
+        for (int i = f1; i < i1; ++i) tile(i);
     }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // (LDS must not be given up while something is on its way to it)
     if (unbounded)
         for (int i = i0; i < i1; ++i)
-            for (int base = tiles.at(i) * kTileKeys, end = base + kTileKeys; base < end; base += 32)
-                if (any_seen<RULES>(r, pre, base) && !all_seen<RULES>(r, pre, base))
-                    add_unbounded<RULES, NDT>(r, pre, base, run, [&](int d, int e) { return 32 * d + 8 * (e >> 2) + 4 * half + (e & 3); },
-                                              [&](int j, int dim) { return bf16_to_f32(v_of[(size_t)s.table[j >> 4] * page_elems + vf_elem(j & 15, dim)]); });
+            if (any(i) && !all(i))
+                add_unbounded<RULES, NDT>(r, pre, tiles.at(i) * kTileKeys, run, [&](int d, int e) { return 32 * d + 8 * (e >> 2) + 4 * half + (e & 3); },
+                                          [&](int j, int dim) { return bf16_to_f32(v_of[(size_t)s.table[j >> 4] * page_elems + vf_elem(j & 15, dim)]); });
     const float l = both_halves_sum(run.l);
     if (!r.live) return;
-    if (a.part) {
-        float *to = a.part + (((size_t)block * a.n_kv_heads + kvh) * a.n_splits + split) * part_floats(kTileRows, DH);
+    if (a.part && tiles.n > a.chunk) {   // (otherwise this split is all there is)
+        float *to = a.part + (((size_t)block * a.n_kv_heads + kvh) * a.n_splits + split) * part_floats(ROWS, DH);
         const int row = kRowTile * wave + m;
-        if (half == 0) *(float2 *)(to + kTileRows * DH + 2 * row) = make_float2(run.m, l);
+        if (half == 0) *(float2 *)(to + ROWS * DH + 2 * row) = make_float2(run.m, l);
 #pragma unroll
         for (int d = 0; d < NDT; ++d)
 #pragma unroll
@@ -826,7 +1038,7 @@ __global__ __launch_bounds__(256, 1) void cache_attn_plain_kernel(const AttnArgs
     float sum = 0.f;
 #pragma unroll
     for (int w = 0; w < kStreamWaves; ++w) sum = fmaf(wl[w][m], __builtin_amdgcn_exp2f(wm[w][m] - top), sum);
-    float *to = a.part ? a.part + (((size_t)block * a.n_kv_heads + kvh) * a.n_splits + split) * part_floats(kRowTile, DH) : nullptr;
+    float *to = a.part && tiles.n > a.chunk ? a.part + (((size_t)block * a.n_kv_heads + kvh) * a.n_splits + split) * part_floats(kRowTile, DH) : nullptr;
     if (wave == 0 && half == 0 && r.live) {   // (beyond the last row nobody asks)
         if (to) *(float2 *)(to + kRowTile * DH + 2 * m) = make_float2(top, sum);
         else store_lse(a, r.row, r.head, top, sum);
@@ -854,36 +1066,40 @@ __global__ __launch_bounds__(256, 1) void cache_attn_plain_kernel(const AttnArgs
 
 // ------------------------------------------------------------------ the splits meet
 //
-// Block = a row: four adjacent dims per thread, the splits dealt to the block's groups of DH / 4 threads, whose sums meet in LDS in
-// their order.  (With a block for all rows of a key / value head and the splits one after the other a token behind 65535 positions
-// waited 23 us for 128 of them.)   row_block: rows of the blocks that were split; tile: keys of their tiles.
-// grid: n_kv_heads * n_blocks * row_block
-template <int DH>
+// Four adjacent dims of a row per thread.  TOGETHER: a block per row, the splits dealt to its groups of DH / 4 threads, whose sums
+// meet in LDS in their order, for few rows of many splits (with a block for all rows of a key / value head and the splits one after the
+// other a token behind 65535 positions waited 23 us for 128 of them, so 5).  Otherwise a group has a row to itself: 1536 rows of 32 heads
+// in two or three splits took 70 us with a block for each row.
+// row_block: rows of the blocks that were split; tile: keys of their tiles.
+// grid: n_kv_heads * n_blocks * (row_block, or row_block / rows of a block)
+template <int DH, bool TOGETHER>
 __global__ __launch_bounds__(256) void cache_attn_join_kernel(const AttnArgs a, int row_block, int tile)
 {
-    constexpr int TPR = DH / 4, GROUPS = 256 / TPR;
+    constexpr int TPR = DH / 4, GROUPS = 256 / TPR, STEP = TOGETHER ? GROUPS : 1;
     __shared__ float tops[GROUPS], sums[GROUPS];
     __shared__ f32x4 part[GROUPS][TPR];
-    const int row = blockIdx.x % row_block, rest = blockIdx.x / row_block, kvh = rest % a.n_kv_heads, block = rest / a.n_kv_heads;
+    const int group = threadIdx.x / TPR, d = threadIdx.x % TPR;
+    const int per = TOGETHER ? row_block : row_block / GROUPS;
+    const int row = TOGETHER ? blockIdx.x % per : blockIdx.x % per * GROUPS + group, rest = blockIdx.x / per, kvh = rest % a.n_kv_heads, block = rest / a.n_kv_heads;
     const SeqView s = a.seq[seq_of_block(a, block)];
     const int vb = (block - s.block0) * row_block, rows = s.n * a.group, v = vb + row;
-    if (v >= rows) return;
+    if (v >= rows) return;   // (TOGETHER: the whole block)
     const int p_lo = s.pos0 + vb / a.group, p_hi = s.pos0 + (vb + row_block <= rows ? vb + row_block - 1 : rows - 1) / a.group;
     const KeyTiles tiles = key_tiles(p_lo, p_hi, s.pos0 + s.n, a.window, a.prefix, tile);
     const int used = (tiles.n + a.chunk - 1) / a.chunk;
+    if (used < 2) return;   // (written by the split itself)
     const size_t stride = part_floats(row_block, DH);
     const float *from = a.part + ((size_t)block * a.n_kv_heads + kvh) * a.n_splits * stride;
-    const int group = threadIdx.x / TPR, d = threadIdx.x % TPR;
     const float *ml = from + row_block * DH + 2 * row, *o = from + row * DH + 4 * d;
     float top = kNoKey, sum = 0.f;
     f32x4 x = {0.f, 0.f, 0.f, 0.f};
     // (requested side by side, four splits at a time; one that does not exist weighs nothing)
-    for (int k0 = group; k0 < used; k0 += 4 * GROUPS) {
+    for (int k0 = TOGETHER ? group : 0; k0 < used; k0 += 4 * STEP) {
         float2 t[4];
         f32x4 y[4];
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-            const int k = k0 + u * GROUPS < used ? k0 + u * GROUPS : k0;
+            const int k = k0 + u * STEP < used ? k0 + u * STEP : k0;
             t[u] = *(const float2 *)(ml + k * stride);
             y[u] = *(const f32x4 *)(o + k * stride);
         }
@@ -896,29 +1112,31 @@ __global__ __launch_bounds__(256) void cache_attn_join_kernel(const AttnArgs a, 
         x = x * f0;
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-            if (k0 + u * GROUPS >= used) continue;
+            if (k0 + u * STEP >= used) continue;
             const float f = __builtin_amdgcn_exp2f(t[u].x - t0);
             sum = fmaf(t[u].y, f, sum);
             x += y[u] * f;
         }
     }
-    if (d == 0) { tops[group] = top; sums[group] = sum; }
-    part[group][d] = x;
-    __syncthreads();
-    if (group > 0) return;
-    float all = tops[0];
+    if constexpr (TOGETHER) {
+        if (d == 0) { tops[group] = top; sums[group] = sum; }
+        part[group][d] = x;
+        __syncthreads();
+        if (group > 0) return;
+        top = tops[0];
 #pragma unroll
-    for (int g = 1; g < GROUPS; ++g) all = fmaxf(all, tops[g]);
-    sum = 0.f;
-    x = (f32x4){0.f, 0.f, 0.f, 0.f};
+        for (int g = 1; g < GROUPS; ++g) top = fmaxf(top, tops[g]);
+        sum = 0.f;
+        x = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int g = 0; g < GROUPS; ++g) {
-        const float f = __builtin_amdgcn_exp2f(tops[g] - all);
-        sum = fmaf(sums[g], f, sum);
-        x += part[g][d] * f;
+        for (int g = 0; g < GROUPS; ++g) {
+            const float f = __builtin_amdgcn_exp2f(tops[g] - top);
+            sum = fmaf(sums[g], f, sum);
+            x += part[g][d] * f;
+        }
     }
     const int r = v / a.group, out_row = s.row0 + r, head = kvh * a.group + (v - r * a.group);
-    if (d == 0) store_lse(a, out_row, head, all, sum);
+    if (d == 0) store_lse(a, out_row, head, top, sum);
     store_out4(a, DH, out_row, head, 4 * d, x * inverse_sum(sum));
 }
 

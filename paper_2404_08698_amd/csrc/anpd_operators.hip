@@ -104,65 +104,104 @@ int32_t rows_in(const char *who, const CacheShape &c, int32_t layer, const void 
 // ---- attention: how the work is divided
 
 struct Plan {
-    bool shared;   // 128 rows share keys through LDS; otherwise blocks of 32 rows
+    bool shared;   // many rows share keys through LDS; otherwise blocks of 32 rows
     int row_block, key_tile;
     size_t part_bytes;
 };
 
-// Sets the row blocks of a's sequences, the splits and their size.
+// The key tiles of all row blocks of a sequence, by a sum over its ends (rows in between have as many, more or less), and the most
+// that a block can have.
+void count_tiles(const AttnArgs &a, const SeqView &v, int row_block, int key_tile, int64_t &blocks, int64_t &tiles, int &most)
+{
+    const int64_t rows = (int64_t)v.n * a.group;
+    const int total = v.pos0 + v.n, span = row_block / a.group;
+    blocks = (rows + row_block - 1) / row_block;
+    const KeyTiles first = key_tiles(v.pos0, v.pos0 + (span < v.n ? span : v.n) - 1, total, a.window, a.prefix, key_tile);
+    const KeyTiles last = key_tiles(total - 1 - (span < v.n ? span : v.n) + 1, total - 1, total, a.window, a.prefix, key_tile);
+    tiles = blocks * (first.n + last.n) / 2;
+    // (a window's tiles depend on where it begins inside the first one)
+    const int pre = a.prefix < total ? a.prefix : total, all = (total > pre ? total : pre) - 1;
+    int64_t bound = all / key_tile + 1;
+    if (a.window > 0) {
+        const int64_t some = (pre + key_tile - 1) / key_tile + ((int64_t)a.window + span + 1) / key_tile + 2;
+        if (some < bound) bound = some;
+    }
+    most = (int)bound;
+}
+
+// Sets the row blocks of a's sequences, the splits and their size: by the sizes for bf16 rows, so that the workspace is the same for both types
+// (blocks of fp32 rows are half as many rows in the shared form).
 Plan plan_attention(AttnArgs &a, const CacheShape &c, int n_cu)
 {
     Plan p;
-    int64_t blocks32 = 0, blocks128 = 0;
+    const int shared_rows = tile_rows(1);
+    int64_t blocks[2] = {0, 0}, tiles[2] = {0, 0};   // of either form
+    int most[2] = {0, 0};
     for (int s = 0; s < a.n_seq; ++s) {
-        const int64_t v = (int64_t)a.seq[s].n * a.group;
-        blocks32 += (v + kRowTile - 1) / kRowTile;
-        blocks128 += (v + kTileRows - 1) / kTileRows;
+        if (a.seq[s].n == 0) continue;
+        for (int form = 0; form < 2; ++form) {
+            int64_t b, t;
+            int m;
+            count_tiles(a, a.seq[s], form ? shared_rows : kRowTile, form ? kTileKeys : kStreamTile, b, t, m);
+            blocks[form] += b;
+            tiles[form] += t * a.n_kv_heads;
+            if (m > most[form]) most[form] = m;
+        }
     }
-    p.shared = c.fragments && blocks128 * a.n_kv_heads >= n_cu && blocks128 * 3 <= blocks32;
-    p.row_block = p.shared ? kTileRows : kRowTile;
+    // The shared form, a block per compute unit: as many splits as give all of them a block, none shorter than twelve tiles.
+    const int64_t shared_items = blocks[1] * a.n_kv_heads;
+    int64_t splits = shared_items > 0 ? n_cu / shared_items : 1;
+    if (splits > most[1] / 12) splits = most[1] / 12;
+    if (splits < 1) splits = 1;
+    const int64_t shared_chunk = (most[1] + splits - 1) / splits;
+    // Which form, by what tiles were measured to take, us: 0.95 of a compute unit for 32 rows x 128 keys (two blocks share it); 0.9 for the
+    // 256 x 32 of the longest block, 1.1 for those of all blocks where they are many; six to begin with and eight to be joined.
+    // 32 heads of 128, 32 rows / shared: 1024 rows 27 / 36, 1536 46 / 50, 2048 74 / 64, 3584 187 / 120; behind 4096 positions
+    // 128 rows 33 / 36, 256 50 / 41.
+    const double longest_us = 0.9 * (double)shared_chunk, all_us = 1.1 * (double)tiles[1] / n_cu;
+    p.shared = c.fragments && (longest_us > all_us ? longest_us : all_us) + (splits > 1 ? 14.0 : 6.0) < 0.95 * (double)tiles[0] / n_cu + 4.0;
+    p.row_block = p.shared ? tile_rows(a.q_f32 ? 3 : 1) : kRowTile;
     p.key_tile = p.shared ? kTileKeys : kStreamTile;
     a.n_blocks = 0;
-    int most = 0;   // tiles of a row block
     for (int s = 0; s < a.n_seq; ++s) {
-        SeqView &v = a.seq[s];
-        v.block0 = a.n_blocks;
-        if (v.n == 0) continue;
-        const int64_t rows = (int64_t)v.n * a.group;
-        a.n_blocks += (int32_t)((rows + p.row_block - 1) / p.row_block);
-        const int total = v.pos0 + v.n, pre = a.prefix < total ? a.prefix : total, pre_tiles = (pre + p.key_tile - 1) / p.key_tile;
-        const int all = (total - 1) / p.key_tile + 1;
-        int64_t tiles = all > pre_tiles ? all : pre_tiles;
-        if (a.window > 0) {
-            const int64_t some = pre_tiles + ((int64_t)a.window + p.row_block / a.group + 1) / p.key_tile + 2;
-            if (some < tiles) tiles = some;
-        }
-        if (tiles > most) most = (int)tiles;
+        a.seq[s].block0 = a.n_blocks;
+        a.n_blocks += (int32_t)(((int64_t)a.seq[s].n * a.group + p.row_block - 1) / p.row_block);
     }
-    const int64_t items = (int64_t)a.n_blocks * a.n_kv_heads;
-    int64_t splits = items > 0 ? (2 * n_cu + items - 1) / items : 1;
-    if (splits > most / 2) splits = most / 2;
-    if (splits < 1) splits = 1;
-    a.chunk = most > 0 ? (int)((most + splits - 1) / splits) : 1;
-    a.n_splits = most > 0 ? (most + a.chunk - 1) / a.chunk : 1;
-    p.part_bytes = a.n_splits > 1 ? align_up((size_t)items * a.n_splits * part_floats(p.row_block, c.head_dim) * sizeof(float)) : 0;
+    const int64_t items = blocks[p.shared] * a.n_kv_heads;
+    const int longest = most[p.shared];
+    if (p.shared) a.chunk = (int)shared_chunk;
+    else {
+        splits = items > 0 ? (2 * n_cu + items - 1) / items : 1;
+        if (splits > longest / 2) splits = longest / 2;
+        if (splits < 1) splits = 1;
+        a.chunk = (int)((longest + splits - 1) / splits);
+    }
+    if (a.chunk < 1) a.chunk = 1;
+    a.n_splits = longest > 0 ? (longest + a.chunk - 1) / a.chunk : 1;
+    p.part_bytes = a.n_splits > 1 ? align_up((size_t)items * a.n_splits * part_floats(p.shared ? shared_rows : kRowTile, c.head_dim) * sizeof(float)) : 0;
     return p;
 }
 
 template <int DH, int TERMS, bool RULES>
-void launch_fragments(const AttnArgs &a, const Plan &p, hipStream_t st)
+int32_t launch_fragments(const AttnArgs &a, const Plan &p, hipStream_t st)
 {
     const dim3 grid((unsigned)((int64_t)a.n_blocks * a.n_splits * a.n_kv_heads));
-    if (p.shared) hipLaunchKernelGGL((cache_attn_tile_kernel<DH, TERMS, RULES>), grid, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((cache_attn_stream_kernel<DH, TERMS, RULES>), grid, dim3(256), 0, st, a);
+    if (p.shared) {
+        constexpr size_t lds = tile_lds_bytes(DH);
+        // (at every call: the attribute is the current device's)
+        if (lds > 65536) HIP_TRY(hipFuncSetAttribute((const void *)cache_attn_tile_kernel<DH, TERMS, RULES>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+        hipLaunchKernelGGL((cache_attn_tile_kernel<DH, TERMS, RULES>), grid, dim3(tile_waves(TERMS) * 64), lds, st, a);
+    } else hipLaunchKernelGGL((cache_attn_stream_kernel<DH, TERMS, RULES>), grid, dim3(256), 0, st, a);
+    return ANPD_OK;
 }
 template <int DH>
 int32_t launch_attention(const AttnArgs &a, const Plan &p, const CacheShape &c, hipStream_t st)
 {
     const bool rules = ruled(a);
     if (c.fragments) {
-        if (a.q_f32) { if (rules) launch_fragments<DH, 3, true>(a, p, st); else launch_fragments<DH, 3, false>(a, p, st); }
-        else { if (rules) launch_fragments<DH, 1, true>(a, p, st); else launch_fragments<DH, 1, false>(a, p, st); }
+        const int32_t rc = a.q_f32 ? (rules ? launch_fragments<DH, 3, true>(a, p, st) : launch_fragments<DH, 3, false>(a, p, st))
+                                   : (rules ? launch_fragments<DH, 1, true>(a, p, st) : launch_fragments<DH, 1, false>(a, p, st));
+        if (rc != ANPD_OK) return rc;
     } else {
         const dim3 grid((unsigned)((int64_t)a.n_blocks * a.n_splits * a.n_kv_heads));
         if (c.dtype == ANPD_BF16) hipLaunchKernelGGL((cache_attn_plain_kernel<bf16_t, DH>), grid, dim3(256), 0, st, a);
@@ -170,8 +209,11 @@ int32_t launch_attention(const AttnArgs &a, const Plan &p, const CacheShape &c, 
     }
     HIP_TRY(hipGetLastError());
     if (a.part) {
-        hipLaunchKernelGGL((cache_attn_join_kernel<DH>), dim3((unsigned)((int64_t)a.n_blocks * a.n_kv_heads * p.row_block)), dim3(256), 0, st, a, p.row_block,
-                           p.key_tile);
+        const int64_t rows = (int64_t)a.n_blocks * a.n_kv_heads * p.row_block;
+        const dim3 block(256);
+        // (a block per row while those are few enough to run side by side)
+        if (a.n_splits > 4 && rows <= 4096) hipLaunchKernelGGL((cache_attn_join_kernel<DH, true>), dim3((unsigned)rows), block, 0, st, a, p.row_block, p.key_tile);
+        else hipLaunchKernelGGL((cache_attn_join_kernel<DH, false>), dim3((unsigned)(rows / (1024 / DH))), block, 0, st, a, p.row_block, p.key_tile);
         HIP_TRY(hipGetLastError());
     }
     return ANPD_OK;

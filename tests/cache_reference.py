@@ -120,3 +120,9 @@ def check_attention(filled, q, spans, out, lse, **rules):
     assert not wrong[~dead].any(), ((got_lse - want_lse).abs() / off)[~dead].max().item()
     if dead.any():
         assert (got.reshape(*dead.shape, -1)[dead] == 0).all()
+
+
+#: (heads, key / value heads, head dim, [(pos0, rows)]) that take the form whose rows share keys through LDS, whatever rules there are
+#: besides a short window; with and without splits of the keys, blocks that are not full, several sequences
+SHARED_SHAPES = [(8, 8, 128, [(3000, 1000)]), (32, 4, 64, [(0, 2222)]), (16, 1, 128, [(5000, 700)]), (32, 2, 128, [(2000, 513), (0, 3), (2400, 777)]),
+                 (48, 48, 64, [(0, 1700)])]

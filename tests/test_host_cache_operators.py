@@ -267,5 +267,27 @@ def test_failed_launches_are_reported(stub):
     run(stub, "child_failures")
 
 
+def child_forms():
+    """Shapes whose rows share keys through LDS, which tests elsewhere rely on; a token and a short prompt do not."""
+    sys.path.insert(0, HERE)
+    c = Caches()
+    import ast
+    shapes = next(ast.literal_eval(n.value) for n in ast.parse(open(os.path.join(HERE, "cache_reference.py")).read()).body
+                  if isinstance(n, ast.Assign) and n.targets[0].id == "SHARED_SHAPES")
+    assert len(shapes) >= 4
+    for heads, kv_heads, dim, spans in shapes + [(32, 32, 128, [(500, 1)]), (32, 32, 128, [(0, 500)])]:
+        kvs = [c.cache(p + n, p + n, heads, kv_heads, dim, layers=1) for p, n in spans]
+        ws = c.memory(64 << 20)
+        for dtype in (0, 1):
+            c.stub.stub_forget()
+            assert c.attention(kvs, [n for _, n in spans], [p for p, _ in spans], dtype=dtype, ldq=heads * dim, ldo=heads * dim, ws=ws, nb=64 << 20) == 0, c.L.anpd_last_error()
+            shared = "cache_attn_tile_kernel" in c.names()[0]
+            assert shared == ((heads, kv_heads, dim, spans) in shapes), (heads, spans, c.names())
+
+
+def test_forms(stub):
+    run(stub, "child_forms")
+
+
 if __name__ == "__main__":
     globals()[sys.argv[1]](*sys.argv[2:])
