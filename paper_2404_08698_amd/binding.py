@@ -542,7 +542,7 @@ class AttentionRules:
 
 
 def _sequences(kvs, q, n_rows, pos0, rules):
-    """(first cache, n_seq, handles, rows, positions or None) for the calls on several caches."""
+    """(shape of the caches, n_seq, handles, rows, positions or None) for the calls on several caches."""
     import torch
     if isinstance(kvs, KVCache):
         kvs = (kvs,)
@@ -551,26 +551,30 @@ def _sequences(kvs, q, n_rows, pos0, rules):
         raise ValueError("no cache")
     first = kvs[0]
     shape = first.model.shape
-    if not (q.is_cuda and q.device == first.pool.device and q.dim() == 2 and q.stride(1) == 1 and q.shape[1] == shape.n_heads * shape.head_dim
-            and q.dtype in (torch.float32, torch.bfloat16)):
+    if q.dim() != 2 or q.stride(1) != 1 or q.shape[1] != shape.n_heads * shape.head_dim or q.device != first.pool.device or q.dtype not in (torch.float32, torch.bfloat16):
         raise ValueError("rows must be a 2-d float32 or bfloat16 tensor on the caches' device, n_heads * head_dim wide")
+    rows = q.shape[0]
     handles = (C.c_void_p * n)(*[kv._h.value for kv in kvs])
     if n_rows is None:      # the same number of each sequence
-        if q.shape[0] % n:
-            raise ValueError("n_rows is needed: %d rows do not divide among %d sequences" % (q.shape[0], n))
-        counts = (C.c_int32 * n)(*([q.shape[0] // n] * n))
+        if rows % n:
+            raise ValueError("n_rows is needed: %d rows do not divide among %d sequences" % (rows, n))
+        counts = (C.c_int32 * n)(*([rows // n] * n))
     else:
-        if len(n_rows) != n or sum(n_rows) != q.shape[0] or min(n_rows) < 0:
+        if len(n_rows) != n or sum(n_rows) != rows or min(n_rows) < 0:
             raise ValueError("n_rows does not add up to the rows")
         counts = (C.c_int32 * n)(*n_rows)
-    if pos0 is not None and len(pos0) != n:
-        raise ValueError("pos0: one per sequence")
+    if pos0 is not None:
+        if len(pos0) != n:
+            raise ValueError("pos0: one per sequence")
+        pos0 = (C.c_int32 * n)(*pos0)
     if rules is not None:
-        if rules.slopes is not None and (rules.slopes.numel() < shape.n_heads or rules.slopes.device != q.device):
-            raise ValueError("slopes: one per head")
-        if rules.first_key is not None and (rules.first_key.numel() < q.shape[0] or rules.first_key.device != q.device):
-            raise ValueError("first_key: one per row")
-    return first, n, handles, counts, None if pos0 is None else (C.c_int32 * n)(*pos0)
+        t = rules.slopes
+        if t is not None and (t.numel() < shape.n_heads or t.device != q.device):
+            raise ValueError("slopes: one per head, on the caches' device")
+        t = rules.first_key
+        if t is not None and (t.numel() < rows or t.device != q.device):
+            raise ValueError("first_key: one per row, on the caches' device")
+    return shape, n, handles, counts, pos0
 
 
 def _pitch(t) -> int:
@@ -578,19 +582,33 @@ def _pitch(t) -> int:
     return t.stride(0) if t.shape[0] > 1 else t.shape[1]
 
 
-def _workspace(workspace, nbytes, device):
-    import torch
-    if nbytes == 0:
-        return None, 0
-    if workspace is None:
-        workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
-    return workspace, workspace.numel() * workspace.element_size()
-
-
-def _on_device(device, stream):
+def _stream_of(device, stream) -> int:
     """The stream of a call: the given one, or the device's current one."""
+    if stream is not None:
+        return stream.cuda_stream
     import torch
-    return (stream if stream is not None else torch.cuda.current_stream(device)).cuda_stream
+    return torch._C._cuda_getCurrentRawStream(device.index)
+
+
+def _with_workspace(fn, bytes_of, seqs, ref, head, tail, workspace, device, stream) -> None:
+    """fn(*seqs, *head, workspace, its bytes, stream): most calls need no workspace, so how much is only asked for
+    where none was given and the call says so."""
+    st = _stream_of(device, stream)
+    if workspace is not None:
+        _check(fn(*seqs, *head, *tail, workspace.data_ptr(), workspace.numel() * workspace.element_size(), st))
+        return
+    rc = fn(*seqs, *head, *tail, None, 0, st)
+    if rc == E_INVAL:
+        nbytes = bytes_of(*seqs, ref)
+        if nbytes:
+            import torch
+            ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
+            if stream is not None:
+                ws.record_stream(stream)
+            rc = fn(*seqs, *head, *tail, ws.data_ptr(), nbytes, st)
+        else:
+            rc = fn(*seqs, *head, *tail, None, 0, st)   # (for its message)
+    _check(rc)
 
 
 def attention_workspace_bytes(kvs, n_rows: Sequence[int], pos0: Optional[Sequence[int]] = None, rules: Optional[AttentionRules] = None) -> int:
@@ -605,21 +623,21 @@ def attention(kvs, layer: int, q, n_rows: Optional[Sequence[int]] = None, pos0: 
     """anpd_attention: new rows of one cache or of a list of caches over what is cached.  q: CUDA float32 or bfloat16
     [rows of all sequences][n_heads * head_dim].  Returns out, or (out, lse) where lse was given or asked for."""
     import torch
-    first, n, handles, counts, at = _sequences(kvs, q, n_rows, pos0, rules)
+    shape, n, handles, counts, at = _sequences(kvs, q, n_rows, pos0, rules)
+    rows = q.shape[0]
     if out is None:
-        out = torch.empty((q.shape[0], q.shape[1]), dtype=q.dtype, device=q.device)
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
     elif not (out.device == q.device and out.dtype == q.dtype and out.shape == q.shape and out.stride(1) == 1):
         raise ValueError("out must be like the rows")
-    if lse is None and want_lse:
-        lse = torch.empty((q.shape[0], first.model.shape.n_heads), dtype=torch.float32, device=q.device)
-    elif lse is not None and not (lse.device == q.device and lse.dtype == torch.float32 and lse.is_contiguous()
-                                  and tuple(lse.shape) == (q.shape[0], first.model.shape.n_heads)):
-        raise ValueError("lse: contiguous float32 [rows][n_heads]")
+    if lse is not None:
+        if not (lse.device == q.device and lse.dtype == torch.float32 and lse.is_contiguous() and tuple(lse.shape) == (rows, shape.n_heads)):
+            raise ValueError("lse: contiguous float32 [rows][n_heads]")
+    elif want_lse:
+        lse = torch.empty((rows, shape.n_heads), dtype=torch.float32, device=q.device)
     L, ref = lib(), None if rules is None else rules.ref
-    ws, nbytes = _workspace(workspace, L.anpd_attention_workspace_bytes(handles, n, counts, at, ref), q.device)
-    _check(L.anpd_attention(handles, n, counts, at, layer, q.data_ptr(), _pitch(q), F32 if q.dtype == torch.float32 else BF16, ref,
-                            out.data_ptr(), _pitch(out), None if lse is None else lse.data_ptr(), None if ws is None else ws.data_ptr(), nbytes,
-                            _on_device(q.device, stream)))
+    _with_workspace(L.anpd_attention, L.anpd_attention_workspace_bytes, (handles, n, counts, at), ref,
+                    (layer, q.data_ptr(), _pitch(q), F32 if q.dtype == torch.float32 else BF16, ref),
+                    (out.data_ptr(), _pitch(out), None if lse is None else lse.data_ptr()), workspace, q.device, stream)
     return out if lse is None else (out, lse)
 
 
@@ -628,8 +646,7 @@ def key_mass(kvs, layer: int, q, lse, mass, n_rows: Optional[Sequence[int]] = No
     """anpd_key_mass: adds the rows' weights to mass and returns it.  mass: CUDA float32 [n_kv_heads][>= keys] for one
     cache, [sequences][n_kv_heads][>= keys] for several; rows apart as they like, keys side by side."""
     import torch
-    first, n, handles, counts, at = _sequences(kvs, q, n_rows, pos0, rules)
-    shape = first.model.shape
+    shape, n, handles, counts, at = _sequences(kvs, q, n_rows, pos0, rules)
     each = mass if mass.dim() == 3 else mass[None]
     kv_heads = getattr(shape, "n_kv_heads", 0) or shape.n_heads
     if not (mass.dtype == torch.float32 and mass.device == q.device and each.dim() == 3 and each.shape[0] == n and each.shape[1] == kv_heads and each.stride(2) == 1):
@@ -637,15 +654,15 @@ def key_mass(kvs, layer: int, q, lse, mass, n_rows: Optional[Sequence[int]] = No
     if not (lse.device == q.device and lse.dtype == torch.float32 and lse.is_contiguous() and tuple(lse.shape) == (q.shape[0], shape.n_heads)):
         raise ValueError("lse: contiguous float32 [rows][n_heads]")
     ld = each.stride(1) if kv_heads > 1 else each.shape[2]
-    if ld < each.shape[2] or any(c + (kv.length if at is None else at[i]) > each.shape[2]
+    if ld < each.shape[2] or any(c and c + (kv.length if at is None else at[i]) > each.shape[2]
                                  for i, (c, kv) in enumerate(zip(counts, (kvs,) if isinstance(kvs, KVCache) else kvs))):
         raise ValueError("mass has fewer columns than there are keys")
     step, base = each.stride(0) * 4, each.data_ptr()
     ptrs = (C.c_void_p * n)(*[base + i * step for i in range(n)])
     L, ref = lib(), None if rules is None else rules.ref
-    ws, nbytes = _workspace(workspace, L.anpd_key_mass_workspace_bytes(handles, n, counts, at, ref), q.device)
-    _check(L.anpd_key_mass(handles, n, counts, at, layer, q.data_ptr(), _pitch(q), F32 if q.dtype == torch.float32 else BF16, ref,
-                           lse.data_ptr(), ptrs, ld, None if ws is None else ws.data_ptr(), nbytes, _on_device(q.device, stream)))
+    _with_workspace(L.anpd_key_mass, L.anpd_key_mass_workspace_bytes, (handles, n, counts, at), ref,
+                    (layer, q.data_ptr(), _pitch(q), F32 if q.dtype == torch.float32 else BF16, ref),
+                    (lse.data_ptr(), ptrs, ld), workspace, q.device, stream)
     return mass
 
 
@@ -666,7 +683,7 @@ def evict(src: KVCache, mass, keep: int, first: int = 0, last: int = 0, into: Op
     out = torch.empty((layers, kv_heads, max(0, keep)), dtype=torch.float32, device=mass.device)
     dst = src if into is None else into
     _check(lib().anpd_kv_evict(src._h, dst._h, mass.data_ptr(), ld, keep, first, last, rope_base, kept.data_ptr(), out.data_ptr(), max(0, keep),
-                               _on_device(mass.device, stream)))
+                               _stream_of(mass.device, stream)))
     return kept, out
 
 

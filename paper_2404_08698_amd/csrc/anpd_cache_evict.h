@@ -19,6 +19,14 @@ __device__ __forceinline__ uint32_t mass_rank(float x)
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
+__device__ __forceinline__ float mass_of_rank(uint32_t r) { return r == 0 ? __builtin_nanf("") : __uint_as_float(r & 0x80000000u ? r & 0x7fffffffu : ~r); }
+
+// n and the lanes of the mask before this one
+__device__ __forceinline__ uint32_t lanes_below(unsigned long long mask, uint32_t n)
+{
+    return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, n));
+}
+
 struct SelectArgs {
     const float *mass;   // [layer][head][ld]
     int32_t *kept;       // [layer][head][keep]
@@ -89,11 +97,18 @@ __global__ __launch_bounds__(kSelectThreads) void cache_select_kernel(const Sele
     if constexpr (HELD > 0) {
         for (int bit = 31; bit >= 0; --bit) {
             const uint32_t t = limit | (1u << bit);
-            uint32_t n = 0;
+            // (two of three are counted by the scalar unit, which the compute unit's waves share, the third by the lanes themselves)
+            uint32_t n = 0, own = 0;
 #pragma unroll
             for (int k = 0; k < HELD; ++k) {
-                n += (uint32_t)__builtin_popcountll(__builtin_amdgcn_ballot_w64(held[k] >= t));
-                if (k % 4 == 3) asm volatile("" : "+s"(n));   // (all comparisons first would be more than the scalar registers hold)
+                if (HELD >= 16 && k % 3 == 2) {
+                    own += held[k] >= t ? 1u : 0u;
+                    asm volatile("" : "+s"(n), "+v"(own));   // (all comparisons first would be more than the scalar registers hold)
+                } else n += (uint32_t)__builtin_popcountll(__builtin_amdgcn_ballot_w64(held[k] >= t));
+            }
+            if (HELD >= 16) {
+#pragma unroll
+                for (int b = 0; b < 5; ++b) n += (uint32_t)__builtin_popcountll(__builtin_amdgcn_ballot_w64((own >> b) & 1u)) << b;   // (21 at most)
             }
             if (lane == 0) ((uint32_t *)counts[bit & 1])[wave] = n;
             __syncthreads();   // (the other half of the counts is read until the next one)
@@ -160,25 +175,34 @@ __global__ __launch_bounds__(kSelectThreads) void cache_select_kernel(const Sele
     limit = (uint32_t)__builtin_amdgcn_readfirstlane((int)limit);
     int from = lane;
     asm volatile("" : "+s"(limit), "+v"(from));   // (comparisons and addresses are made again: those of above would fill the registers)
-    const unsigned long long below = (1ull << lane) - 1;
-    // (eight times 64 positions side by side: the masses that go along are loads)
+    // (eight times 64 positions side by side)
     constexpr int BATCH = HELD > 0 && HELD < 8 ? HELD : 8;
     auto write = [&](int k0, const uint32_t (&rank)[BATCH]) __attribute__((always_inline)) {
         uint32_t to[BATCH];
         float x[BATCH];
 #pragma unroll
         for (int u = 0; u < BATCH; ++u) {
-            const bool tie = rank[u] == limit && k0 + u < steps;
-            const unsigned long long e = __builtin_amdgcn_ballot_w64(tie);
-            const bool stays = (rank[u] > limit && k0 + u < steps) || (tie && ties + (uint32_t)__builtin_popcountll(e & below) < left);
-            const unsigned long long g = __builtin_amdgcn_ballot_w64(stays);
-            to[u] = stays ? at + (uint32_t)__builtin_popcountll(g & below) : ~0u;
+            bool stays = rank[u] > limit && k0 + u < steps;
+            unsigned long long g = __builtin_amdgcn_ballot_w64(stays);
+            if (ties < left) {   // (the same for the whole wave, as what follows)
+                const bool tie = rank[u] == limit && k0 + u < steps;
+                const unsigned long long e = __builtin_amdgcn_ballot_w64(tie);
+                if (e != 0) {
+                    stays = stays || (tie && lanes_below(e, ties) < left);
+                    g = __builtin_amdgcn_ballot_w64(stays);
+                    ties += (uint32_t)__builtin_popcountll(e);
+                }
+            }
+            to[u] = stays ? lanes_below(g, at) : ~0u;
             at += (uint32_t)__builtin_popcountll(g);
-            ties += (uint32_t)__builtin_popcountll(e);
         }
+        // (a rank says which number it was made from; those that stay in any case are read again)
         if (out) {
 #pragma unroll
-            for (int u = 0; u < BATCH; ++u) x[u] = to[u] != ~0u ? mass[p0 + 64 * (k0 + u) + from] : 0.f;
+            for (int u = 0; u < BATCH; ++u) {
+                x[u] = mass_of_rank(rank[u]);
+                if (rank[u] == ~0u && to[u] != ~0u) x[u] = mass[p0 + 64 * (k0 + u) + from];
+            }
         }
 #pragma unroll
         for (int u = 0; u < BATCH; ++u) {
@@ -213,6 +237,7 @@ struct MoveArgs {
     const void *src;
     void *dst;
     const int32_t *src_table, *dst_table, *kept;
+    int32_t *dst_len;   // (device copy of the length)
     double turn[64];    // theta / (2 pi) of every rotary pair
     int32_t rotate, keep, n_layers, n_kv_heads, page_tokens;
 };
@@ -239,6 +264,7 @@ template <int DH>
 __global__ __launch_bounds__(kMoveThreads) void cache_move_kernel(const MoveArgs a)
 {
     const int tid = threadIdx.x, layer = blockIdx.x / a.n_kv_heads, head = blockIdx.x - layer * a.n_kv_heads, kind = blockIdx.y;
+    if (blockIdx.x + blockIdx.y + blockIdx.z == 0 && tid == 0) *a.dst_len = a.keep;
     const int32_t *kept = a.kept + (size_t)blockIdx.x * a.keep;
     const int pages = (a.keep + 15) / 16;
     const bf16_t *src = (const bf16_t *)a.src;
@@ -326,6 +352,7 @@ __global__ __launch_bounds__(kMoveThreads) void cache_move_plain_kernel(const Mo
 {
     constexpr int PAIRS = DH / 2, TOKENS = kMovePages * 16, STEPS = TOKENS * PAIRS / kMoveThreads;
     const int tid = threadIdx.x, layer = blockIdx.x / a.n_kv_heads, head = blockIdx.x - layer * a.n_kv_heads, kind = blockIdx.y, pt = a.page_tokens;
+    if (blockIdx.x + blockIdx.y + blockIdx.z == 0 && tid == 0) *a.dst_len = a.keep;
     const int32_t *kept = a.kept + (size_t)blockIdx.x * a.keep;
     const KT *src = (const KT *)a.src;
     KT *dst = (KT *)a.dst;

@@ -452,6 +452,7 @@ int32_t anpd_kv_evict(const anpd_kv_t *src, anpd_kv_t *dst, const float *mass, i
         m.dst = dst->pool;
         m.src_table = src->d_table;
         m.dst_table = dst->d_table;
+        m.dst_len = dst->d_len;
         m.kept = out_kept;
         m.rotate = rope_base > 0.f;
         m.keep = keep;
@@ -471,8 +472,12 @@ int32_t anpd_kv_evict(const anpd_kv_t *src, anpd_kv_t *dst, const float *mass, i
         else hipLaunchKernelGGL((cache_move_plain_kernel<float, 64>), grid, dim3(kMoveThreads), 0, st, m);
 #undef ANPD_MOVE
         HIP_TRY(hipGetLastError());
+        HIP_TRY(hipStreamSynchronize(st));
+        dst->len = keep;
+        release_pages(dst, keep);
+        return ANPD_OK;
     }
-    return anpd_kv_truncate(dst, keep, stream);
+    return anpd_kv_truncate(dst, 0, stream);
 }
 
 }  // extern "C"
