@@ -355,7 +355,7 @@ int32_t anpd_linear_static(const float *X, const void *W, float *Y, int32_t M, i
  * Operators on caches, one layer at a time: attention of new rows over the cached keys and values, the weight that
  * every cached key receives, and the eviction of the keys that receive little.  For programs whose layers are their
  * own (other projections, capped or biased scores, sliding windows, packed documents), beside anpd_linear, and to
- * shorten the cache that anpd_prefill has filled before the steps that follow.
+ * shorten the cache that anpd_prefill has filled before the steps that follow (anpd_kv_observe).
  * Head dims 64 and 128.  Sums, maxima and outputs are formed in 32 bits; results do not depend on timing (no
  * floating-point atomics), but on how the keys are divided among blocks, which depends on the sizes of a call.
  * ---------------------------------------------------------------------- */
@@ -417,6 +417,17 @@ size_t anpd_key_mass_workspace_bytes(const anpd_kv_t *const *kvs, int32_t n_seq,
 int32_t anpd_key_mass(const anpd_kv_t *const *kvs, int32_t n_seq, const int32_t *n_rows, const int32_t *pos0, int32_t layer,
                       const void *q, int64_t ldq, int32_t dtype, const anpd_attn_rules *rules, const float *lse,
                       float *const *mass, int64_t ld_mass, void *workspace, size_t workspace_bytes, void *stream);
+
+/* The weights of a model's own prompts.  While set, every anpd_prefill into kv adds, per layer, what the last `rows` positions
+ * of its prompt (all of a shorter one) give to the keys they see, as anpd_key_mass does, for an eviction before the steps
+ * that follow: rows that look back at the whole prompt say which of it matters.  The prompt's results are the same.
+ *   mass: DEVICE, [n_layers][n_kv_heads][ld_mass] floats, borrowed until the next call of this; NULL = no longer.  An
+ *   anpd_prefill that reaches beyond ld_mass positions is refused (ANPD_E_CAPACITY).
+ *   rows: 1..ANPD_MAX_WINDOW.  workspace: DEVICE, 256-byte aligned, >= anpd_kv_observe_workspace_bytes(kv, rows), borrowed like mass
+ *   and used by those prompts only.
+ * Steps (anpd_verify and its like) add nothing.  Matrix-core models only: ANPD_E_UNIMPLEMENTED otherwise. */
+size_t anpd_kv_observe_workspace_bytes(const anpd_kv_t *kv, int32_t rows);
+int32_t anpd_kv_observe(anpd_kv_t *kv, float *mass, int64_t ld_mass, int32_t rows, void *workspace, size_t workspace_bytes);
 
 /* Eviction: of src's committed positions `keep` stay, per layer and key / value head those with the largest mass
  * (equal ones: the lowest position; NaN counts as less than every number), the first `first` and the last `last` in any case.  They

@@ -35,6 +35,7 @@ EXPORTS = (
     "anpd_model_trace", "anpd_model_set_barrier_spin_limit", "anpd_linear_static",
     "anpd_cache_pool_bytes", "anpd_cache_create", "anpd_attention_workspace_bytes", "anpd_attention",
     "anpd_key_mass_workspace_bytes", "anpd_key_mass", "anpd_kv_evict",
+    "anpd_kv_observe_workspace_bytes", "anpd_kv_observe",
 )
 PROF_CATEGORIES = ("gemm_qkv", "gemm_o", "gemm_gate_up", "gemm_down", "gemm_lm_head", "attn", "other", "step")
 
@@ -172,6 +173,10 @@ def lib():
     L.anpd_key_mass.argtypes = seqs + [C.c_int32, vp, C.c_int64, C.c_int32, vp, vp, vp, C.c_int64, vp, C.c_size_t, vp]
     L.anpd_kv_evict.restype = C.c_int32
     L.anpd_kv_evict.argtypes = [vp, vp, vp, C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_float, vp, vp, C.c_int64, vp]
+    L.anpd_kv_observe_workspace_bytes.restype = C.c_size_t
+    L.anpd_kv_observe_workspace_bytes.argtypes = [vp, C.c_int32]
+    L.anpd_kv_observe.restype = C.c_int32
+    L.anpd_kv_observe.argtypes = [vp, vp, C.c_int64, C.c_int32, vp, C.c_size_t]
     _lib = L
     return L
 
@@ -351,6 +356,7 @@ class KVCache:
         self._h = h
         self.max_tokens = max_tokens
         self.n_layers = model.shape.n_layers
+        self.n_kv_heads = int(getattr(model.shape, "n_kv_heads", 0) or model.shape.n_heads)
 
     def close(self):
         try:
@@ -393,6 +399,24 @@ class KVCache:
         v = torch.empty(n, d, dtype=torch.float32, device=self.model.device)
         _check(lib().anpd_kv_read(self._h, layer, pos0, n, k.data_ptr(), v.data_ptr(), _stream_ptr(stream)))
         return k, v
+
+    def observe(self, mass, rows: int = 32) -> None:
+        """anpd_kv_observe: prompts into this cache add the weights of their last rows to mass, CUDA float32
+        [n_layers][n_kv_heads][positions that they may reach], contiguous (None: no longer)."""
+        import torch
+        if mass is None:
+            _check(lib().anpd_kv_observe(self._h, None, 0, 0, None, 0))
+            self._observed = None
+            return
+        if not (mass.is_cuda and mass.device == self.pool.device and mass.dtype == torch.float32 and mass.dim() == 3 and mass.is_contiguous()
+                and tuple(mass.shape[:2]) == (self.n_layers, self.n_kv_heads)):
+            raise ValueError("mass: contiguous float32 [n_layers][n_kv_heads][positions] on the cache's device")
+        nbytes = lib().anpd_kv_observe_workspace_bytes(self._h, rows)
+        if nbytes == 0:
+            _check(E_INVAL)
+        ws = torch.empty(nbytes, dtype=torch.uint8, device=mass.device)
+        _check(lib().anpd_kv_observe(self._h, mass.data_ptr(), mass.shape[2], rows, ws.data_ptr(), nbytes))
+        self._observed = (mass, ws)     # kept alive
 
 
 def verify(model: Model, kv: KVCache, window: Sequence[int], mode: int = VERIFY, want_predicts: bool = False,
@@ -525,6 +549,7 @@ class LayerCache(KVCache):
         self._h = h
         self.max_tokens = max_tokens
         self.n_layers = n_layers
+        self.n_kv_heads = n_kv_heads or n_heads
 
 
 class AttentionRules:
@@ -648,7 +673,7 @@ def key_mass(kvs, layer: int, q, lse, mass, n_rows: Optional[Sequence[int]] = No
     import torch
     shape, n, handles, counts, at = _sequences(kvs, q, n_rows, pos0, rules)
     each = mass if mass.dim() == 3 else mass[None]
-    kv_heads = getattr(shape, "n_kv_heads", 0) or shape.n_heads
+    kv_heads = (kvs if isinstance(kvs, KVCache) else kvs[0]).n_kv_heads
     if not (mass.dtype == torch.float32 and mass.device == q.device and each.dim() == 3 and each.shape[0] == n and each.shape[1] == kv_heads and each.stride(2) == 1):
         raise ValueError("mass: float32 [sequences][n_kv_heads][keys] on the caches' device")
     if not (lse.device == q.device and lse.dtype == torch.float32 and lse.is_contiguous() and tuple(lse.shape) == (q.shape[0], shape.n_heads)):
@@ -673,9 +698,7 @@ def evict(src: KVCache, mass, keep: int, first: int = 0, last: int = 0, into: Op
     import torch
     if not (mass.is_cuda and mass.device == src.pool.device and mass.dtype == torch.float32 and mass.dim() == 3 and mass.stride(2) == 1):
         raise ValueError("mass: float32 [n_layers][n_kv_heads][positions] on the cache's device")
-    shape = src.model.shape
-    kv_heads = getattr(shape, "n_kv_heads", 0) or shape.n_heads
-    layers = src.n_layers
+    layers, kv_heads = src.n_layers, src.n_kv_heads
     if mass.shape[:2] != (layers, kv_heads) or mass.shape[2] < src.length or (layers > 1 and mass.stride(0) != kv_heads * mass.stride(1)):
         raise ValueError("mass: one row of at least the cache's length per layer and key / value head, equally far apart")
     ld = mass.stride(1) if layers * kv_heads > 1 else mass.shape[2]

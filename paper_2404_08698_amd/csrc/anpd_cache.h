@@ -48,6 +48,11 @@ struct anpd_kv {
     int32_t *d_table, *d_len;
     int32_t *pin;                    // pinned staging: [0] length, [1..] table
     bool table_dirty;
+    // prompts whose last rows' weights are wanted (anpd_kv_observe)
+    float *seen_mass;
+    int64_t seen_ld;
+    int32_t seen_rows;
+    char *seen_ws;
 };
 
 namespace anpd {
@@ -58,5 +63,9 @@ int32_t ensure_pages(anpd_kv *kv, int32_t upto, hipStream_t st);
 void release_pages(anpd_kv *kv, int32_t len);
 // A cache in caller-owned device memory (checked by the caller of this); `who` names the entry point in messages.
 int32_t make_cache(const char *who, const anpd_model *m, const CacheShape &shape, void *pool, size_t pool_bytes, int32_t max_tokens, anpd_kv **out);
+
+// Adds the weights of the last rows of a prompt of P rows, whose queries are the split operand qp of G row groups, to the cache's
+// observed mass of this layer (their keys are cached, the length is still that before the prompt).
+int32_t observe_layer(const anpd_kv *kv, int32_t layer, const void *qp, int32_t G, int32_t P, hipStream_t st);
 
 }  // namespace anpd

@@ -1378,4 +1378,15 @@ __global__ void cache_mass_join_kernel(const AttnArgs a, const MassOut to)
     if (key < total && used > 0) to.mass[seq][(size_t)kvh * to.ld + key] += sum;
 }
 
+// ------------------------------------------------------------------ rows of a prompt
+//
+// The last rows of a prompt out of its queries' split operand [head][row group][dims / 32][hi | lo][lane][8] (lane = 16 * (dims % 32 / 8) +
+// row of the group) as fp32 rows [n][heads * DH]; m0: first one among the operand's rows.   grid: (n, heads), DH threads
+__global__ void prompt_rows_kernel(const bf16_t *__restrict__ qp, float *__restrict__ q, int G, int m0, int head_dim)
+{
+    const int r = blockIdx.x, head = blockIdx.y, dim = threadIdx.x, m = m0 + r;
+    const size_t at = ((((size_t)head * G + (m >> 4)) * (head_dim >> 5) + (dim >> 5)) * 2 * 64 + ((dim >> 3) & 3) * 16 + (m & 15)) * 8 + (dim & 7);
+    q[((size_t)r * gridDim.y + head) * head_dim + dim] = bf16_to_f32(qp[at]) + bf16_to_f32(qp[at + 64 * 8]);
+}
+
 }  // namespace anpd

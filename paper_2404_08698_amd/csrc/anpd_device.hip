@@ -314,6 +314,7 @@ int32_t make_cache(const char *who, const anpd_model *m, const CacheShape &shape
     kv->d_table = kv->d_len + 1;
     kv->table_dirty = true;
     kv->pin = nullptr;
+    kv->seen_mass = nullptr;
     hipError_t e = hipHostMalloc((void **)&kv->pin, ((size_t)kv->n_pages + 1) * sizeof(int32_t), hipHostMallocDefault);
     if (e == hipSuccess) e = hipMemset(kv->pool, 0, need);  // unwritten slots must read as zeros, never as NaN patterns
     if (e == hipSuccess) {
@@ -1267,7 +1268,9 @@ int32_t run_prefill_mfma(anpd_model *m, anpd_kv *kv, int P, char *pws, const Pre
         // Behind the last layer's keys and values only the last row is wanted, so everything from its queries on works on that row's
         // group alone (4 layers, 205 / 512 / 3584 rows 1116 -> 1028 us (ChatGLM3 shape), 1546 -> 1369, 10641 -> 8811; a layer's GEMMs
         // and attention are then 0.11 ms whatever the rows: of 32 layers it saves the better part of one).
-        const int g0 = l + 1 == c.n_layers ? G - 1 : 0;
+        // (an observed prompt: on the groups of the rows whose weights are wanted)
+        const int last_rows = kv->seen_mass && kv->seen_rows < P ? kv->seen_rows : (kv->seen_mass ? P : 1);
+        const int g0 = l + 1 == c.n_layers ? (r0 + P - last_rows) / 16 : 0;
         {
             PrefillArgs a = base;
             a.Wp = (const uint4 *)(ws + L.wp_qkv[(size_t)l]);
@@ -1298,6 +1301,10 @@ int32_t run_prefill_mfma(anpd_model *m, anpd_kv *kv, int P, char *pws, const Pre
             else if (shared) ANPD_ATTN_P(64, true);
             else ANPD_ATTN_P(64, false);
 #undef ANPD_ATTN_P
+        }
+        if (kv->seen_mass) {
+            HIP_TRY(hipGetLastError());
+            if ((rc = observe_layer(kv, l, qp, G, P, st)) != ANPD_OK) return rc;
         }
         mark(m, ANPD_PROF_ATTN, st);
         {
@@ -1993,6 +2000,8 @@ int32_t anpd_prefill(anpd_model_t *m, anpd_kv_t *kv, const int32_t *tokens, int3
     for (int i = 0; i < n_tokens; ++i)
         if (tokens[i] < 0 || tokens[i] >= m->cfg.vocab)
             return fail(ANPD_E_RANGE, "anpd_prefill: token %d at tokens[%d] outside [0, %d)", tokens[i], i, m->cfg.vocab);
+    if (kv->seen_mass && kv->len + n_tokens > kv->seen_ld)
+        return fail(ANPD_E_CAPACITY, "anpd_prefill: length %d + %d tokens exceeds the observed mass (%lld)", kv->len, n_tokens, (long long)kv->seen_ld);
     hipStream_t st = (hipStream_t)stream;
     const size_t V = (size_t)m->cfg.vocab;
 

@@ -63,9 +63,9 @@ int32_t gather(const char *who, const anpd_kv *const *kvs, int32_t n_seq, const 
         if (n < 0 || at < 0) return fail(ANPD_E_INVAL, "%s: sequence %d: %d rows from position %d on", who, s, n, at);
         if ((int64_t)at + n > kv->max_tokens)
             return fail(ANPD_E_CAPACITY, "%s: sequence %d: position %d + %d rows exceeds capacity %d", who, s, at, n, kv->max_tokens);
-        if (n > 0)
-            for (int lp = (at + n - 1) / c.page_tokens; lp >= 0; --lp)
-                if (kv->table[(size_t)lp] < 0) return fail(ANPD_E_INVAL, "%s: sequence %d: position %d has no page", who, s, lp * c.page_tokens);
+        // (pages are given from the first position on and taken from the last: the last row's is there only with all before it)
+        if (n > 0 && kv->table[(size_t)((at + n - 1) / c.page_tokens)] < 0)
+            return fail(ANPD_E_INVAL, "%s: sequence %d: position %d has no page", who, s, at + n - 1);
         if ((int64_t)n * a.group >= (1 << 30)) return fail(ANPD_E_CAPACITY, "%s: sequence %d has too many rows", who, s);
         a.seq[s] = {kv->pool, kv->d_table, at, n, (int32_t)rows, 0};
         rows += n;
@@ -314,7 +314,52 @@ bool cache_cfg_ok(const char *who, const anpd_cache_cfg *c, int32_t max_tokens, 
     return true;
 }
 
+// What an observed prompt needs per layer: queries, outputs, logarithms and a workspace that suffices at every length. Attention's: a block of
+// rows per split and item, splits as plan_attention bounds them; the mass's: a sum per key and part of at least eight row tiles.
+struct ObserveLayout {
+    size_t q, out, lse, work, work_bytes, total;
+};
+ObserveLayout observe_layout(const CacheShape &c, int max_tokens, int rows, int n_cu)
+{
+    ObserveLayout L;
+    const size_t width = (size_t)c.n_heads * c.head_dim, v = (size_t)rows * (c.n_heads / c.n_kv_heads), cu = (size_t)n_cu;
+    size_t o = 0;
+    auto take = [&](size_t bytes) { const size_t at = o; o = align_up(o + bytes); return at; };
+    L.q = take((size_t)rows * width * sizeof(float));
+    L.out = take((size_t)rows * width * sizeof(float));
+    L.lse = take((size_t)rows * c.n_heads * sizeof(float));
+    const size_t few = (v + kRowTile - 1) / kRowTile * c.n_kv_heads, many = (v + tile_rows(1) - 1) / tile_rows(1) * c.n_kv_heads;
+    const size_t keys = ((size_t)max_tokens + 2 * kMassKeys - 1) / (2 * kMassKeys) * (2 * kMassKeys), parts = ((v + 31) / 32 + 1 + 7) / 8;
+    size_t floats = (few + 2 * cu) * part_floats(kRowTile, c.head_dim);
+    const size_t shared = (many + cu) * part_floats(tile_rows(1), c.head_dim), mass = parts > 1 ? keys * c.n_kv_heads * parts : 0;
+    if (shared > floats) floats = shared;
+    if (mass > floats) floats = mass;
+    L.work_bytes = align_up(floats * sizeof(float));
+    L.work = take(L.work_bytes);
+    L.total = o;
+    return L;
+}
+
 }  // namespace
+
+namespace anpd {
+
+int32_t observe_layer(const anpd_kv *kv, int32_t layer, const void *qp, int32_t G, int32_t P, hipStream_t st)
+{
+    const CacheShape &c = kv->shape;
+    const int rows = kv->seen_rows < P ? kv->seen_rows : P, pos0 = kv->len + P - rows;
+    const ObserveLayout L = observe_layout(c, kv->max_tokens, kv->seen_rows, kv->n_cu);
+    float *q = (float *)(kv->seen_ws + L.q), *lse = (float *)(kv->seen_ws + L.lse), *mass = kv->seen_mass + (size_t)layer * c.n_kv_heads * kv->seen_ld;
+    const int64_t width = (int64_t)c.n_heads * c.head_dim;
+    hipLaunchKernelGGL(prompt_rows_kernel, dim3((unsigned)rows, (unsigned)c.n_heads), dim3((unsigned)c.head_dim), 0, st, (const bf16_t *)qp, q, G,
+                       (kv->len & 15) + P - rows, c.head_dim);
+    HIP_TRY(hipGetLastError());
+    const int32_t rc = anpd_attention(&kv, 1, &rows, &pos0, layer, q, width, ANPD_F32, nullptr, kv->seen_ws + L.out, width, lse, kv->seen_ws + L.work, L.work_bytes, st);
+    if (rc != ANPD_OK) return rc;
+    return anpd_key_mass(&kv, 1, &rows, &pos0, layer, q, width, ANPD_F32, nullptr, lse, &mass, kv->seen_ld, kv->seen_ws + L.work, L.work_bytes, st);
+}
+
+}  // namespace anpd
 
 extern "C" {
 
@@ -412,6 +457,37 @@ int32_t anpd_key_mass(const anpd_kv_t *const *kvs, int32_t n_seq, const int32_t 
     OnDevice on;
     if ((rc = on.enter(who, kvs[0]->device)) != ANPD_OK) return rc;
     return c.head_dim == 128 ? launch_mass<128>(a, to, c, sets, (hipStream_t)stream) : launch_mass<64>(a, to, c, sets, (hipStream_t)stream);
+}
+
+size_t anpd_kv_observe_workspace_bytes(const anpd_kv_t *kv, int32_t rows)
+{
+    if (!kv || rows < 1 || rows > ANPD_MAX_WINDOW) {
+        fail(ANPD_E_INVAL, "anpd_kv_observe_workspace_bytes: bad argument");
+        return 0;
+    }
+    return observe_layout(kv->shape, kv->max_tokens, rows, kv->n_cu).total;
+}
+
+int32_t anpd_kv_observe(anpd_kv_t *kv, float *mass, int64_t ld_mass, int32_t rows, void *workspace, size_t workspace_bytes)
+{
+    const char *who = "anpd_kv_observe";
+    if (!kv) return fail(ANPD_E_INVAL, "%s: NULL cache", who);
+    if (!mass) {
+        kv->seen_mass = nullptr;
+        return ANPD_OK;
+    }
+    if (!kv->m) return fail(ANPD_E_INVAL, "%s: the cache has no model whose prompts could be observed", who);
+    if (!kv->shape.fragments) return fail(ANPD_E_UNIMPLEMENTED, "%s: matrix-core models only", who);
+    if (rows < 1 || rows > ANPD_MAX_WINDOW) return fail(ANPD_E_INVAL, "%s: rows must be in 1..%d", who, ANPD_MAX_WINDOW);
+    if (ld_mass < 1 || ((uintptr_t)mass & 3) != 0) return fail(ANPD_E_INVAL, "%s: bad mass", who);
+    if (!workspace || ((uintptr_t)workspace & 255) != 0) return fail(ANPD_E_INVAL, "%s: workspace must be a 256-byte aligned device buffer", who);
+    const size_t need = observe_layout(kv->shape, kv->max_tokens, rows, kv->n_cu).total;
+    if (workspace_bytes < need) return fail(ANPD_E_CAPACITY, "%s: workspace has %zu bytes, %zu needed", who, workspace_bytes, need);
+    kv->seen_mass = mass;
+    kv->seen_ld = ld_mass;
+    kv->seen_rows = rows;
+    kv->seen_ws = (char *)workspace;
+    return ANPD_OK;
 }
 
 int32_t anpd_kv_evict(const anpd_kv_t *src, anpd_kv_t *dst, const float *mass, int64_t ld_mass, int32_t keep, int32_t first, int32_t last, float rope_base,

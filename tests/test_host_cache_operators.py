@@ -228,6 +228,31 @@ def test_workspaces(stub):
     run(stub, "child_workspace")
 
 
+def child_observed():
+    """What is asked for observed prompts suffices for their rows at every length."""
+    c = Caches()
+    import random
+    rng = random.Random(1)
+    for heads, kv_heads, dim in ((4, 2, 64), (32, 32, 128), (32, 2, 128), (64, 1, 64), (71, 1, 64)):
+        for cap in (40, 700, 9000, 200000):
+            kv = c.cache(cap, cap, heads, kv_heads, dim, layers=1)
+            for _ in range(40):
+                rows = rng.randint(1, min(cap, 32))
+                n = rng.choice((cap, rng.randint(rows, cap)))
+                h, r, p = (C.c_void_p * 1)(kv), (C.c_int32 * 1)(rows), (C.c_int32 * 1)(n - rows)
+                need = max(c.L.anpd_attention_workspace_bytes(h, 1, r, p, None), c.L.anpd_key_mass_workspace_bytes(h, 1, r, p, None))
+                assert c.L.anpd_kv_observe_workspace_bytes(kv, rows) >= need + 8 * rows * heads * dim + 4 * rows * heads, (heads, cap, rows, n)
+    assert c.L.anpd_kv_observe_workspace_bytes(kv, 0) == c.L.anpd_kv_observe_workspace_bytes(kv, 33) == c.L.anpd_kv_observe_workspace_bytes(None, 1) == 0
+    m = c.memory(1 << 12)
+    assert c.L.anpd_kv_observe(kv, m, 10, 1, m, 1 << 12) == c.B.E_INVAL      # no model
+    assert c.L.anpd_kv_observe(None, m, 10, 1, m, 1 << 12) == c.B.E_INVAL
+    assert c.L.anpd_kv_observe(kv, None, 0, 0, None, 0) == 0
+
+
+def test_observed_prompts_workspace(stub):
+    run(stub, "child_observed")
+
+
 def child_device():
     c = Caches()
     kv = c.cache(100, 50, device=3)
