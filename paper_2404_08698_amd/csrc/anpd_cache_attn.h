@@ -992,6 +992,15 @@ __global__ __launch_bounds__(256, 1) void cache_attn_plain_kernel(const AttnArgs
     for (int i = i0; i < i1; ++i) {
         const int base = tiles.at(i) * kStreamTile + 32 * wave;
         if (!any_seen<true>(r, pre, base)) continue;
+        // (all of the tile's loads before the first product: one at a time, between the products, they were most of the time)
+        float v[16][NDT];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const int j = base + 8 * (e >> 2) + 4 * half + (e & 3), key = j < total ? j : total - 1;
+            const KT *p = pool + kv_offset(s.table[key / pt], a.layer, a.n_layers, 1, kvh, a.n_kv_heads, key % pt, pt, DH) + m;
+#pragma unroll
+            for (int d = 0; d < NDT; ++d) v[e][d] = load_f32(p, 32 * d);
+        }
         f32x16 sc[1];
 #pragma unroll
         for (int e = 0; e < 16; ++e) sc[0][e] = 0.f;
@@ -1003,22 +1012,19 @@ __global__ __launch_bounds__(256, 1) void cache_attn_plain_kernel(const AttnArgs
             for (int t = 0; t < DH / 2; ++t) sc[0] = mfma32f(k[t], q[t], sc[0]);
         }
         weigh<true, 1, NDT>(a, r, pre, base, sc, run);
-        const bool hidden = !all_seen<true>(r, pre, base);
+        if (!all_seen<true>(r, pre, base))
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            const int j = base + 8 * (e >> 2) + 4 * half + (e & 3), key = j < total ? j : total - 1;
-            const KT *p = pool + kv_offset(s.table[key / pt], a.layer, a.n_layers, 1, kvh, a.n_kv_heads, key % pt, pt, DH) + m;
+            for (int e = 0; e < 16; ++e)
 #pragma unroll
-            for (int d = 0; d < NDT; ++d) {
-                float v = load_f32(p, 32 * d);
-                if (hidden) {
-                    const bool fin = fabsf(v) <= 3.4028234e38f;
+                for (int d = 0; d < NDT; ++d) {
+                    const bool fin = fabsf(v[e][d]) <= 3.4028234e38f;
                     unbounded |= __builtin_amdgcn_ballot_w64(!fin) != 0;
-                    v = fin ? v : 0.f;
+                    v[e][d] = fin ? v[e][d] : 0.f;
                 }
-                run.o[d] = mfma32f(v, sc[0][e], run.o[d]);
-            }
-        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+#pragma unroll
+            for (int d = 0; d < NDT; ++d) run.o[d] = mfma32f(v[e][d], sc[0][e], run.o[d]);
     }
     if (unbounded)
         for (int i = i0; i < i1; ++i) {

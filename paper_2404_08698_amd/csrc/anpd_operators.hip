@@ -171,8 +171,12 @@ Plan plan_attention(AttnArgs &a, const CacheShape &c, int n_cu)
     const int longest = most[p.shared];
     if (p.shared) a.chunk = (int)shared_chunk;
     else {
-        splits = items > 0 ? (2 * n_cu + items - 1) / items : 1;
-        if (splits > longest / 2) splits = longest / 2;
+        // Two blocks for each compute unit, of at least two tiles: a tile is about 1.3 us, joining 2.5 (32 heads of 128, 1 / 32 rows behind
+        // 1000 positions 9.1 / 11.3 us, a tile each 9.7 / 14.4).  Caches in plain order, whose tiles take four times that, a tile each, and one block
+        // of heads of 128, which fill a unit's registers (fp32, 4 heads of 64, 8 rows behind 1000 16 -> 13, 32 of 128, a row behind 1000 23 -> 19).
+        const int per_unit = c.fragments || c.head_dim == 64 ? 2 : 1, least = c.fragments ? 2 : 1;
+        splits = items > 0 ? (per_unit * n_cu + items - 1) / items : 1;
+        if (splits > longest / least) splits = longest / least;
         if (splits < 1) splits = 1;
         a.chunk = (int)((longest + splits - 1) / splits);
     }
