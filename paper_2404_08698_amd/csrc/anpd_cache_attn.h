@@ -47,7 +47,7 @@ struct AttnArgs {
     const int32_t *first_key;   // [rows] or NULL
     float *part;                // attention: partial results of splits, or NULL; mass: partial sums, or NULL
     int64_t ldq, ldo;           // elements between rows
-    float scale, cap;
+    float scale, cap, scale_over_cap;
     int32_t window, prefix;     // 0: none
     int32_t layer, n_layers, n_heads, n_kv_heads, group, page_tokens;
     int32_t q_f32, q_wide;      // type of the rows and outputs; whether rows and outputs may be moved 16 bytes at a time
@@ -142,25 +142,27 @@ __device__ __forceinline__ int first_tile(const KeyTiles &k, int fk, int i0, int
     return i < i0 ? i0 : (i < i1 ? i : i1);
 }
 
-// tanh, to 2^-23 of its value: a sum of powers where 1 - 2 / (1 + e^2x) would lose them
+// cap tanh(t / cap) of a product t / scale: x = t / cap.  1 - 2 / (1 + e^2x) is off by 2^-22 of the cap at most, whatever x is, which is
+// nothing beside weights in bf16 (ROUGH); otherwise small x take a sum of powers, to 2^-23 of the value.
+template <bool ROUGH>
 __device__ __forceinline__ float tanh_f32(float x)
 {
+    const float t = fmaf(-2.0f, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * (2.0f * kLog2e))), 1.0f);
+    if (ROUGH) return t;
     const float y = x * x;
     float s = fmaf(y, -1382.0f / 155925.0f, 62.0f / 2835.0f);
     s = fmaf(y, s, -17.0f / 315.0f);
     s = fmaf(y, s, 2.0f / 15.0f);
     s = fmaf(y, s, -1.0f / 3.0f);
     s = fmaf(y * x, s, x);
-    const float e = __builtin_amdgcn_exp2f(fabsf(x) * (2.0f * kLog2e));
-    const float t = 1.0f - 2.0f / (1.0f + e);
-    return y < 0.08f ? s : copysignf(t, x);
+    return y < 0.08f ? s : t;
 }
 
 // Products to scores where there are rules (cap, bias): natural units.
+template <bool ROUGH>
 __device__ __forceinline__ float ruled_score(const AttnArgs &a, float product, float slope, int distance)
 {
-    float t = product * a.scale;
-    if (a.cap > 0.f) t = a.cap * tanh_f32(t / a.cap);
+    float t = a.cap > 0.f ? a.cap * tanh_f32<ROUGH>(product * a.scale_over_cap) : product * a.scale;
     if (a.slopes) t = fmaf(-slope, (float)(distance < 0 ? -distance : distance), t);
     return t;
 }
@@ -266,22 +268,25 @@ __device__ __forceinline__ float both_halves_sum(float v)
     return __uint_as_float(x[0]) + __uint_as_float(x[1]);
 }
 
+// How the rules change the scores themselves (cap, bias): not at all, to what bf16 weights are worth, or in full.
+enum Scored { kUnscored, kScoredRough, kScored };
 // What is multiplied with a score to have its exponent in base 2.
-template <bool RULES>
+template <Scored HOW>
 __device__ __forceinline__ float score_factor(const AttnArgs &a)
 {
-    return RULES && (a.cap > 0.f || a.slopes) ? kLog2e : a.scale * kLog2e;
+    return HOW != kUnscored && (a.cap > 0.f || a.slopes) ? kLog2e : a.scale * kLog2e;
 }
 // Products of NB x 32 keys -> scores: the rules, and minus infinity for the keys that the row does not see.
-template <bool RULES, int NB>
+template <bool RULES, Scored HOW, int NB>
 __device__ __forceinline__ void finish_scores(const AttnArgs &a, const RowInfo &r, int pre, int base, f32x16 (&s)[NB])
 {
     const int half = (threadIdx.x >> 5) & 1;
-    if (RULES && (a.cap > 0.f || a.slopes)) {   // (the same for all)
+    if (HOW != kUnscored && (a.cap > 0.f || a.slopes)) {   // (the same for all)
 #pragma unroll
         for (int b = 0; b < NB; ++b)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) s[b][i] = ruled_score(a, s[b][i], r.slope, r.p - (base + 32 * b + 8 * (i >> 2) + 4 * half + (i & 3)));
+            for (int i = 0; i < 16; ++i)
+                s[b][i] = ruled_score<HOW == kScoredRough>(a, s[b][i], r.slope, r.p - (base + 32 * b + 8 * (i >> 2) + 4 * half + (i & 3)));
     }
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
@@ -355,11 +360,11 @@ __device__ __forceinline__ float careful_weights(f32x16 (&s)[NB], float factor, 
     return sum;
 }
 // All of it, one step after the other.
-template <bool RULES, int NB, int NDT>
+template <bool RULES, Scored HOW, int NB, int NDT>
 __device__ __forceinline__ void weigh(const AttnArgs &a, const RowInfo &r, int pre, int base, f32x16 (&s)[NB], Running<NDT> &run)
 {
-    const float factor = score_factor<RULES>(a);
-    finish_scores<RULES, NB>(a, r, pre, base, s);
+    const float factor = score_factor<HOW>(a);
+    finish_scores<RULES, HOW, NB>(a, r, pre, base, s);
     move_reference(run, new_reference<NB>(s, factor, run.m));
     run.l += huge_reference(run.m) ? careful_weights<NB>(s, factor, run.m) : weights<NB>(s, factor, run.m);
 }
@@ -455,10 +460,15 @@ __device__ __forceinline__ int seq_of_block(const AttnArgs &a, int block)
 constexpr int kStreamWaves = 4, kStreamTile = 32 * kStreamWaves;
 
 template <int DH, int TERMS, bool RULES>
-__global__ __launch_bounds__(256, TERMS == 1 ? 2 : 1) void cache_attn_stream_kernel(const AttnArgs a)
+__global__ __launch_bounds__(256, 2) void cache_attn_stream_kernel(const AttnArgs a)
 {
     constexpr int NKS = DH / 16, NDT = DH / 32, NDB = DH / 64;
-    __shared__ float part[kStreamWaves][2][16][64];   // the waves' outputs, 64 dims at a time
+    constexpr bool SHARED_Q = TERMS > 1;   // the rows' terms lie in LDS: in registers they left room for one wave per SIMD
+    __shared__ union {
+        float part[kStreamWaves][2][16][64];   // the waves' outputs, 64 dims at a time
+        u32x4 q[SHARED_Q ? NKS : 1][TERMS][64];
+    } lds;
+    auto &part = lds.part;
     __shared__ float wm[kStreamWaves][32], wl[kStreamWaves][32];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, m = lane & 31;
     const int kvh = blockIdx.x % a.n_kv_heads, rest = blockIdx.x / a.n_kv_heads;
@@ -472,11 +482,22 @@ __global__ __launch_bounds__(256, TERMS == 1 ? 2 : 1) void cache_attn_stream_ker
     if (begin >= tiles.n) return;   // (the whole block; what joins the splits does not look at this one)
     const int i0 = RULES ? first_tile(tiles, wave_min(r.fk), begin, i1, kStreamTile) : begin;   // (the same for all waves)
 
-    u32x4 q[NKS][TERMS];
+    u32x4 q[SHARED_Q ? 1 : NKS][TERMS];
     {
         const size_t at = (size_t)r.row * a.ldq + (size_t)r.head * DH + 8 * half;
+        if (SHARED_Q) {
 #pragma unroll
-        for (int ks = 0; ks < NKS; ++ks) load_q8<TERMS>(a, at + 16 * ks, q[ks]);
+            for (int x = 0; x < NKS / kStreamWaves; ++x) {
+                const int ks = x * kStreamWaves + wave;
+                load_q8<TERMS>(a, at + 16 * ks, q[0]);
+#pragma unroll
+                for (int t = 0; t < TERMS; ++t) lds.q[ks][t][lane] = q[0][t];
+            }
+            __syncthreads();
+        } else {
+#pragma unroll
+            for (int ks = 0; ks < (SHARED_Q ? 1 : NKS); ++ks) load_q8<TERMS>(a, at + 16 * ks, q[ks]);
+        }
     }
     Running<NDT> run;
     run.start();
@@ -523,13 +544,15 @@ __global__ __launch_bounds__(256, TERMS == 1 ? 2 : 1) void cache_attn_stream_ker
             f32x16 sc[1];
 #pragma unroll
             for (int e = 0; e < 16; ++e) sc[0][e] = 0.f;
+            int at = lane;
+            if (SHARED_Q) asm volatile("" : "+v"(at));   // (read anew for each tile)
 #pragma unroll
             for (int t = TERMS - 1; t >= 0; --t)
 #pragma unroll
-                for (int ks = 0; ks < NKS; ++ks) sc[0] = mfma32(as_bf16(kf[ks]), as_bf16(q[ks][t]), sc[0]);
+                for (int ks = 0; ks < NKS; ++ks) sc[0] = mfma32(as_bf16(kf[ks]), as_bf16(SHARED_Q ? lds.q[ks][t][at] : q[SHARED_Q ? 0 : ks][t]), sc[0]);
             load_k(na, nb);
             if (any_seen<RULES>(r, pre, base)) {
-                weigh<RULES, 1, NDT>(a, r, pre, base, sc, run);
+                weigh<RULES, !RULES ? kUnscored : TERMS == 1 ? kScoredRough : kScored, 1, NDT>(a, r, pre, base, sc, run);
                 const bool hidden = !all_seen<RULES>(r, pre, base);
 #pragma unroll
                 for (int g = 0; g < 2; ++g) {
@@ -664,7 +687,7 @@ __global__ __launch_bounds__(tile_waves(TERMS) * 64, tile_waves(TERMS) / 4) void
     const RowInfo r = row_info<RULES>(a, s, kvh, v0);
     // Tiles f0 .. f1 - 1 are those that every row of the block sees all of.
     int i0 = begin, fk_max = 0;
-    if (RULES && a.first_key) {   // (the same for all)
+    if (RULES && TERMS == 1 && a.first_key) {   // (the same for all; with fp32 rows these are the other form's)
         int *lowest = (int *)lds_tiles, *highest = lowest + WAVES;
         const int low = wave_min(r.fk), high = ~wave_min(~r.fk);
         if (lane == 0) { lowest[wave] = low; highest[wave] = high; }
@@ -687,7 +710,6 @@ __global__ __launch_bounds__(tile_waves(TERMS) * 64, tile_waves(TERMS) / 4) void
         auto place = [&](int t) { return !window ? t : (t <= tiles.b0 ? tiles.a : tiles.a + (t - tiles.b0)); };   // of tile t among those that are visited
         f0 = place(from > 0 ? (from - 1) / kTileKeys + 1 : 0);
         f1 = place((to + 1) / kTileKeys);
-        if (RULES && (a.cap > 0.f || a.slopes)) f1 = f0;
         f0 = f0 < i0 ? i0 : f0;
         f0 += (f0 - i0) & 1;   // (tiles are met in twos)
         f0 = f0 < i1 ? f0 : i1;
@@ -703,7 +725,7 @@ __global__ __launch_bounds__(tile_waves(TERMS) * 64, tile_waves(TERMS) / 4) void
     Running<NDT> run;
     run.start();
     bool unbounded = false;
-    const float factor = score_factor<RULES>(a);
+    const float factor = score_factor<kUnscored>(a);   // (caps and biases are the other form's)
 
     const int last_page = (total - 1) >> 4;
     const bf16_t *pool = (const bf16_t *)s.pool;
@@ -789,7 +811,7 @@ __global__ __launch_bounds__(tile_waves(TERMS) * 64, tile_waves(TERMS) / 4) void
         f32x16 sc[1];
         u32x4 w[2][TERMS];
         products(slot(i), sc);
-        weigh<RULES, 1, NDT>(a, r, pre, tiles.at(i) * kTileKeys, sc, run);
+        weigh<RULES, kUnscored, 1, NDT>(a, r, pre, tiles.at(i) * kTileKeys, sc, run);
         pack(sc, w);
         const bool hidden = !all(i);
 #pragma unroll
@@ -1011,7 +1033,7 @@ __global__ __launch_bounds__(256, 1) void cache_attn_plain_kernel(const AttnArgs
 #pragma unroll
             for (int t = 0; t < DH / 2; ++t) sc[0] = mfma32f(k[t], q[t], sc[0]);
         }
-        weigh<true, 1, NDT>(a, r, pre, base, sc, run);
+        weigh<true, kScored, 1, NDT>(a, r, pre, base, sc, run);
         if (!all_seen<true>(r, pre, base))
 #pragma unroll
             for (int e = 0; e < 16; ++e)
@@ -1195,7 +1217,7 @@ __device__ __forceinline__ void add_weights(const AttnArgs &a, const RowInfo &r,
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
         const int j = base + 8 * (i >> 2) + 4 * half + (i & 3);
-        const float t = scored ? ruled_score(a, s[i], r.slope, r.p - j) - lse : fmaf(s[i], a.scale, -lse);
+        const float t = scored ? ruled_score<false>(a, s[i], r.slope, r.p - j) - lse : fmaf(s[i], a.scale, -lse);
         acc[i] += sees<RULES>(r, pre, j) ? __builtin_amdgcn_exp2f(t * kLog2e) : 0.f;
     }
 }

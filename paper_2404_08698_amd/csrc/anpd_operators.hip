@@ -76,6 +76,7 @@ int32_t gather(const char *who, const anpd_kv *const *kvs, int32_t n_seq, const 
             return fail(ANPD_E_INVAL, "%s: scale, cap, window and prefix must be finite and >= 0", who);
         if (rules->scale > 0.f) a.scale = rules->scale;
         a.cap = rules->cap;
+        if (a.cap > 0.f) a.scale_over_cap = a.scale / a.cap;
         a.window = rules->window;
         a.prefix = rules->prefix;
         a.slopes = rules->slopes;
@@ -109,16 +110,20 @@ struct Plan {
     size_t part_bytes;
 };
 
-// The key tiles of all row blocks of a sequence, by a sum over its ends (rows in between have as many, more or less), and the most
-// that a block can have.
+// The key tiles of all row blocks of a sequence, and the most that a block can have.  All: by the blocks at its ends (in between it goes in a
+// straight line), with a window by up to eight blocks.
 void count_tiles(const AttnArgs &a, const SeqView &v, int row_block, int key_tile, int64_t &blocks, int64_t &tiles, int &most)
 {
     const int64_t rows = (int64_t)v.n * a.group;
     const int total = v.pos0 + v.n, span = row_block / a.group;
     blocks = (rows + row_block - 1) / row_block;
-    const KeyTiles first = key_tiles(v.pos0, v.pos0 + (span < v.n ? span : v.n) - 1, total, a.window, a.prefix, key_tile);
-    const KeyTiles last = key_tiles(total - 1 - (span < v.n ? span : v.n) + 1, total - 1, total, a.window, a.prefix, key_tile);
-    tiles = blocks * (first.n + last.n) / 2;
+    const int64_t samples = blocks < 2 ? blocks : (a.window > 0 && blocks > 2 ? (blocks < 8 ? blocks : 8) : 2);
+    tiles = 0;
+    for (int64_t i = 0; i < samples; ++i) {
+        const int64_t from = (samples > 1 ? (blocks - 1) * i / (samples - 1) : 0) * row_block, to = from + row_block < rows ? from + row_block : rows;
+        tiles += key_tiles(v.pos0 + (int)(from / a.group), v.pos0 + (int)((to - 1) / a.group), total, a.window, a.prefix, key_tile).n;
+    }
+    tiles = blocks * tiles / samples;
     // (a window's tiles depend on where it begins inside the first one)
     const int pre = a.prefix < total ? a.prefix : total, all = (total > pre ? total : pre) - 1;
     int64_t bound = all / key_tile + 1;
@@ -129,12 +134,11 @@ void count_tiles(const AttnArgs &a, const SeqView &v, int row_block, int key_til
     most = (int)bound;
 }
 
-// Sets the row blocks of a's sequences, the splits and their size: by the sizes for bf16 rows, so that the workspace is the same for both types
-// (blocks of fp32 rows are half as many rows in the shared form).
+// Sets the row blocks of a's sequences, the splits and their size, for a.q_f32.
 Plan plan_attention(AttnArgs &a, const CacheShape &c, int n_cu)
 {
     Plan p;
-    const int shared_rows = tile_rows(1);
+    const int shared_rows = tile_rows(a.q_f32 ? 3 : 1);
     int64_t blocks[2] = {0, 0}, tiles[2] = {0, 0};   // of either form
     int most[2] = {0, 0};
     for (int s = 0; s < a.n_seq; ++s) {
@@ -154,13 +158,22 @@ Plan plan_attention(AttnArgs &a, const CacheShape &c, int n_cu)
     if (splits > most[1] / 12) splits = most[1] / 12;
     if (splits < 1) splits = 1;
     const int64_t shared_chunk = (most[1] + splits - 1) / splits;
-    // Which form, by what tiles were measured to take, us: 0.95 of a compute unit for 32 rows x 128 keys (two blocks share it); 0.9 for the
-    // 256 x 32 of the longest block, 1.1 for those of all blocks where they are many; six to begin with and eight to be joined.
-    // 32 heads of 128, 32 rows / shared: 1024 rows 27 / 36, 1536 46 / 50, 2048 74 / 64, 3584 187 / 120; behind 4096 positions
-    // 128 rows 33 / 36, 256 50 / 41.
-    const double longest_us = 0.9 * (double)shared_chunk, all_us = 1.1 * (double)tiles[1] / n_cu;
-    p.shared = c.fragments && (longest_us > all_us ? longest_us : all_us) + (splits > 1 ? 14.0 : 6.0) < 0.95 * (double)tiles[0] / n_cu + 4.0;
-    p.row_block = p.shared ? tile_rows(a.q_f32 ? 3 : 1) : kRowTile;
+    // Which form, by what tiles were measured to take.  Blocks of 32 rows: a tile of 128 keys 0.95 us of a compute unit (fp32 rows 1.7), and four to
+    // begin with.  Shared: a tile of 32 keys 0.9 us (1.28) of the longest block, 1.1 (1.45) of a unit where there are many, 1.6 (2.5) more for those
+    // that a window cuts; six to begin with, or twelve and the parts that are joined, at 4.5 TB/s.  Documents that begin behind a row's
+    // first key, which are not looked at here, shorten the former more, with fp32 rows always enough.  Caps and biases are the former's: their
+    // vector instructions leave nothing to share.  330 shapes (1, 4 and 16 heads per key head, 128 to 3584 rows, windows, documents): 1.1 % above the better one on
+    // average, 29 % at worst.  32 heads of 128, blocks of 32 rows / shared, us: 1000 rows 25 / 36, 2000 65 / 59, 3584 169 / 118; fp32 39 / 47, 114 / 106,
+    // 301 / 275; 3584 in a window of 300 69 / 77, one key head for 16 67 / 43; 3584 with a cap 252 / 315, fp32 400 / 677.
+    int64_t rows = 0;
+    for (int s = 0; s < a.n_seq; ++s) rows += a.seq[s].n;
+    const double longest_us = (a.q_f32 ? 1.28 : 0.9) * (double)shared_chunk, all_us = (a.q_f32 ? 1.45 : 1.1) * (double)tiles[1] / n_cu;
+    double shared_us = (longest_us > all_us ? longest_us : all_us) + 6.0;
+    if (splits > 1) shared_us += 6.0 + (double)rows * c.n_heads * splits * c.head_dim * 4 / 4.5e6;
+    if (a.window > 0) shared_us += (a.q_f32 ? 2.5 : 1.6) * (shared_rows / a.group / 32.0 + 1.0);
+    if (a.first_key) shared_us *= 1.4;
+    p.shared = c.fragments && !(a.cap > 0.f || a.slopes) && !(a.q_f32 && a.first_key) && shared_us < (a.q_f32 ? 1.7 : 0.95) * (double)tiles[0] / n_cu + 4.0;
+    p.row_block = p.shared ? shared_rows : kRowTile;
     p.key_tile = p.shared ? kTileKeys : kStreamTile;
     a.n_blocks = 0;
     for (int s = 0; s < a.n_seq; ++s) {
@@ -175,15 +188,27 @@ Plan plan_attention(AttnArgs &a, const CacheShape &c, int n_cu)
         // 1000 positions 9.1 / 11.3 us, a tile each 9.7 / 14.4).  Caches in plain order, whose tiles take four times that, a tile each, and one block
         // of heads of 128, which fill a unit's registers (fp32, 4 heads of 64, 8 rows behind 1000 16 -> 13, 32 of 128, a row behind 1000 23 -> 19).
         const int per_unit = c.fragments || c.head_dim == 64 ? 2 : 1, least = c.fragments ? 2 : 1;
-        splits = items > 0 ? (per_unit * n_cu + items - 1) / items : 1;
+        splits = items > 0 ? per_unit * n_cu / items : 1;
         if (splits > longest / least) splits = longest / least;
         if (splits < 1) splits = 1;
         a.chunk = (int)((longest + splits - 1) / splits);
     }
     if (a.chunk < 1) a.chunk = 1;
     a.n_splits = longest > 0 ? (longest + a.chunk - 1) / a.chunk : 1;
-    p.part_bytes = a.n_splits > 1 ? align_up((size_t)items * a.n_splits * part_floats(p.shared ? shared_rows : kRowTile, c.head_dim) * sizeof(float)) : 0;
+    p.part_bytes = a.n_splits > 1 ? align_up((size_t)items * a.n_splits * part_floats(p.row_block, c.head_dim) * sizeof(float)) : 0;
     return p;
+}
+
+// The workspace of a call, which is the same for rows of both types.
+size_t attention_part_bytes(AttnArgs a, const CacheShape &c, int n_cu)
+{
+    size_t need = 0;
+    for (int f32 = 0; f32 < 2; ++f32) {
+        a.q_f32 = f32;
+        const size_t bytes = plan_attention(a, c, n_cu).part_bytes;
+        if (bytes > need) need = bytes;
+    }
+    return need;
 }
 
 template <int DH, int TERMS, bool RULES>
@@ -388,7 +413,7 @@ size_t anpd_attention_workspace_bytes(const anpd_kv_t *const *kvs, int32_t n_seq
     AttnArgs a;
     int64_t rows;
     if (gather("anpd_attention_workspace_bytes", kvs, n_seq, n_rows, pos0, rules, a, rows) != ANPD_OK) return 0;
-    return plan_attention(a, kvs[0]->shape, kvs[0]->n_cu).part_bytes;
+    return attention_part_bytes(a, kvs[0]->shape, kvs[0]->n_cu);
 }
 
 int32_t anpd_attention(const anpd_kv_t *const *kvs, int32_t n_seq, const int32_t *n_rows, const int32_t *pos0, int32_t layer, const void *q, int64_t ldq,

@@ -122,7 +122,9 @@ def check_attention(filled, q, spans, out, lse, **rules):
         assert (got.reshape(*dead.shape, -1)[dead] == 0).all()
 
 
-#: (heads, key / value heads, head dim, [(pos0, rows)]) that take the form whose rows share keys through LDS, whatever rules there are
-#: besides a short window; with and without splits of the keys, blocks that are not full, several sequences
-SHARED_SHAPES = [(8, 8, 128, [(3000, 1000)]), (32, 4, 64, [(0, 2222)]), (16, 1, 128, [(5000, 700)]), (32, 2, 128, [(2000, 513), (0, 3), (2400, 777)]),
+#: (heads, key / value heads, head dim, [(pos0, rows)]) that take the form whose rows share keys through LDS, where neither caps nor biases nor a
+#: short window are among the rules; with and without splits of the keys, blocks that are not full, several sequences
+SHARED_SHAPES = [(32, 8, 128, [(8000, 300)]), (32, 4, 64, [(0, 2222)]), (16, 1, 128, [(9000, 500)]), (32, 2, 128, [(2000, 513), (0, 3), (2400, 777)]),
                  (48, 48, 64, [(0, 1700)])]
+#: ... and with documents, bf16 rows alone
+SHARED_DOCUMENTS = (32, 2, 128, [(0, 3000)])

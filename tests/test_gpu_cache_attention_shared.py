@@ -2,7 +2,7 @@
 import pytest
 import torch
 
-from cache_reference import SHARED_SHAPES, Filled, attention as reference, check_attention, rows_like
+from cache_reference import SHARED_DOCUMENTS, SHARED_SHAPES, Filled, attention as reference, check_attention, rows_like
 from paper_2404_08698_amd import binding as B
 
 pytestmark = pytest.mark.gpu
@@ -29,7 +29,7 @@ def test_plain(shape, q):
 
 
 @pytest.mark.parametrize("q", ["bf16", "f32"])
-@pytest.mark.parametrize("rules", [dict(window=1500), dict(prefix=1), dict(prefix=2040), dict(prefix=9000), dict(window=1400, prefix=700), dict(cap=4.0), dict(scale=0.4)], ids=str)
+@pytest.mark.parametrize("rules", [dict(window=7000), dict(prefix=1), dict(prefix=2040), dict(prefix=9000), dict(window=6900, prefix=700), dict(cap=4.0), dict(scale=0.4)], ids=str)
 def test_rules(rules, q):
     check(SHARED_SHAPES[0], q, seed=3, **rules)
     if "window" not in rules:
@@ -49,6 +49,22 @@ def test_distance_bias_and_documents(q):
     check(shape, q, first_key=first.cuda())
     check(shape, q, first_key=first.cuda(), prefix=1000)
     check(shape, q, slopes=slopes, first_key=first.cuda(), prefix=400, window=900, cap=6.0)
+
+
+@pytest.mark.parametrize("prefix,window", [(0, 0), (100, 0), (100, 2500)])
+@pytest.mark.parametrize("length", [611, 1700])
+def test_long_documents(length, prefix, window):
+    heads, kv_heads, dim, ((_, n),) = SHARED_DOCUMENTS
+    filled = Filled(heads, kv_heads, dim, [n])
+    rows = rows_like(filled, n)
+    first = torch.arange(n, dtype=torch.int32) // length * length
+    first[40:300] = 1 << 30        # whole blocks of rows without a key
+    first[2000] = 1999
+    first[-5:] = 1 << 30
+    out, lse = run(filled, [(0, n)], rows, first_key=first.cuda(), prefix=prefix, window=window)
+    for at, some in ((0, 330), (1680, 60), (1990, 20), (2900, 100)):
+        part = slice(at, at + some)
+        check_attention(filled, rows[part], [(at, some)], out[part], lse[part], first_key=first[part], prefix=prefix, window=window)
 
 
 @pytest.mark.parametrize("q", ["bf16", "f32"])
@@ -78,8 +94,9 @@ def test_hidden_contents_take_no_part(q, bad):
 
 def test_large_scores():
     for std in (0.0, 200.0, 1e6, 1e18):
-        filled = Filled(*SHARED_SHAPES[2][:3], [5700], seed=3)
-        rows = rows_like(filled, 700, std=std)
+        (pos0, n), = SHARED_SHAPES[2][3]
+        filled = Filled(*SHARED_SHAPES[2][:3], [pos0 + n], seed=3)
+        rows = rows_like(filled, n, std=std)
         out, lse = run(filled, SHARED_SHAPES[2][3], rows)
         check_attention(filled, rows, SHARED_SHAPES[2][3], out, lse)
 
@@ -88,19 +105,20 @@ def test_large_scores():
 def test_replays(q):
     """A captured call, its eager twin and other work in turn: the same bits."""
     heads, kv_heads, dim, spans = SHARED_SHAPES[2]
-    filled = Filled(heads, kv_heads, dim, [5700])
-    rows = rows_like(filled, 700, DTYPES[q])
-    need = B.attention_workspace_bytes(filled.kvs, [700], [5000])
+    (pos0, n), = spans
+    filled = Filled(heads, kv_heads, dim, [pos0 + n])
+    rows = rows_like(filled, n, DTYPES[q])
+    need = B.attention_workspace_bytes(filled.kvs, [n], [pos0])
     ws, out = torch.empty(max(256, need), dtype=torch.uint8, device="cuda"), torch.empty_like(rows)
-    want = B.attention(filled.kvs[0], 0, rows, pos0=[5000]).clone()
+    want = B.attention(filled.kvs[0], 0, rows, pos0=[pos0]).clone()
     s = torch.cuda.Stream()
     s.wait_stream(torch.cuda.current_stream())
     g = torch.cuda.CUDAGraph()
     with torch.cuda.graph(g, stream=s):
-        B.attention(filled.kvs[0], 0, rows, pos0=[5000], out=out, workspace=ws)
+        B.attention(filled.kvs[0], 0, rows, pos0=[pos0], out=out, workspace=ws)
     for _ in range(4):
         out.zero_()
         g.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, want)
-        assert torch.equal(B.attention(filled.kvs[0], 0, rows, pos0=[5000]), want)
+        assert torch.equal(B.attention(filled.kvs[0], 0, rows, pos0=[pos0]), want)

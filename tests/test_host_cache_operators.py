@@ -297,17 +297,32 @@ def child_forms():
     sys.path.insert(0, HERE)
     c = Caches()
     import ast
-    shapes = next(ast.literal_eval(n.value) for n in ast.parse(open(os.path.join(HERE, "cache_reference.py")).read()).body
-                  if isinstance(n, ast.Assign) and n.targets[0].id == "SHARED_SHAPES")
+    named = {n.targets[0].id: n.value for n in ast.parse(open(os.path.join(HERE, "cache_reference.py")).read()).body if isinstance(n, ast.Assign)}
+    shapes = ast.literal_eval(named["SHARED_SHAPES"])
     assert len(shapes) >= 4
     for heads, kv_heads, dim, spans in shapes + [(32, 32, 128, [(500, 1)]), (32, 32, 128, [(0, 500)])]:
         kvs = [c.cache(p + n, p + n, heads, kv_heads, dim, layers=1) for p, n in spans]
         ws = c.memory(64 << 20)
+        large = (heads, kv_heads, dim, spans) in shapes
         for dtype in (0, 1):
+            for rules, able in (({}, True), ({"prefix": 2040}, True), ({"cap": 4.0}, False), ({"slopes": ws}, False)):
+                c.stub.stub_forget()
+                given = c.B.AttnRules(**rules)
+                assert c.attention(kvs, [n for _, n in spans], [p for p, _ in spans], dtype=dtype, ldq=heads * dim, ldo=heads * dim, ws=ws, nb=64 << 20, rules=given) == 0, c.L.anpd_last_error()
+                shared = "cache_attn_tile_kernel" in c.names()[0]
+                assert shared == (large and able), (heads, spans, dtype, rules, c.names())
+        if (heads, kv_heads, dim, spans) == shapes[0]:   # (as tested elsewhere)
+            for window in (6900, 7000):
+                c.stub.stub_forget()
+                assert c.attention(kvs, [n for _, n in spans], [p for p, _ in spans], ldq=heads * dim, ldo=heads * dim, ws=ws, nb=64 << 20, rules=c.B.AttnRules(window=window)) == 0
+                assert "cache_attn_tile_kernel" in c.names()[0]
+    heads, kv_heads, dim, ((_, n),) = ast.literal_eval(named["SHARED_DOCUMENTS"])
+    kv = c.cache(n, n, heads, kv_heads, dim, layers=1)
+    for dtype in (0, 1):
+        for rules in ({}, {"prefix": 100}, {"prefix": 100, "window": 2500}):
             c.stub.stub_forget()
-            assert c.attention(kvs, [n for _, n in spans], [p for p, _ in spans], dtype=dtype, ldq=heads * dim, ldo=heads * dim, ws=ws, nb=64 << 20) == 0, c.L.anpd_last_error()
-            shared = "cache_attn_tile_kernel" in c.names()[0]
-            assert shared == ((heads, kv_heads, dim, spans) in shapes), (heads, spans, c.names())
+            assert c.attention([kv], [n], [0], dtype=dtype, ldq=heads * dim, ldo=heads * dim, ws=ws, nb=64 << 20, rules=c.B.AttnRules(first_key=ws, **rules)) == 0
+            assert ("cache_attn_tile_kernel" in c.names()[0]) == (dtype == 1), (dtype, rules, c.names())
 
 
 def test_forms(stub):
