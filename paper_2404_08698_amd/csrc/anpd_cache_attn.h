@@ -1269,23 +1269,31 @@ __global__ __launch_bounds__(256, 2) void cache_mass_kernel(const AttnArgs a, co
 #pragma unroll
         for (int ks = 0; ks < NKS; ++ks) kf[x][ks] = p[(ks >> 1) * 64 + (ks & 1) * 32];
     }
-    // what the next tile is made of: its rows' pieces, and every lane's row
-    u32x4 piece[UNITS][TERMS];
+    // what the next tile is made of, as it comes from memory (nothing is done to it before the tile at hand is through): its rows' pieces,
+    // and every lane's row
+    u32x4 piece[UNITS][1];
+    float wide[UNITS][8];
     RowInfo r_next;
     float lse_next = 0.f;
     auto request = [&](int t) __attribute__((always_inline)) {
         r_next = row_info<RULES>(a, s, kvh, t * kRowTile);
         const size_t at = (size_t)r_next.row * a.ldq + (size_t)r_next.head * DH + 8 * half;
 #pragma unroll
-        for (int u = 0; u < UNITS; ++u) load_q8<TERMS>(a, at + 16 * (wave + 4 * u), piece[u]);
-        const float lse = a.lse[(size_t)r_next.row * a.n_heads + r_next.head];
-        lse_next = r_next.live && lse != -INFINITY ? lse : INFINITY;   // (no row, or one without keys: weights of 0)
+        for (int u = 0; u < UNITS; ++u) {
+            if constexpr (TERMS == 1) load_q8<1>(a, at + 16 * (wave + 4 * u), piece[u]);
+            else load_q8(a, at + 16 * (wave + 4 * u), wide[u]);
+        }
+        lse_next = a.lse[(size_t)r_next.row * a.n_heads + r_next.head];
     };
     auto put = [&](int buf) __attribute__((always_inline)) {
 #pragma unroll
-        for (int u = 0; u < UNITS; ++u)
+        for (int u = 0; u < UNITS; ++u) {
+            u32x4 t[TERMS];
+            if constexpr (TERMS == 1) t[0] = piece[u][0];
+            else split_terms<TERMS>(wide[u], t);
 #pragma unroll
-            for (int k = 0; k < TERMS; ++k) lds.q[buf][k][wave + 4 * u][lane] = piece[u][k];
+            for (int k = 0; k < TERMS; ++k) lds.q[buf][k][wave + 4 * u][lane] = t[k];
+        }
     };
     f32x16 acc[SETS] = {};
     request(t0);
@@ -1293,7 +1301,7 @@ __global__ __launch_bounds__(256, 2) void cache_mass_kernel(const AttnArgs a, co
     for (int t = t0; t < t1; ++t) {
         const int buf = (t - t0) & 1;
         const RowInfo r = r_next;
-        const float lse = lse_next;
+        const float lse = r.live && lse_next != -INFINITY ? lse_next : INFINITY;   // (no row, or one without keys: weights of 0)
         __syncthreads();
         if (t + 1 < t1) request(t + 1);
         bool seen = false;
