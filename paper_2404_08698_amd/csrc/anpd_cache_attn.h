@@ -14,8 +14,8 @@
 // fragment order has both operands ready: K in 16-byte pieces of 8 dims of a key, V in 8-byte pieces of 4 keys of a dim.
 //
 // Precision.  Scores, maxima, sums and outputs are held in 32 bits.  bf16 rows meet bf16 keys exactly; their weights are
-// rounded to bf16 for the second product (2^-9 of a weight, as much as the output's own rounding).  fp32 rows are three bf16
-// terms, 24 bits, and so are their weights: two terms keep 2^-18 of every weight, which was ten times the error of fp32 sums.
+// rounded to bf16 for the second product (2^-8 of a weight at most, as the output's own rounding).  fp32 rows are three bf16
+// terms, 24 bits, and so are their weights: two terms lose up to 2^-16 of every weight, which was ten times the error of fp32 sums.
 #pragma once
 #include <type_traits>
 
@@ -455,15 +455,20 @@ __device__ __forceinline__ int seq_of_block(const AttnArgs &a, int block)
 //
 // Block = (32 virtual rows, kv head, split of the keys), four waves; wave w takes keys 32 w .. of every 128.  Nothing is shared
 // while the keys go by: a wave's loads are the operands, the next keys are requested when this tile's scores are done, its values
-// when its output is, and the waves meet at the end.  This is the form of single tokens, of windows and of prompts whose
-// blocks of 128 rows would leave compute units without one.   grid: n_blocks * n_splits * n_kv_heads
+// when its output is, and the waves meet at the end.  This is the form of single tokens, of windows, of prompts whose larger blocks
+// would leave compute units without one, and of scores with caps and biases.
+// A token or a window is bound by the cache's bytes: 32 tokens of 32 sequences, 271 MB in 54 us (5.0 TB/s), one behind 65535 positions of 8 key heads,
+// 268 MB in 49 us (5.5); 17 rows behind 2048, 34 MB in 14 us, are start, three tiles one after the other and end.  A prompt is bound by L2: every
+// block reads its keys for 32 rows (512 rows of 32 heads 11 us, 0.19 PFLOP/s).  fp32 rows: three times the matrix instructions; their terms lie in LDS
+// once for the four waves, which leaves a wave 192 registers, not 350, and a SIMD two of them: 512 rows 22 -> 15 us, packed documents 49 -> 26.
+// grid: n_blocks * n_splits * n_kv_heads
 constexpr int kStreamWaves = 4, kStreamTile = 32 * kStreamWaves;
 
 template <int DH, int TERMS, bool RULES>
 __global__ __launch_bounds__(256, 2) void cache_attn_stream_kernel(const AttnArgs a)
 {
     constexpr int NKS = DH / 16, NDT = DH / 32, NDB = DH / 64;
-    constexpr bool SHARED_Q = TERMS > 1;   // the rows' terms lie in LDS: in registers they left room for one wave per SIMD
+    constexpr bool SHARED_Q = TERMS > 1;   // (the rows' terms in LDS)
     __shared__ union {
         float part[kStreamWaves][2][16][64];   // the waves' outputs, 64 dims at a time
         u32x4 q[SHARED_Q ? NKS : 1][TERMS][64];
@@ -635,15 +640,16 @@ __global__ __launch_bounds__(256, 2) void cache_attn_stream_kernel(const AttnArg
 
 // ------------------------------------------------------------------ many rows: keys and values shared through LDS
 //
-// Block = (128 virtual rows, kv head, split of the keys), four waves of 32 rows each against the same 32 keys, which go from the
-// cache through registers into one of two LDS buffers while the other one is multiplied: a key is read from L2 once for 128 rows
-// where the form above reads it for 32.
-// 64 keys take a wave about 1000 cycles of matrix instructions, as many of vector instructions (a score: a fused product, an exponential,
-// a sum, its share of a maximum and of a rounding) and LDS as many for the four waves; two waves share a SIMD, which is what the registers
+// Block = (256 bf16 or 128 fp32 virtual rows, kv head, split of the keys), eight or four waves of 32 rows each against the same 32 keys, which go
+// from the cache straight into one of eight slots of LDS, six tiles ahead: a key is read from L2 once for the block where the form above
+// reads it for 32 rows.  The waves meet at every other tile, where the loads in flight are counted, not waited for.
+// 32 keys take a wave about 500 cycles of matrix instructions, as many of vector instructions (a score: a fused product, an exponential,
+// a sum, its share of a maximum and of a rounding) and LDS as many for four waves; two waves share a SIMD, which is what the registers
 // hold.  One step after the other, the three took turns (each 37 % busy, 143 us for 3584 rows of 32 heads).  So the keys of tile i + 1
 // are multiplied while the weights of tile i are formed, and the maximum of tile i + 1 is found while the weights of
 // tile i meet its values: both halves of the loop have matrix and vector instructions that do not wait for each other, dealt out in
-// turn.  Keys are a tile ahead of values for that.
+// turn.  3584 rows of 32 heads now take 117 us, 0.90 PFLOP/s of 105 GFLOP (the library's largest product 1.24); 64 rows per wave, which halves
+// what LDS is read for, needed more registers than there are (267 us).
 // grid: n_blocks * n_splits * n_kv_heads, blocks with the most keys first
 constexpr int kTileKeys = 32;
 constexpr int kTileSlots = 8;   // tiles that LDS holds
@@ -1173,8 +1179,8 @@ __global__ __launch_bounds__(256) void cache_attn_join_kernel(const AttnArgs a, 
 // Block = (128 SETS keys, kv head, part of the rows), four waves of SETS x 32 keys, whose operands a wave holds in registers while the
 // rows go by in tiles of 32 through LDS (fp32 rows are split into their terms there, once for the four waves).  A lane adds the weights
 // of its row's 16 keys per set to as many sums over all tiles; the lanes meet at the end.  Two sets use a row operand twice for
-// one read of it: with one, LDS was as busy as the matrix cores (1800 fp32 rows of 40 heads: 127 us).  One block owns a key's sum, so there are no atomics and
-// the order is always the same; where keys are too few for all compute units, the rows are dealt to several blocks whose sums are
+// one read of it: with one, LDS was as busy as the matrix cores (1800 fp32 rows of 40 heads 127 us, with two 75: 50 GFLOP of terms at
+// 0.66 PFLOP/s).  One block owns a key's sum, so there are no atomics and the order is always the same; where keys are too few for all compute units, the rows are dealt to several blocks whose sums are
 // added in order by a second kernel.  exp(t - lse) is formed from the difference, not from two numbers scaled to base 2 first,
 // whose roundings would stay in it.
 // a.block0 / n_blocks / n_splits / chunk: blocks of keys; parts of the rows, row tiles in each.

@@ -41,7 +41,8 @@ struct SelectArgs {
 // HELD: positions per lane, whose ranks stay in registers: the search goes bit by bit, a comparison and a count of the lanes per 64 positions,
 // and ends as soon as a rank separates as many as are wanted.  HELD = 0 (beyond 65536 positions): byte by byte, each time with a
 // histogram of the candidates' next byte in LDS (whole numbers: the order of the counts does not matter), for which all is
-// read again.  8 heads of 65536 positions took 132 us so, 60 of them in instructions around the histogram's.
+// read again.  8 heads of 65536 positions: 132 us with the histogram, 64 with registers, of them 9 to load, 30 for some 22 steps of the search
+// (64 comparisons a wave, and a meeting of the waves), 18 to write; 64 heads of 3584 14 us, a step 0.4 of them, the meeting.
 // grid: n_layers * n_kv_heads
 template <int HELD>
 __global__ __launch_bounds__(kSelectThreads) void cache_select_kernel(const SelectArgs a)
@@ -259,7 +260,9 @@ __device__ __forceinline__ void turn_of(double turn, int moved, float &c, float 
 
 // The cache in matrix-core order.  Block = (layer, head; keys or values; every gridDim.z-th group of eight pages): all that goes into the
 // group is read before any of it is written, and a position never moves up, so a cache may be moved into itself with one block
-// per layer, head and kind (gridDim.z = 1).   grid: (n_layers * n_kv_heads, 2, groups)
+// per layer, head and kind (gridDim.z = 1).  A line of the cache has eight keys' pieces or 16 dims of four values, so that every line with
+// something that stays is read: of 65536 positions a quarter at random, 320 MB in 89 us (3.6 TB/s) for 134 MB that are kept; of 3584 two layers of 32
+// heads, 150 MB in 40 us.   grid: (n_layers * n_kv_heads, 2, groups)
 template <int DH>
 __global__ __launch_bounds__(kMoveThreads) void cache_move_kernel(const MoveArgs a)
 {
