@@ -378,7 +378,7 @@ int32_t anpd_cache_create(const anpd_cache_cfg *cfg, void *pool, size_t pool_byt
  * A row at position p sees key j if j >= first_key[row] and (j < prefix or (j <= p and (window == 0 or j > p - window))). */
 typedef struct {
     float scale;                /* 0 = 1 / sqrt(head_dim) */
-    float cap;                  /* 0 = none */
+    float cap;                  /* 0 = none; scale / cap must be a normal fp32 number */
     int32_t window;             /* 0 = none */
     int32_t prefix;             /* keys below it are seen from every position */
     const float *slopes;        /* DEVICE, n_heads floats, or NULL */
@@ -438,7 +438,8 @@ int32_t anpd_kv_observe(anpd_kv_t *kv, float *mass, int64_t ld_mass, int32_t row
  *   (half-split pairing, as the model's own keys), so that it is the key of a token at position i, which is what
  *   the steps that follow take it for.
  *   out_kept: DEVICE, [n_layers][n_kv_heads][keep] ints, the positions that stayed, ascending.
- *   out_mass (nullable): DEVICE, [n_layers][n_kv_heads][ld_out] floats, ld_out >= keep: their mass.  Must not overlap mass.
+ *   out_mass (nullable): DEVICE, [n_layers][n_kv_heads][ld_out] floats, ld_out >= keep: their mass.  Neither output may overlap mass or
+ *   the other.
  * 0 <= first + last <= keep <= length.  Blocks until it is done.
  * Errors: ANPD_E_INVAL, ANPD_E_CAPACITY (keep against length or dst), ANPD_E_HIP (contents and length of dst undefined). */
 int32_t anpd_kv_evict(const anpd_kv_t *src, anpd_kv_t *dst, const float *mass, int64_t ld_mass, int32_t keep, int32_t first,

@@ -615,6 +615,16 @@ def _stream_of(device, stream) -> int:
     return torch._C._cuda_getCurrentRawStream(device.index)
 
 
+def _empty(shape, dtype, device, stream):
+    """An output or workspace of a call on `stream` (None: the current one), from that stream's memory: what its last owner
+    still does with it is done before."""
+    import torch
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 def _with_workspace(fn, bytes_of, seqs, ref, head, tail, workspace, device, stream) -> None:
     """fn(*seqs, *head, workspace, its bytes, stream): most calls need no workspace, so how much is only asked for
     where none was given and the call says so."""
@@ -627,9 +637,7 @@ def _with_workspace(fn, bytes_of, seqs, ref, head, tail, workspace, device, stre
         nbytes = bytes_of(*seqs, ref)
         if nbytes:
             import torch
-            ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
-            if stream is not None:
-                ws.record_stream(stream)
+            ws = _empty(nbytes, torch.uint8, device, stream)
             rc = fn(*seqs, *head, *tail, ws.data_ptr(), nbytes, st)
         else:
             rc = fn(*seqs, *head, *tail, None, 0, st)   # (for its message)
@@ -651,14 +659,14 @@ def attention(kvs, layer: int, q, n_rows: Optional[Sequence[int]] = None, pos0: 
     shape, n, handles, counts, at = _sequences(kvs, q, n_rows, pos0, rules)
     rows = q.shape[0]
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        out = _empty(q.shape, q.dtype, q.device, stream)
     elif not (out.device == q.device and out.dtype == q.dtype and out.shape == q.shape and out.stride(1) == 1):
         raise ValueError("out must be like the rows")
     if lse is not None:
         if not (lse.device == q.device and lse.dtype == torch.float32 and lse.is_contiguous() and tuple(lse.shape) == (rows, shape.n_heads)):
             raise ValueError("lse: contiguous float32 [rows][n_heads]")
     elif want_lse:
-        lse = torch.empty((rows, shape.n_heads), dtype=torch.float32, device=q.device)
+        lse = _empty((rows, shape.n_heads), torch.float32, q.device, stream)
     L, ref = lib(), None if rules is None else rules.ref
     _with_workspace(L.anpd_attention, L.anpd_attention_workspace_bytes, (handles, n, counts, at), ref,
                     (layer, q.data_ptr(), _pitch(q), F32 if q.dtype == torch.float32 else BF16, ref),
@@ -702,8 +710,8 @@ def evict(src: KVCache, mass, keep: int, first: int = 0, last: int = 0, into: Op
     if mass.shape[:2] != (layers, kv_heads) or mass.shape[2] < src.length or (layers > 1 and mass.stride(0) != kv_heads * mass.stride(1)):
         raise ValueError("mass: one row of at least the cache's length per layer and key / value head, equally far apart")
     ld = mass.stride(1) if layers * kv_heads > 1 else mass.shape[2]
-    kept = torch.empty((layers, kv_heads, max(0, keep)), dtype=torch.int32, device=mass.device)
-    out = torch.empty((layers, kv_heads, max(0, keep)), dtype=torch.float32, device=mass.device)
+    kept = _empty((layers, kv_heads, max(0, keep)), torch.int32, mass.device, stream)
+    out = _empty((layers, kv_heads, max(0, keep)), torch.float32, mass.device, stream)
     dst = src if into is None else into
     _check(lib().anpd_kv_evict(src._h, dst._h, mass.data_ptr(), ld, keep, first, last, rope_base, kept.data_ptr(), out.data_ptr(), max(0, keep),
                                _stream_of(mass.device, stream)))

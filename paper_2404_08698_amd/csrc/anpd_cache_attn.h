@@ -142,8 +142,9 @@ __device__ __forceinline__ int first_tile(const KeyTiles &k, int fk, int i0, int
     return i < i0 ? i0 : (i < i1 ? i : i1);
 }
 
-// cap tanh(t / cap) of a product t / scale: x = t / cap.  1 - 2 / (1 + e^2x) is off by 2^-22 of the cap at most, whatever x is, which is
-// nothing beside weights in bf16 (ROUGH); otherwise small x take a sum of powers, to 2^-23 of the value.
+// For cap tanh(t / cap): 1 - 2 / (1 + e^2x) is off by 2^-22 at most, whatever x is, which is nothing beside weights in bf16 unless the cap
+// is large (ROUGH: caps up to kRoughCap, 2^-14 of a score); otherwise small x take a sum of powers, to 2^-23 of the value.
+constexpr float kRoughCap = 256.f;
 template <bool ROUGH>
 __device__ __forceinline__ float tanh_f32(float x)
 {
@@ -268,7 +269,7 @@ __device__ __forceinline__ float both_halves_sum(float v)
     return __uint_as_float(x[0]) + __uint_as_float(x[1]);
 }
 
-// How the rules change the scores themselves (cap, bias): not at all, to what bf16 weights are worth, or in full.
+// How the rules change the scores themselves (cap, bias): not at all, to what bf16 weights are worth where that will do, or in full.
 enum Scored { kUnscored, kScoredRough, kScored };
 // What is multiplied with a score to have its exponent in base 2.
 template <Scored HOW>
@@ -282,11 +283,17 @@ __device__ __forceinline__ void finish_scores(const AttnArgs &a, const RowInfo &
 {
     const int half = (threadIdx.x >> 5) & 1;
     if (HOW != kUnscored && (a.cap > 0.f || a.slopes)) {   // (the same for all)
+        if (HOW == kScoredRough && a.cap <= kRoughCap) {
 #pragma unroll
-        for (int b = 0; b < NB; ++b)
+            for (int b = 0; b < NB; ++b)
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
-                s[b][i] = ruled_score<HOW == kScoredRough>(a, s[b][i], r.slope, r.p - (base + 32 * b + 8 * (i >> 2) + 4 * half + (i & 3)));
+                for (int i = 0; i < 16; ++i) s[b][i] = ruled_score<true>(a, s[b][i], r.slope, r.p - (base + 32 * b + 8 * (i >> 2) + 4 * half + (i & 3)));
+        } else {
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[b][i] = ruled_score<false>(a, s[b][i], r.slope, r.p - (base + 32 * b + 8 * (i >> 2) + 4 * half + (i & 3)));
+        }
     }
 #pragma unroll
     for (int b = 0; b < NB; ++b) {

@@ -77,6 +77,8 @@ int32_t gather(const char *who, const anpd_kv *const *kvs, int32_t n_seq, const 
         if (rules->scale > 0.f) a.scale = rules->scale;
         a.cap = rules->cap;
         if (a.cap > 0.f) a.scale_over_cap = a.scale / a.cap;
+        if (a.cap > 0.f && !std::isnormal(a.scale_over_cap)) return fail(ANPD_E_INVAL, "%s: scale / cap is beyond the range of fp32", who);
+        if ((((uintptr_t)rules->slopes | (uintptr_t)rules->first_key) & 3) != 0) return fail(ANPD_E_INVAL, "%s: slopes or first_key are not aligned to their type", who);
         a.window = rules->window;
         a.prefix = rules->prefix;
         a.slopes = rules->slopes;
@@ -429,6 +431,7 @@ int32_t anpd_attention(const anpd_kv_t *const *kvs, int32_t n_seq, const int32_t
     if (ldo < (int64_t)c.n_heads * c.head_dim) return fail(ANPD_E_INVAL, "%s: ldo %lld is less than a row", who, (long long)ldo);
     if (rows == 0) return ANPD_OK;
     if (!q || !out) return fail(ANPD_E_INVAL, "%s: NULL rows", who);
+    if (((uintptr_t)lse & 3) != 0) return fail(ANPD_E_INVAL, "%s: lse is not aligned to its type", who);
     if (((uintptr_t)out & (a.q_f32 ? 3 : 1)) != 0) return fail(ANPD_E_INVAL, "%s: out is not aligned to its type", who);
     a.out = out;
     a.ldo = ldo;
@@ -463,13 +466,14 @@ int32_t anpd_key_mass(const anpd_kv_t *const *kvs, int32_t n_seq, const int32_t 
     if ((rc = rows_in(who, c, layer, q, ldq, dtype, a)) != ANPD_OK) return rc;
     if (rows == 0) return ANPD_OK;
     if (!q || !lse || !mass) return fail(ANPD_E_INVAL, "%s: NULL argument", who);
+    if (((uintptr_t)lse & 3) != 0) return fail(ANPD_E_INVAL, "%s: lse is not aligned to its type", who);
     MassOut to;
     std::memset(&to, 0, sizeof(to));
     to.ld = ld_mass;
     for (int s = 0; s < n_seq; ++s) {
         if (a.seq[s].n == 0) continue;
         const int total = a.seq[s].pos0 + a.seq[s].n;
-        if (!mass[s]) return fail(ANPD_E_INVAL, "%s: sequence %d: NULL mass", who, s);
+        if (!mass[s] || ((uintptr_t)mass[s] & 3) != 0) return fail(ANPD_E_INVAL, "%s: sequence %d: NULL mass, or not aligned to its type", who, s);
         if (ld_mass < total) return fail(ANPD_E_CAPACITY, "%s: sequence %d has %d keys, ld_mass is %lld", who, s, total, (long long)ld_mass);
         for (int t = 0; t < s; ++t) {
             if (a.seq[t].n == 0) continue;
@@ -534,8 +538,12 @@ int32_t anpd_kv_evict(const anpd_kv_t *src, anpd_kv_t *dst, const float *mass, i
     if (keep > 0) {
         if (!mass || !out_kept) return fail(ANPD_E_INVAL, "%s: NULL argument", who);
         if (ld_mass < len || (out_mass && ld_out < keep)) return fail(ANPD_E_CAPACITY, "%s: rows of mass are shorter than their positions", who);
-        if (out_mass && overlap(mass, ((size_t)(heads - 1) * ld_mass + len) * sizeof(float), out_mass, ((size_t)(heads - 1) * ld_out + keep) * sizeof(float)))
-            return fail(ANPD_E_INVAL, "%s: out_mass overlaps mass", who);
+        if ((((uintptr_t)mass | (uintptr_t)out_kept | (uintptr_t)out_mass) & 3) != 0) return fail(ANPD_E_INVAL, "%s: an argument is not aligned to its type", who);
+        const size_t mass_bytes = ((size_t)(heads - 1) * ld_mass + len) * sizeof(float), kept_bytes = (size_t)heads * keep * sizeof(int32_t);
+        const size_t out_bytes = out_mass ? ((size_t)(heads - 1) * ld_out + keep) * sizeof(float) : 0;
+        if (out_mass && overlap(mass, mass_bytes, out_mass, out_bytes)) return fail(ANPD_E_INVAL, "%s: out_mass overlaps mass", who);
+        if (overlap(mass, mass_bytes, out_kept, kept_bytes) || (out_mass && overlap(out_mass, out_bytes, out_kept, kept_bytes)))
+            return fail(ANPD_E_INVAL, "%s: out_kept overlaps mass or out_mass", who);
     }
     OnDevice on;
     int32_t rc = on.enter(who, src->device);

@@ -50,8 +50,18 @@ def test_several_sequences(cache, q):
     check(8, 1, 64, [(100 * i, 1) for i in range(64)], cache, q)
 
 
-RULES = [dict(cap=5.0), dict(window=1), dict(window=40), dict(window=200), dict(prefix=1), dict(prefix=130), dict(prefix=5000), dict(scale=0.3),
+RULES = [dict(cap=5.0), dict(cap=256.0), dict(cap=300.0), dict(window=1), dict(window=40), dict(window=200), dict(prefix=1), dict(prefix=130), dict(prefix=5000), dict(scale=0.3),
          dict(cap=30.0, window=33, prefix=50), dict(window=64, prefix=64)]
+
+
+@pytest.mark.parametrize("cap", [1e6, 1e18, 1e30])
+@pytest.mark.parametrize("cache,q", TYPES)
+def test_caps_far_above_the_scores_change_nothing(cache, q, cap):
+    spans = [(180, 20)]
+    filled = Filled(4, 2, 64, [200], cache)
+    rows = rows_like(filled, 20, DTYPES[q])
+    out, lse = run(filled, spans, rows, cap=cap)
+    check_attention(filled, rows, spans, out, lse)
 
 
 @pytest.mark.parametrize("cache,q", TYPES)

@@ -119,6 +119,11 @@ def child_refusals():
     inf, nan = float("inf"), float("nan")
     for scale, cap, window, prefix in ((-1.0, 0, 0, 0), (inf, 0, 0, 0), (nan, 0, 0, 0), (0, -1.0, 0, 0), (0, inf, 0, 0), (0, nan, 0, 0), (0, 0, -1, 0), (0, 0, 0, -1)):
         refused(E.E_INVAL, A([kv], [1], pos0=[5], rules=B.AttnRules(scale, cap, window, prefix)), "finite")
+    for cap, scale in ((1e-45, 0), (3e38, 0), (1e30, 1e-20), (1e-30, 1e20)):
+        refused(E.E_INVAL, A([kv], [1], pos0=[5], rules=B.AttnRules(scale, cap)), "range")
+    for rules in (B.AttnRules(slopes=m + 2), B.AttnRules(first_key=m + 1)):
+        refused(E.E_INVAL, A([kv], [1], pos0=[5], rules=rules), "aligned")
+    refused(E.E_INVAL, A([kv], [1], pos0=[5], lse=m + 2), "aligned")
     for args in (([kv], None), (None, [1])):
         kvs = None if args[0] is None else (C.c_void_p * 1)(*args[0])
         rows = None if args[1] is None else (C.c_int32 * 1)(*args[1])
@@ -138,6 +143,8 @@ def child_refusals():
     refused(E.E_INVAL, M([kv, other], [1, 1], [a, a + 4 * 5], pos0=[5, 5], ld=6), "share")
     refused(E.E_INVAL, M([kv], [1], [a], pos0=[5], layer=7), "layer")
     refused(E.E_INVAL, M([kv], [50], [a], pos0=[70]), "no page")
+    refused(E.E_INVAL, M([kv], [1], [a + 2], pos0=[5]), "aligned")
+    refused(E.E_INVAL, M([kv], [1], [a], pos0=[5], lse=m + 1), "aligned")
     refused(0, M([kv], [0], [None]))
 
     V = c.evict
@@ -162,6 +169,10 @@ def child_refusals():
     refused(E.E_CAPACITY, V(kv, other, 5, out=a, ld_out=4))
     refused(E.E_INVAL, V(kv, other, 5, mass=a, out=a), "overlaps")
     refused(E.E_INVAL, V(kv, other, 5, mass=a, out=a + 4 * (512 + 99)), "overlaps")
+    refused(E.E_INVAL, V(kv, other, 5, mass=a, kept=a + 400), "out_kept overlaps")
+    refused(E.E_INVAL, V(kv, other, 5, mass=a, kept=a + 16000, out=a + 16004), "out_kept overlaps")
+    for change in (dict(mass=a + 2), dict(kept=a + 16001), dict(out=a + 16002)):
+        refused(E.E_INVAL, V(kv, other, 5, **{**dict(mass=a, kept=a + 20000), **change}), "aligned")
     assert [c.L.anpd_kv_length(x) for x in (kv, other, small)] == [100, 40, 0]
 
     good = dict(n_layers=1, n_heads=4, head_dim=64, n_kv_heads=2, dtype=1, page_tokens=16)
