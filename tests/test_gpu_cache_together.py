@@ -7,7 +7,7 @@ import numpy as np
 import pytest
 import torch
 
-from cache_reference import U, Filled, attention, check_attention, rows_like
+from cache_reference import SHARED_SHAPES, U, Filled, attention, check_attention, rows_like
 from oracle import decoder as od
 from paper_2404_08698_amd import binding as B
 from paper_2404_08698_amd import synth
@@ -99,6 +99,40 @@ def test_captured_together():
         torch.cuda.synchronize()
         for a, b in zip(want, (out, lse, mass)):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("q_dtype", [torch.bfloat16, torch.float32])
+def test_pages_far_into_a_large_pool(q_dtype):
+    """Where a page's offset passes 32 bits, in elements: attention of many and of few rows, mass and eviction."""
+    (heads, kv_heads, dim, ((pos0, n),)), layers, capacity = SHARED_SHAPES[0], 40, 62000
+    total = pos0 + n
+    kv = B.LayerCache(layers, heads, dim, capacity, n_kv_heads=kv_heads)
+    kv.set_page_order(list(range(kv.num_pages))[::-1])      # the first positions on the last pages
+    assert (kv.num_pages - total // 16 - 1) * layers * 2 * kv_heads * 16 * dim > 1 << 32
+    gen = torch.Generator().manual_seed(3)
+    f = Filled(heads, kv_heads, dim, (), layer=layers - 1)
+    k, v = (torch.randn(total, kv_heads * dim, generator=gen).bfloat16().float() for _ in range(2))
+    f.k, f.v, f.kvs = [k], [v], [kv]
+    kv.write(layers - 1, 0, k.cuda(), v.cuda())
+    kv.truncate(total)
+    q = rows_like(f, n, q_dtype)
+    out, lse = B.attention(kv, layers - 1, q, pos0=[pos0], want_lse=True)
+    last = slice(n - 32, n)
+    check_attention(f, q[last], [(total - 32, 32)], out[last], lse[last])
+    few, few_lse = B.attention(kv, layers - 1, q[last], pos0=[total - 32], want_lse=True)
+    check_attention(f, q[last], [(total - 32, 32)], few, few_lse)
+    mass = torch.zeros(layers, kv_heads, total, device="cuda")
+    B.key_mass(kv, layers - 1, q[last].contiguous(), few_lse, mass[layers - 1], pos0=[total - 32])
+    _, _, _, off, want = attention(f, q[last], [(total - 32, 32)])
+    mass_close(mass[layers - 1], want[0], off.max().item() * 2, 32 * heads // kv_heads)
+    dst = B.LayerCache(layers, heads, dim, 4000, n_kv_heads=kv_heads)
+    kept, _ = B.evict(kv, mass, 4000, 4, 32, into=dst)
+    at = kept[layers - 1].cpu().long()
+    assert torch.equal(at, torch.cat([torch.cat([torch.arange(4), 4 + m[4:-32].argsort(descending=True, stable=True)[:4000 - 36].sort().values,
+                                                 torch.arange(total - 32, total)])[None] for m in mass[layers - 1].cpu()]))
+    for got, whole in zip(dst.read(layers - 1, 0, 4000), (k, v)):
+        whole = whole.reshape(total, kv_heads, dim)
+        assert torch.equal(got.cpu().reshape(4000, kv_heads, dim), torch.stack([whole[at[h], h] for h in range(kv_heads)], 1))
 
 
 BF16 = dataclasses.replace(synth.TINY_BF16, n_layers=2)
