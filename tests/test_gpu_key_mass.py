@@ -101,3 +101,25 @@ def test_weights_of_all_keys_add_up_to_the_rows():
         again = torch.zeros_like(mass)
         B.key_mass(filled.kvs, 0, rows, lse, again, n_rows=n_rows, pos0=pos0)
         assert torch.equal(again, mass)
+
+
+@pytest.mark.parametrize("cache,q", TYPES)
+@pytest.mark.parametrize("rules", [{}, dict(window=300), dict(cap=5.0)], ids=str)
+def test_rows_that_add_nothing_may_hold_anything(cache, q, rules):
+    """An lse of -infinity takes a row out of the sums: the bits are those of a call whose row holds zeros there.  First, last and in
+    between, in row tiles of one and of several rows, and with keys that all rows see."""
+    filled = Filled(4, 2, 64, [400], cache)
+    given = B.AttentionRules(**rules) if rules else None
+    for n, out in ((300, (0, 20, 299)), (75, (0, 20, 74)), (1, (0,)), (16, (3, 15))):
+        rows = rows_like(filled, n, DTYPES[q]).clone()
+        at = dict(pos0=[400 - n], rules=given)
+        _, lse = B.attention(filled.kvs[0], 0, rows, want_lse=True, **at)
+        masses = []
+        for value in (0.0, float("nan"), float("inf"), float("-inf")):
+            for r in out:
+                rows[r] = value
+                lse[r] = -math.inf
+            masses.append(B.key_mass(filled.kvs[0], 0, rows, lse, torch.zeros(2, 400, device="cuda"), **at))
+        assert torch.isfinite(masses[0]).all() and (masses[0].sum() > 0) == (n > len(out))
+        for got in masses[1:]:
+            assert torch.equal(got, masses[0])
