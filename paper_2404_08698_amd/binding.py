@@ -341,6 +341,16 @@ class Model:
         return {"steps": steps.value, "ms": dict(zip(PROF_CATEGORIES, list(ms))),
                 "intervals": dict(zip(PROF_CATEGORIES, list(cnt)))}
 
+
+def _settled(nbytes: int, device):
+    """Memory that calls on any stream are going to use: what its last owner may still do with it, on the current stream, is
+    waited for."""
+    import torch
+    t = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    torch.cuda.current_stream(t.device).synchronize()
+    return t
+
+
 class KVCache:
     """anpd_kv_*: one sequence's paged KV cache in a torch-allocated pool."""
 
@@ -414,7 +424,7 @@ class KVCache:
         nbytes = lib().anpd_kv_observe_workspace_bytes(self._h, rows)
         if nbytes == 0:
             _check(E_INVAL)
-        ws = torch.empty(nbytes, dtype=torch.uint8, device=mass.device)
+        ws = _settled(nbytes, mass.device)      # (prompts bring streams of their own)
         _check(lib().anpd_kv_observe(self._h, mass.data_ptr(), mass.shape[2], rows, ws.data_ptr(), nbytes))
         self._observed = (mass, ws)     # kept alive
 

@@ -276,3 +276,22 @@ def test_observe_refusals():
         assert L.anpd_kv_observe(*args) == code, args
     assert L.anpd_kv_observe(kv._h, m, 64, 32, p, need) == B.OK
     kv.observe(None)
+
+
+def test_the_workspace_of_observed_prompts_is_nobody_elses_any_more():
+    """It is taken from the current stream's memory and written by prompts on any other: what is queued on the first, and may use the
+    same memory, is done when the call returns."""
+    model = B.Model(BF16, synth.make_weights(BF16, 5, device="cuda"), max_positions=64)
+    kv = B.KVCache(model, 64)
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        mass = torch.zeros(2, 4, 64, device="cuda")
+        x = torch.zeros(8192, 8192, dtype=torch.bfloat16, device="cuda")
+        for _ in range(2):          # (the first time loads the product's kernel)
+            kv.observe(mass)
+            for _ in range(30):
+                x @ x
+        assert not stream.query()
+        kv.observe(mass)
+        assert stream.query()
+    kv.observe(None)
