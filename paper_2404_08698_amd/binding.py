@@ -360,7 +360,7 @@ class KVCache:
         nbytes = lib().anpd_kv_pool_bytes(model._h, max_tokens)
         if nbytes == 0:
             _check(E_INVAL)
-        self.pool = torch.empty(nbytes, dtype=torch.uint8, device=model.device)
+        self.pool = _settled(nbytes, model.device)
         h = C.c_void_p()
         _check(lib().anpd_kv_create(model._h, self.pool.data_ptr(), nbytes, max_tokens, C.byref(h)))
         self._h = h
@@ -549,7 +549,7 @@ class LayerCache(KVCache):
         nbytes = lib().anpd_cache_pool_bytes(C.byref(cfg), max_tokens)
         if nbytes == 0:
             _check(E_INVAL)
-        self.pool = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        self.pool = _settled(nbytes, device)
         # (what KVCache asks of its model)
         self.model = SimpleNamespace(shape=SimpleNamespace(n_layers=n_layers, n_heads=n_heads, head_dim=head_dim, n_kv_heads=n_kv_heads or n_heads, dtype=dtype),
                                      device=self.pool.device)

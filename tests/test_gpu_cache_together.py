@@ -295,3 +295,26 @@ def test_the_workspace_of_observed_prompts_is_nobody_elses_any_more():
         kv.observe(mass)
         assert stream.query()
     kv.observe(None)
+
+
+@pytest.mark.parametrize("own", [True, False], ids=["layer_cache", "model_cache"])
+def test_the_memory_of_a_cache_is_nobody_elses_any_more(own):
+    """Taken from a side stream's memory and cleared on the device's default stream: what is queued on the first, and may use the
+    same memory, is done before it is cleared, or unwritten positions would not read as zeros."""
+    model = B.Model(BF16, synth.make_weights(BF16, 5, device="cuda"), max_positions=64)
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        x = torch.zeros(8192, 8192, dtype=torch.bfloat16, device="cuda")
+
+        def make():
+            return B.LayerCache(2, 4, 64, 64) if own else B.KVCache(model, 64)
+        make()
+        x @ x
+        stream.synchronize()
+        for _ in range(30):
+            x @ x
+        before = stream.query()
+        kv = make()
+        assert not before and stream.query()
+    kv.truncate(64)
+    assert not any(t.any() for layer in range(2) for t in kv.read(layer, 0, 64))
