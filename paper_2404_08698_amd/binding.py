@@ -399,8 +399,12 @@ class KVCache:
     def write(self, layer: int, pos0: int, k, v, stream=None) -> None:
         """k, v: CUDA float32 [n][n_kv_heads * head_dim]."""
         import torch
-        assert k.is_cuda and k.dtype == torch.float32 and k.is_contiguous() and v.is_contiguous()
-        _check(lib().anpd_kv_write(self._h, layer, pos0, k.shape[0], k.data_ptr(), v.data_ptr(), _stream_ptr(stream)))
+        n = k.shape[0] if k.dim() else 0
+        for t in (k, v):
+            if not (t.device == self.pool.device and t.dtype == torch.float32 and t.is_contiguous()
+                    and t.dim() >= 2 and t.shape[0] == n and t.numel() == n * self.n_kv_heads * self.model.shape.head_dim):
+                raise ValueError("k and v: contiguous float32 [positions][n_kv_heads * head_dim] on the cache's device")
+        _check(lib().anpd_kv_write(self._h, layer, pos0, n, k.data_ptr(), v.data_ptr(), _stream_ptr(stream)))
 
     def read(self, layer: int, pos0: int, n: int, stream=None):
         import torch

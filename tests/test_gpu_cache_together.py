@@ -318,3 +318,18 @@ def test_the_memory_of_a_cache_is_nobody_elses_any_more(own):
         assert not before and stream.query()
     kv.truncate(64)
     assert not any(t.any() for layer in range(2) for t in kv.read(layer, 0, 64))
+
+
+def test_what_is_written_has_the_caches_width_and_type():
+    """Refused by the host: other numbers of rows, widths and types would be read beyond their ends."""
+    f = Filled(4, 2, 64, [40])
+    kv, good = f.kvs[0], torch.ones(3, 128, device="cuda")
+    for bad in (good[:2], good[:, :64].contiguous(), good.bfloat16(), good.double(), good.cpu(), good.repeat(1, 2)[:, ::2], good.reshape(-1), good.sum()):
+        for k, v in ((good, bad), (bad, good)):
+            with pytest.raises(ValueError):
+                kv.write(0, 5, k, v)
+    assert torch.equal(kv.read(0, 0, 40)[0].cpu(), f.k[0])
+    kv.write(0, 5, good, good.reshape(3, 2, 64))
+    kv.write(0, 8, good[:0], good[:0])
+    k, v = kv.read(0, 4, 5)
+    assert (k[1:4] == 1).all() and (v[1:4] == 1).all() and torch.equal(k[::4].cpu(), f.k[0][4:9:4])
