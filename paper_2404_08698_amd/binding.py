@@ -408,9 +408,8 @@ class KVCache:
 
     def read(self, layer: int, pos0: int, n: int, stream=None):
         import torch
-        d = (getattr(self.model.shape, "n_kv_heads", 0) or self.model.shape.n_heads) * self.model.shape.head_dim
-        k = torch.empty(n, d, dtype=torch.float32, device=self.model.device)
-        v = torch.empty(n, d, dtype=torch.float32, device=self.model.device)
+        d = self.n_kv_heads * self.model.shape.head_dim
+        k, v = (_empty((n, d), torch.float32, self.pool.device, stream) for _ in range(2))
         _check(lib().anpd_kv_read(self._h, layer, pos0, n, k.data_ptr(), v.data_ptr(), _stream_ptr(stream)))
         return k, v
 
@@ -748,7 +747,7 @@ def prefill(model: Model, kv: KVCache, prompt: Sequence[int], stream=None, out_l
     nb = prefill_workspace_bytes(model, n) if n >= 1 else 0
     ws = workspace
     if ws is None or ws.numel() < nb:
-        ws = torch.empty(max(nb, 256), dtype=torch.uint8, device="cuda")
+        ws = _empty(max(nb, 256), torch.uint8, kv.pool.device, stream)
     lp = 0
     if out_logits is not None:
         assert out_logits.is_cuda and out_logits.dtype == torch.float32 and out_logits.is_contiguous()

@@ -333,3 +333,27 @@ def test_what_is_written_has_the_caches_width_and_type():
     kv.write(0, 8, good[:0], good[:0])
     k, v = kv.read(0, 4, 5)
     assert (k[1:4] == 1).all() and (v[1:4] == 1).all() and torch.equal(k[::4].cpu(), f.k[0][4:9:4])
+
+
+def test_what_a_call_allocates_is_its_streams_memory(monkeypatch):
+    """Outputs and workspaces of a call on another stream than the current one come from that stream's memory, where it follows
+    what their last owner does with them."""
+    model = B.Model(BF16, synth.make_weights(BF16, 5, device="cuda"), max_positions=64)
+    kv, own = B.KVCache(model, 64), Filled(8, 1, 64, [3000], capacity=3001)
+    own.kvs[0].truncate(2999)
+    q, lse, mass = rows_like(own, 1), torch.zeros(1, 8, device="cuda"), torch.zeros(1, 1, 3000, device="cuda")
+    stream, seen, empty = torch.cuda.Stream(), [], torch.empty
+    torch.cuda.synchronize()
+    monkeypatch.setattr(torch, "empty", lambda *a, **k: (seen.append(torch.cuda.current_stream()), empty(*a, **k))[1])
+
+    def calls():
+        yield "prefill", lambda: B.prefill(model, kv, [1, 2, 3], stream=stream), 1
+        yield "read", lambda: kv.read(0, 0, 3, stream=stream), 2
+        yield "attention", lambda: B.attention(own.kvs, 0, q, want_lse=True, stream=stream), 3
+        yield "key_mass", lambda: B.key_mass(own.kvs, 0, q, lse, mass, stream=stream), 0
+        yield "evict", lambda: B.evict(own.kvs[0], mass, 20, stream=stream), 2
+    for name, call, n in calls():
+        del seen[:]
+        call()
+        assert len(seen) == n and all(s == stream for s in seen), (name, seen)
+    stream.synchronize()
