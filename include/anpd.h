@@ -409,10 +409,10 @@ int32_t anpd_attention(const anpd_kv_t *const *kvs, int32_t n_seq, const int32_t
                        float *lse, void *workspace, size_t workspace_bytes, void *stream);
 
 /* What the rows' weights add up to, per cached key: mass[g][j] += sum of exp(t - lse) over the rows and the query heads
- * that share key / value head g.  Arguments as in anpd_attention, whose lse this takes.  A row with an
- *   lse of -infinity adds nothing, whatever it holds itself.
+ * that share key / value head g.  Arguments as in anpd_attention, whose lse this takes.  A row with an lse of -infinity
+ * adds nothing, whatever it holds itself.
  *   mass (host, n_seq DEVICE pointers): [n_kv_heads][ld_mass] floats per sequence, ld_mass >= pos0[s] + n_rows[s]; no two
- *   sequences may share any of it.  Columns from pos0[s] + n_rows[s] on are left as they are. */
+ *   sequences may share any of it (one's rows may lie between another's).  Columns from pos0[s] + n_rows[s] on are left as they are. */
 size_t anpd_key_mass_workspace_bytes(const anpd_kv_t *const *kvs, int32_t n_seq, const int32_t *n_rows, const int32_t *pos0,
                                      const anpd_attn_rules *rules);
 int32_t anpd_key_mass(const anpd_kv_t *const *kvs, int32_t n_seq, const int32_t *n_rows, const int32_t *pos0, int32_t layer,

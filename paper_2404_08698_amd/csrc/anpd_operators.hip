@@ -328,6 +328,16 @@ bool overlap(const void *a, size_t na, const void *b, size_t nb)
     return (const char *)a < (const char *)b + nb && (const char *)b < (const char *)a + na;
 }
 
+// Do two arrays of `heads` rows, ld numbers apart in both, of na and nb numbers each (<= ld), share any?  Rows may lie between the other's.
+bool rows_overlap(const float *a, int64_t na, const float *b, int64_t nb, int64_t heads, int64_t ld)
+{
+    // row i of a and row i + h of b meet where -nb < d + h ld < na: the lowest h that is not too low
+    const int64_t d = ((intptr_t)b - (intptr_t)a) / (int64_t)sizeof(float), low = -nb - d;
+    int64_t h = (low >= 0 ? low / ld : -((-low - 1) / ld + 1)) + 1;
+    if (h < 1 - heads) h = 1 - heads;
+    return h < heads && d + h * ld < na;
+}
+
 bool cache_cfg_ok(const char *who, const anpd_cache_cfg *c, int32_t max_tokens, CacheShape *out)
 {
 #define REQ(cond, msg) if (!(cond)) { fail(ANPD_E_INVAL, "%s: " msg, who); return false; }
@@ -478,7 +488,7 @@ int32_t anpd_key_mass(const anpd_kv_t *const *kvs, int32_t n_seq, const int32_t 
         for (int t = 0; t < s; ++t) {
             if (a.seq[t].n == 0) continue;
             const int other = a.seq[t].pos0 + a.seq[t].n;
-            if (overlap(mass[s], ((size_t)(c.n_kv_heads - 1) * ld_mass + total) * sizeof(float), mass[t], ((size_t)(c.n_kv_heads - 1) * ld_mass + other) * sizeof(float)))
+            if (rows_overlap(mass[s], total, mass[t], other, c.n_kv_heads, ld_mass))
                 return fail(ANPD_E_INVAL, "%s: sequences %d and %d share mass", who, t, s);
         }
         to.mass[s] = mass[s];

@@ -123,3 +123,15 @@ def test_rows_that_add_nothing_may_hold_anything(cache, q, rules):
         assert torch.isfinite(masses[0]).all() and (masses[0].sum() > 0) == (n > len(out))
         for got in masses[1:]:
             assert torch.equal(got, masses[0])
+
+
+def test_masses_of_sequences_between_each_others_rows():
+    """[key heads][sequences][keys] seen as [sequences][key heads][keys]."""
+    filled = Filled(4, 2, 64, [300, 77, 300])
+    rows = rows_like(filled, 9)
+    at = dict(n_rows=[2, 4, 3], pos0=[298, 60, 200])
+    _, lse = B.attention(filled.kvs, 0, rows, want_lse=True, **at)
+    want, store = torch.zeros(3, 2, 300, device="cuda"), torch.zeros(2, 3, 300, device="cuda")
+    B.key_mass(filled.kvs, 0, rows, lse, want, **at)
+    got = B.key_mass(filled.kvs, 0, rows, lse, store.transpose(0, 1), **at)
+    assert torch.equal(got, want) and want.sum() > 0

@@ -340,5 +340,28 @@ def test_forms(stub):
     run(stub, "child_forms")
 
 
+def child_interleaved():
+    """Masses of several sequences may lie between each other's rows; whether they share any is said for every distance."""
+    c = Caches()
+    for kv_heads, total, other, ld in ((1, 6, 3, 9), (2, 6, 6, 12), (2, 6, 2, 11), (4, 5, 9, 14), (4, 1, 1, 1), (4, 1, 1, 2), (4, 7, 7, 7)):
+        a, b = (c.cache(64, 32, heads=4, kv_heads=kv_heads) for _ in range(2))
+        m = c.memory(1 << 12)
+        base = m + 4 * 256
+        rows = lambda at, n: {at + g * ld + j for g in range(kv_heads) for j in range(n)}      # noqa: E731
+        free = 0
+        for d in range(-4 * ld - 12, 4 * ld + 13):
+            shared = bool(rows(0, total) & rows(d, other))
+            free += not shared
+            c.stub.stub_forget()
+            rc = c.mass([a, b], [1, 1], [base, base + 4 * d], pos0=[total - 1, other - 1], ld=ld)
+            assert rc == (c.B.E_INVAL if shared else 0), (kv_heads, total, other, ld, d)
+            assert bool(c.names()) != shared and (not shared or "share" in c.L.anpd_last_error().decode())
+        assert free
+
+
+def test_interleaved_masses(stub):
+    run(stub, "child_interleaved")
+
+
 if __name__ == "__main__":
     globals()[sys.argv[1]](*sys.argv[2:])
