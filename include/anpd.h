@@ -439,8 +439,8 @@ int32_t anpd_kv_observe(anpd_kv_t *kv, float *mass, int64_t ld_mass, int32_t row
  *   (half-split pairing, as the model's own keys), so that it is the key of a token at position i, which is what
  *   the steps that follow take it for.
  *   out_kept: DEVICE, [n_layers][n_kv_heads][keep] ints, the positions that stayed, ascending.
- *   out_mass (nullable): DEVICE, [n_layers][n_kv_heads][ld_out] floats, ld_out >= keep: their mass.  Neither output may overlap mass or
- *   the other.
+ *   out_mass (nullable): DEVICE, [n_layers][n_kv_heads][ld_out] floats, ld_out >= keep: their mass.  Neither output may lie between
+ *   the first and the last number of mass or of the other.
  * 0 <= first + last <= keep <= length.  Blocks until it is done.
  * Errors: ANPD_E_INVAL, ANPD_E_CAPACITY (keep against length or dst), ANPD_E_HIP (contents and length of dst undefined). */
 int32_t anpd_kv_evict(const anpd_kv_t *src, anpd_kv_t *dst, const float *mass, int64_t ld_mass, int32_t keep, int32_t first,

@@ -720,9 +720,10 @@ def evict(src: KVCache, mass, keep: int, first: int = 0, last: int = 0, into: Op
     if not (mass.is_cuda and mass.device == src.pool.device and mass.dtype == torch.float32 and mass.dim() == 3 and mass.stride(2) == 1):
         raise ValueError("mass: float32 [n_layers][n_kv_heads][positions] on the cache's device")
     layers, kv_heads = src.n_layers, src.n_kv_heads
-    if mass.shape[:2] != (layers, kv_heads) or mass.shape[2] < src.length or (layers > 1 and mass.stride(0) != kv_heads * mass.stride(1)):
+    # elements between rows: of heads, of layers where there is one head, of a single row its length
+    ld = mass.stride(1) if kv_heads > 1 else mass.stride(0) if layers > 1 else mass.shape[2]
+    if mass.shape[:2] != (layers, kv_heads) or mass.shape[2] < src.length or (layers > 1 and mass.stride(0) != kv_heads * ld):
         raise ValueError("mass: one row of at least the cache's length per layer and key / value head, equally far apart")
-    ld = mass.stride(1) if layers * kv_heads > 1 else mass.shape[2]
     kept = _empty((layers, kv_heads, max(0, keep)), torch.int32, mass.device, stream)
     out = _empty((layers, kv_heads, max(0, keep)), torch.float32, mass.device, stream)
     dst = src if into is None else into

@@ -138,3 +138,19 @@ def test_a_cache_goes_on_after_eviction():
         k, v = torch.cat([k, more]), torch.cat([v, more])
         got = kv.read(0, 0, n // 2 + 60)
         assert torch.equal(got[0].cpu(), k) and torch.equal(got[1].cpu(), v)
+
+
+@pytest.mark.parametrize("layers,heads", [(3, 1), (1, 2), (1, 1), (3, 2)])
+def test_rows_of_mass_any_distance_apart(layers, heads):
+    """The same positions stay whatever the distance, where a layer has one row as well."""
+    kv, _ = filled(heads, 64, 100, "bf16", layers)
+    wide = torch.rand(layers * heads, 130, device="cuda")
+    flat = wide[:, 3:103]
+    mass = flat[:, None] if heads == 1 else wide.reshape(layers, heads, 130)[:, :, 3:103]
+    short = B.LayerCache(layers, heads, 64, 40)
+    a = B.evict(kv, mass, 40, into=short)
+    b = B.evict(kv, flat.contiguous().reshape(layers, heads, 100), 40, into=short)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    for bad in (mass[:, :, :99], torch.cat([mass, mass]), mass.double(), mass.cpu(), mass[0], mass.repeat(1, 1, 2)[:, :, ::2], torch.cat([mass, mass], 1)):
+        with pytest.raises(ValueError):
+            B.evict(kv, bad, 40, into=short)
