@@ -548,7 +548,10 @@ class LayerCache(KVCache):
                  page_tokens: int = 16, device="cuda"):
         import torch
         from types import SimpleNamespace
-        cfg = CacheCfg(n_layers, n_heads, head_dim, n_kv_heads, BF16 if dtype == "bf16" else F32, page_tokens)
+        types = {"bf16": BF16, "f32": F32}
+        if dtype not in types:
+            raise ValueError("dtype must be 'bf16' or 'f32'")
+        cfg = CacheCfg(n_layers, n_heads, head_dim, n_kv_heads, types[dtype], page_tokens)
         nbytes = lib().anpd_cache_pool_bytes(C.byref(cfg), max_tokens)
         if nbytes == 0:
             _check(E_INVAL)

@@ -363,5 +363,14 @@ def test_interleaved_masses(stub):
     run(stub, "child_interleaved")
 
 
+def test_types_of_a_cache():
+    """Any other word, or a type of torch, is no fp32 cache."""
+    import torch
+    from paper_2404_08698_amd import binding as B
+    for bad in ("bfloat16", "BF16", "fp32", "float32", "fp16", "", None, torch.bfloat16, torch.float32, B.BF16):
+        with pytest.raises(ValueError):
+            B.LayerCache(1, 4, 64, 64, dtype=bad)
+
+
 if __name__ == "__main__":
     globals()[sys.argv[1]](*sys.argv[2:])
