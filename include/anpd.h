@@ -375,7 +375,8 @@ int32_t anpd_cache_create(const anpd_cache_cfg *cfg, void *pool, size_t pool_byt
 
 /* Rules of the scores; all zero (or a NULL pointer in place of the struct): causal attention scaled by 1 / sqrt(head_dim).
  *   t = scale * q.k;  cap > 0: t = cap * tanh(t / cap);  t -= slopes[head] * |p - j|
- * A row at position p sees key j if j >= first_key[row] and (j < prefix or (j <= p and (window == 0 or j > p - window))). */
+ * A row at position p sees key j if j >= first_key[row] and (j < prefix or (j <= p and (window == 0 or j > p - window))).
+ * Keys end with the position of the sequence's last new row, whatever prefix says and the cache holds behind it. */
 typedef struct {
     float scale;                /* 0 = 1 / sqrt(head_dim) */
     float cap;                  /* 0 = none; scale / cap must be a normal fp32 number */

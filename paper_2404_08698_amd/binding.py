@@ -576,6 +576,8 @@ class AttentionRules:
         for t, dtype in ((slopes, torch.float32), (first_key, torch.int32)):
             if t is not None and not (t.is_cuda and t.dtype == dtype and t.is_contiguous()):
                 raise ValueError("slopes: contiguous CUDA float32, first_key: contiguous CUDA int32")
+        if not (0 <= window < 1 << 31 and 0 <= prefix < 1 << 31):     # (the struct would take their last 32 bits)
+            raise ValueError("window and prefix must be in 0..2^31 - 1")
         self.slopes, self.first_key = slopes, first_key
         self.struct = AttnRules(scale, cap, window, prefix, None if slopes is None else slopes.data_ptr(),
                                 None if first_key is None else first_key.data_ptr())
@@ -605,8 +607,8 @@ def _sequences(kvs, q, n_rows, pos0, rules):
             raise ValueError("n_rows does not add up to the rows")
         counts = (C.c_int32 * n)(*n_rows)
     if pos0 is not None:
-        if len(pos0) != n:
-            raise ValueError("pos0: one per sequence")
+        if len(pos0) != n or max(pos0) >= 1 << 31 or min(pos0) < 0:
+            raise ValueError("pos0: one position per sequence")
         pos0 = (C.c_int32 * n)(*pos0)
     if rules is not None:
         t = rules.slopes

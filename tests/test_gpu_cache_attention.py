@@ -277,3 +277,16 @@ def test_repeated_calls_agree_bit_for_bit():
     first = B.attention(filled.kvs[0], 0, rows, pos0=[1960])
     for _ in range(5):
         assert torch.equal(B.attention(filled.kvs[0], 0, rows, pos0=[1960]), first)
+
+
+@pytest.mark.parametrize("cache,q", TYPES)
+def test_the_largest_windows_and_prefixes(cache, q):
+    """A window of 2^31 - 1 hides nothing; a prefix of as much is all that is cached, up to the last new row, and no more."""
+    largest = (1 << 31) - 1
+    spans = [(290, 60), (0, 3), (100, 1)]
+    check(4, 2, 64, spans, cache, q, window=largest)
+    check(4, 2, 64, spans, cache, q, prefix=largest)
+    check(4, 2, 64, spans, cache, q, prefix=largest, window=largest)
+    filled = Filled(4, 2, 64, [400], cache)
+    with pytest.raises(ValueError):
+        B.attention(filled.kvs, 0, rows_like(filled, 1, DTYPES[q]), pos0=[1 << 32])

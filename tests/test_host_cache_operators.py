@@ -372,5 +372,16 @@ def test_types_of_a_cache():
             B.LayerCache(1, 4, 64, 64, dtype=bad)
 
 
+def test_rules_beyond_32_bits():
+    """A prefix or window of 2^32 would be none at all."""
+    from paper_2404_08698_amd import binding as B
+    for bad in (1 << 31, 1 << 32, (1 << 32) + 5, -1, -(1 << 32)):
+        for name in ("window", "prefix"):
+            with pytest.raises(ValueError):
+                B.AttentionRules(**{name: bad})
+    r = B.AttentionRules(window=(1 << 31) - 1, prefix=(1 << 31) - 1)
+    assert (r.struct.window, r.struct.prefix) == ((1 << 31) - 1, (1 << 31) - 1)
+
+
 if __name__ == "__main__":
     globals()[sys.argv[1]](*sys.argv[2:])
