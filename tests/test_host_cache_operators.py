@@ -363,6 +363,29 @@ def test_interleaved_masses(stub):
     run(stub, "child_interleaved")
 
 
+def child_forms_with_rules():
+    """Every call that shared_forms.py lists takes the form whose rows share keys, in the instance that it is listed for."""
+    sys.path.insert(0, HERE)
+    from shared_forms import cases
+    c = Caches()
+    ws, seen = c.memory(64 << 20), set()
+    for (heads, kv_heads, dim, spans), q, rules in cases():
+        kvs = [c.cache(p + n, p + n, heads, kv_heads, dim, layers=1) for p, n in spans]
+        rules = dict(rules)
+        given = c.B.AttnRules(first_key=ws if rules.pop("document", 0) else None, **rules)
+        c.stub.stub_forget()
+        assert c.attention(kvs, [n for _, n in spans], [p for p, _ in spans], dtype=c.B.F32 if q == "f32" else c.B.BF16, ldq=heads * dim, ldo=heads * dim,
+                           ws=ws, nb=64 << 20, rules=given) == 0, c.L.anpd_last_error()
+        name = c.names()[0]
+        assert "cache_attn_tile_kernel" in name, (heads, kv_heads, dim, spans, q, rules, name)
+        seen.add((name, len(c.names())))
+    assert len({name for name, _ in seen}) == 4 and {n for _, n in seen} == {1, 2}, seen
+
+
+def test_forms_with_rules(stub):
+    run(stub, "child_forms_with_rules")
+
+
 def test_types_of_a_cache():
     """Any other word, or a type of torch, is no fp32 cache."""
     import torch
