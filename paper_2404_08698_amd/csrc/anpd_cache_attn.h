@@ -766,7 +766,7 @@ __global__ __launch_bounds__(tile_waves(TERMS) * 64, tile_waves(TERMS) / 4) void
     const uint32_t offset = wave % NCH * 1024 + lane * 16;
     // (beyond the last tile: the last one, for nothing, so that the loads in flight can be counted)
     auto request = [&](int i) __attribute__((always_inline)) {
-        const int x = (i < i1 ? i : i1 - 1) - ids0;
+        const int left = i1 - 1 - ids0, last = left > 0 ? left : 0, x = i - ids0 < last ? i - ids0 : last;   // (addresses fetched behind the last tile: all its own)
         const uint32_t at = lds0 + (uint32_t)((i - i0) & (kTileSlots - 1)) * (4 * NCH * 1024);
 #pragma unroll
         for (int c = 0; c < LOADS; ++c) {
