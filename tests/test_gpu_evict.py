@@ -154,3 +154,10 @@ def test_rows_of_mass_any_distance_apart(layers, heads):
     for bad in (mass[:, :, :99], torch.cat([mass, mass]), mass.double(), mass.cpu(), mass[0], mass.repeat(1, 1, 2)[:, :, ::2], torch.cat([mass, mass], 1)):
         with pytest.raises(ValueError):
             B.evict(kv, bad, 40, into=short)
+
+
+@pytest.mark.parametrize("n", [1023, 1024, 1025, 4096, 4097, 16384, 16385, 65536, 65537])
+def test_lengths_around_those_where_the_search_changes(n):
+    """Whole steps of the positions that a lane holds, and one more; most of them equal, and all but one kept."""
+    check(1, 64, n, n // 3, 2, 5, layers=1, equal=0.95, seed=n)
+    check(2, 64, n, n - 1, layers=1, into="self", equal=0.5, seed=n + 1)
