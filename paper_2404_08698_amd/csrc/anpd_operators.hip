@@ -164,9 +164,10 @@ Plan plan_attention(AttnArgs &a, const CacheShape &c, int n_cu)
     // begin with.  Shared: a tile of 32 keys 0.9 us (1.28) of the longest block, 1.1 (1.45) of a unit where there are many, 1.6 (2.5) more for those
     // that a window cuts; six to begin with, or twelve and the parts that are joined, at 4.5 TB/s.  Documents that begin behind a row's
     // first key, which are not looked at here, shorten the former more, with fp32 rows always enough.  Caps and biases are the former's: their
-    // vector instructions leave nothing to share.  330 shapes (1, 4 and 16 heads per key head, 128 to 3584 rows, windows, documents): 1.1 % above the better one on
-    // average, 29 % at worst.  32 heads of 128, blocks of 32 rows / shared, us: 1000 rows 25 / 36, 2000 65 / 59, 3584 169 / 118; fp32 39 / 47, 114 / 106,
-    // 301 / 275; 3584 in a window of 300 69 / 77, one key head for 16 67 / 43; 3584 with a cap 252 / 315, fp32 400 / 677.
+    // vector instructions leave nothing to share.  600 shapes (heads of 128 and 64, 1 to 16 per key head, 128 to 3584 rows, windows, prefixes, documents):
+    // 2.3 % above the better one on average, heads of 128 1.2; 50 by more than a tenth, 57 % at worst (documents, heads of 64: a tile of theirs costs the
+    // former less than is reckoned here).  32 heads of 128, blocks of 32 rows / shared, us: 1000 rows 24 / 35, 2000 63 / 58, 3584 160 / 112; fp32 37 / 45,
+    // 109 / 99, 296 / 271; 3584 in a window of 300 68 / 75, one key head for 16 67 / 42; 3584 with a cap 252 / 315, fp32 400 / 677.
     int64_t rows = 0;
     for (int s = 0; s < a.n_seq; ++s) rows += a.seq[s].n;
     const double longest_us = (a.q_f32 ? 1.28 : 0.9) * (double)shared_chunk, all_us = (a.q_f32 ? 1.45 : 1.1) * (double)tiles[1] / n_cu;
