@@ -306,8 +306,14 @@ int32_t make_cache(const char *who, const anpd_model *m, const CacheShape &shape
     kv->n_pages = (max_tokens + shape.page_tokens - 1) / shape.page_tokens;
     kv->max_tokens = max_tokens;
     kv->len = 0;
-    kv->table.assign((size_t)kv->n_pages, -1);
-    kv->dev_table.assign((size_t)kv->n_pages, -1);
+    try {
+        kv->table.assign((size_t)kv->n_pages, -1);
+        kv->dev_table.assign((size_t)kv->n_pages, -1);
+        kv->free_list.reserve((size_t)kv->n_pages);   // (it never grows later)
+    } catch (const std::bad_alloc &) {
+        delete kv;
+        return fail(ANPD_E_NOMEM, "%s: out of memory", who);
+    }
     for (int p = kv->n_pages - 1; p >= 0; --p) kv->free_list.push_back(p);  // page 0 is handed out first
     char *tail = kv->pool + align_up((size_t)kv->n_pages * shape.page_bytes());
     kv->d_len = (int32_t *)tail;

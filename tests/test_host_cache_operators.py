@@ -386,6 +386,59 @@ def test_forms_with_rules(stub):
     run(stub, "child_forms_with_rules")
 
 
+NO_MEMORY = r"""
+// operator new, which gives nothing from the n-th time on if told so
+#include <cstdlib>
+#include <new>
+static long g_left = -1;
+extern "C" void stub_news_left(long n) { g_left = n; }
+void *operator new(std::size_t n)
+{
+    if (g_left == 0) throw std::bad_alloc();
+    if (g_left > 0) --g_left;
+    if (void *p = std::malloc(n)) return p;
+    throw std::bad_alloc();
+}
+void operator delete(void *p) noexcept { std::free(p); }
+void operator delete(void *p, std::size_t) noexcept { std::free(p); }
+"""
+
+
+def child_no_memory():
+    """Host memory that runs out in the middle is reported: an exception must not leave a C entry."""
+    news = C.CDLL(os.environ["ANPD_NO_MEMORY"], mode=C.RTLD_GLOBAL)
+    news.stub_news_left.argtypes = [C.c_long]
+    c = Caches()
+    cfg = c.B.CacheCfg(2, 4, 64, 2, 1, 16)
+    n, kv = c.L.anpd_cache_pool_bytes(C.byref(cfg), 1 << 16), C.c_void_p()
+    pool = c.memory(n)
+    failed = 0
+    for left in range(8):
+        news.stub_news_left(left)
+        rc = c.L.anpd_cache_create(C.byref(cfg), pool, n, 1 << 16, C.byref(kv))
+        news.stub_news_left(-1)
+        if rc == 0:
+            break
+        failed += 1
+        assert rc == c.B.E_NOMEM and not kv.value and "memory" in c.L.anpd_last_error().decode()
+    assert failed == 4 and rc == 0       # the handle and three lists
+    # growing and shrinking takes no more
+    assert c.L.anpd_kv_truncate(kv, 1 << 16, None) == 0
+    news.stub_news_left(0)
+    rcs = [c.L.anpd_kv_truncate(kv, m, None) for m in (0, 1 << 16, 17, 0)]
+    news.stub_news_left(-1)
+    assert rcs == [0] * 4
+    c.L.anpd_kv_destroy(kv)
+
+
+def test_host_memory_that_runs_out(stub, tmp_path):
+    (tmp_path / "news.cpp").write_text(NO_MEMORY)
+    subprocess.run(["g++", "-O1", "-fPIC", "-shared", str(tmp_path / "news.cpp"), "-o", str(tmp_path / "news.so")], check=True)
+    env = dict(os.environ, ANPD_HIP_STUB=stub, PYTHONPATH=os.path.dirname(HERE), ANPD_NO_MEMORY=str(tmp_path / "news.so"))
+    r = subprocess.run([sys.executable, os.path.abspath(__file__), "child_no_memory"], capture_output=True, text=True, timeout=120, env=env)
+    assert r.returncode == 0, r.stdout + r.stderr
+
+
 def test_types_of_a_cache():
     """Any other word, or a type of torch, is no fp32 cache."""
     import torch
