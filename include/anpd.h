@@ -404,6 +404,7 @@ typedef struct {
  * weights rounded to bf16 for the second product (outputs are off by 2.2e-3 of their norm, where their own rounding makes 1.7e-3), and
  * their capped scores are off by up to 2^-22 of the cap where that is 256 at most, in lse as well; anpd_key_mass takes scores of all
  * rows in full, so the weights of such a row add up to 1 but for that difference.
+ * Weights are up to 2^8 until they are divided by their sum: values of up to 2^99 in magnitude cannot overflow, however many.
  * Asynchronous on stream; may be captured into a graph (which then holds these positions; the page table is read when it
  * runs).  Errors: ANPD_E_CAPACITY (positions, workspace), ANPD_E_INVAL (also: a position without a page), ANPD_E_HIP. */
 size_t anpd_attention_workspace_bytes(const anpd_kv_t *const *kvs, int32_t n_seq, const int32_t *n_rows, const int32_t *pos0,
