@@ -44,7 +44,7 @@ enum {
     ANPD_E_UNIMPLEMENTED = -6
 };
 
-enum { ANPD_F32 = 0, ANPD_BF16 = 1 };               /* storage type of weights and of cached K/V */
+enum { ANPD_F32 = 0, ANPD_BF16 = 1, ANPD_INT8 = 8 };   /* storage type of weights and of cached K/V (INT8: caches without a model) */
 enum { ANPD_VERIFY = 0, ANPD_APPEND = 1 };          /* anpd_verify modes */
 /* GEMM forms.  DOT: exact fp32 products (fp32 matrix cores) on the caller's row-major weights (any dtype).
  * MFMA: matrix cores on bf16 weights repacked into fragment order.  MFMA_STREAM (anpd_linear
@@ -356,6 +356,7 @@ int32_t anpd_linear_static(const float *X, const void *W, float *Y, int32_t M, i
  * every cached key receives, and the eviction of the keys that receive little.  For programs whose layers are their
  * own (other projections, capped or biased scores, sliding windows, packed documents), beside anpd_linear, and to
  * shorten the cache that anpd_prefill has filled before the steps that follow (anpd_kv_observe).
+ * Trees of drafted tokens, caches of 8-bit keys and values and the drawing of tokens are further below.
  * Head dims 64 and 128.  Sums, maxima and outputs are formed in 32 bits; results do not depend on timing (no
  * floating-point atomics), but on how the keys are divided among blocks, which depends on the sizes of a call.
  * ---------------------------------------------------------------------- */
@@ -364,9 +365,15 @@ int32_t anpd_linear_static(const float *X, const void *W, float *Y, int32_t M, i
 typedef struct {
     int32_t n_layers, n_heads, head_dim;
     int32_t n_kv_heads;     /* 0 = n_heads; must divide n_heads */
-    int32_t dtype;          /* ANPD_F32 | ANPD_BF16 */
-    int32_t page_tokens;    /* power of two in 8..256; bf16 pages of 16 are kept in matrix-core order, which is the faster form */
+    int32_t dtype;          /* ANPD_F32 | ANPD_BF16 | ANPD_INT8 */
+    int32_t page_tokens;    /* power of two in 8..256; bf16 pages of 16 are kept in matrix-core order, which is the faster form; INT8: 16 */
 } anpd_cache_cfg;
+/* ANPD_INT8: every position's keys and values are held, per key / value head, as signed codes of 8 bits and an fp32 scale of their own:
+ *   scale = max |x| / 127 (in fp32);  code = 127 x / max |x| to the nearest whole number, ties to the even one;  value = code * scale
+ * (all zeros: scale 0).  Where one of the head_dim numbers is infinite or NaN, the scale is NaN and so are all values of it.  A value is off by at most
+ * half a step, max |x| / 254, and by the rounding of code * scale.  head_dim + 4 bytes each; attention reads half of what bf16 takes.
+ * anpd_kv_write, anpd_kv_read, anpd_kv_store, anpd_kv_load, anpd_kv_commit, anpd_attention and anpd_tree_attention take such caches;
+ * anpd_key_mass and anpd_kv_evict do not (ANPD_E_UNIMPLEMENTED). */
 /* As anpd_kv_pool_bytes / anpd_kv_create; max_tokens in 1..2^20.  Destroy with anpd_kv_destroy. */
 size_t anpd_cache_pool_bytes(const anpd_cache_cfg *cfg, int32_t max_tokens);
 int32_t anpd_cache_create(const anpd_cache_cfg *cfg, void *pool, size_t pool_bytes, int32_t max_tokens, anpd_kv_t **out);
@@ -450,6 +457,80 @@ int32_t anpd_kv_observe(anpd_kv_t *kv, float *mass, int64_t ld_mass, int32_t row
  * Errors: ANPD_E_INVAL, ANPD_E_CAPACITY (keep against length or dst), ANPD_E_HIP (contents and length of dst undefined). */
 int32_t anpd_kv_evict(const anpd_kv_t *src, anpd_kv_t *dst, const float *mass, int64_t ld_mass, int32_t keep, int32_t first,
                       int32_t last, float rope_base, int32_t *out_kept, float *out_mass, int64_t ld_out, void *stream);
+
+/* Rows of keys and values into the caches of a layer, as they come from its projections: rounded to the caches' type, or quantised (ANPD_INT8).
+ *   kvs (host, n_seq handles of different caches of the same shape), n_rows, pos0: as in anpd_attention.  Pages are added as
+ *   needed; lengths do not change (anpd_kv_truncate, anpd_kv_commit).
+ *   k, v: DEVICE, the rows of all sequences one after the other, n_kv_heads * head_dim elements of dtype (ANPD_F32 | ANPD_BF16) each,
+ *   ldk / ldv elements apart.  No alignment is needed beyond the type's; rows that begin on 16 bytes are moved faster.
+ * Asynchronous on stream, except that a call that adds pages (or is the first after others have) waits until it is done; such a call is refused
+ * while the stream is captured (ANPD_E_INVAL): grow the cache before (anpd_kv_truncate), and the call may be captured. */
+int32_t anpd_kv_store(anpd_kv_t *const *kvs, int32_t n_seq, const int32_t *n_rows, const int32_t *pos0, int32_t layer, const void *k, int64_t ldk,
+                      const void *v, int64_t ldv, int32_t dtype, void *stream);
+/* ... and back: what the caches hold at those positions, rounded once to dtype.  One cache may occur twice.  Asynchronous on stream; may be captured.
+ * Both: ANPD_E_CAPACITY (positions), ANPD_E_INVAL (load: also a position without a page), ANPD_E_HIP. */
+int32_t anpd_kv_load(const anpd_kv_t *const *kvs, int32_t n_seq, const int32_t *n_rows, const int32_t *pos0, int32_t layer, void *k, int64_t ldk,
+                     void *v, int64_t ldv, int32_t dtype, void *stream);
+
+/* Attention of trees of drafted tokens: the new rows of a sequence continue one another as in anpd_verify_tree, each seeing the cached positions,
+ * its own ancestors and itself.
+ *   Arguments as in anpd_attention, and parent (DEVICE, one int per row of the call): the row of the same sequence that this one
+ *   continues (0 for a sequence's first row), an earlier one; any other value: the row follows the cached positions, as the root
+ *   does (-1).  At most ANPD_TREE_MAX_ROWS rows per sequence (ANPD_E_CAPACITY).
+ *   Row r's keys and values lie in slot pos0 + r of the cache; its position is pos0 + the number of its ancestors.  The rules
+ *   go by positions: a row at position p sees, of those keys, the ones at positions that anpd_attention would show it.  A chain (parent = row - 1)
+ *   is anpd_attention.
+ * Errors and asynchrony as anpd_attention; parent is read when the kernels run, so a captured call takes the tree that is there then. */
+#define ANPD_TREE_MAX_ROWS 64
+size_t anpd_tree_attention_workspace_bytes(const anpd_kv_t *const *kvs, int32_t n_seq, const int32_t *n_rows, const int32_t *pos0,
+                                           const anpd_attn_rules *rules);
+int32_t anpd_tree_attention(const anpd_kv_t *const *kvs, int32_t n_seq, const int32_t *n_rows, const int32_t *pos0, int32_t layer,
+                            const void *q, int64_t ldq, int32_t dtype, const int32_t *parent, const anpd_attn_rules *rules, void *out,
+                            int64_t ldo, float *lse, void *workspace, size_t workspace_bytes, void *stream);
+/* The rows of a tree that were accepted: those in slots length + rows[0], length + rows[1], ... (host, n ints, ascending, below
+ * ANPD_TREE_MAX_ROWS: a path from the root) move to positions length .. length + n - 1, in all layers, and the length becomes length + n.
+ * n = 0 commits nothing.  What lies behind is given up, pages included.  Blocks until it is done.  Errors: ANPD_E_INVAL (rows, or one without a page),
+ * ANPD_E_CAPACITY, ANPD_E_HIP. */
+int32_t anpd_kv_commit(anpd_kv_t *kv, const int32_t *rows, int32_t n, void *stream);
+
+/* ------------------------------------------------------------------------
+ * Drawing tokens.
+ * ---------------------------------------------------------------------- */
+
+/* Which tokens may be drawn, and how likely.  a_i = (x_i - max x) / temperature, w_i = exp(a_i); tokens in order of their logits, equal ones by index:
+ *   the first top_k of them; of these, those before which less than top_p of their weights' sum has been added up; of these, those with w_i >= min_p.
+ * The first token is always among them.  A NULL pointer in place of the struct: temperature 1, all tokens.
+ * Arrays (DEVICE, one number per row, or NULL) take the place of the numbers; what they hold is read as the numbers are, values that those may not have
+ * as follows: a temperature that is not above 0 is 0, top_k below 1 and top_p above 1 or NaN are none, top_p below 0 is 0, min_p above 1 is 1, below 0 or NaN 0. */
+typedef struct {
+    float temperature;           /* finite, >= 0; 0: the largest logit's token, the lowest index among equal ones */
+    int32_t top_k;               /* 0 = all */
+    float top_p, min_p;          /* 0..1; top_p 1 = all, min_p 0 = all */
+    const float *temperatures;
+    const int32_t *top_ks;
+    const float *top_ps, *min_ps;
+} anpd_sample_rules;
+
+/* One token for each row of logits, by the caller's random numbers.
+ *   logits: DEVICE, rows of vocab (1..2^20) numbers of dtype (ANPD_F32 | ANPD_BF16), ld elements apart.  Minus infinity and NaN are never drawn;
+ *   where some are plus infinity, those are drawn equally.
+ *   uniform: DEVICE, rows floats in [0, 1) (others count as the nearest of these, NaN as 0).
+ *   out_token: DEVICE, rows ints: the lowest index i at which the weights of the tokens that remain, added up by index, exceed uniform times
+ *     their sum; -1 where a row holds no token at all.
+ *   out_logprob (nullable, DEVICE, rows floats): the logarithm of the probability with which it is drawn (temperature 0: 0; no token: NaN).
+ * Weights are formed in 64 bits and held as multiples of 2^-51 of the largest (2^-43 for vocabularies near 2^20), whose sums are exact: the same inputs give the same tokens.
+ * Asynchronous on stream; may be captured.  Errors: ANPD_E_INVAL, ANPD_E_HIP. */
+int32_t anpd_sample(const void *logits, int64_t ld, int32_t dtype, int32_t rows, int32_t vocab, const anpd_sample_rules *rules, const float *uniform,
+                    int32_t *out_token, float *out_logprob, void *stream);
+
+/* One verification step that draws instead of taking the argmax.  The drafts of a table are certain, not drawn, so a token is drawn after every row,
+ * and draft j is accepted while it is the token drawn after row j - 1; the first that is not is the next token.  What is
+ * generated is distributed as if every token had been drawn by itself.
+ *   Arguments as in anpd_verify (ANPD_VERIFY).  uniform: DEVICE, n_window floats.  logits: DEVICE, n_window * vocab floats, written.
+ *   out_tokens (nullable, host, n_window ints): the token drawn after every row.
+ * Errors as anpd_verify and anpd_sample; ANPD_E_RANGE if a row has no token (all NaN): nothing is committed. */
+int32_t anpd_verify_sample(anpd_model_t *m, anpd_kv_t *kv, const int32_t *window, int32_t n_window, const anpd_sample_rules *rules,
+                           const float *uniform, int32_t *out_accepted, int32_t *out_next, int32_t *out_tokens, float *logits, void *stream);
 
 #ifdef __cplusplus
 }

@@ -7,6 +7,7 @@ the stream.  There is no CPU fallback: if the library is missing, importing
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 from typing import Dict, List, Optional, Sequence, Tuple
@@ -15,10 +16,11 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libanpd.so")
 
 OK, E_INVAL, E_RANGE, E_CAPACITY, E_NOMEM, E_HIP, E_UNIMPLEMENTED = 0, -1, -2, -3, -4, -5, -6
-F32, BF16 = 0, 1
+F32, BF16, INT8 = 0, 1, 8
 VERIFY, APPEND = 0, 1
 GEMM_AUTO, GEMM_DOT, GEMM_MFMA, GEMM_MFMA_STREAM, GEMM_MFMA_LAUNCHES = 0, 1, 2, 3, 4
 MAX_WINDOW = 32
+TREE_MAX_ROWS = 64
 
 _PER_LAYER = ("attn_norm", "wq", "wk", "wv", "wo", "ffn_norm", "w_gate", "w_up", "w_down")
 
@@ -36,6 +38,8 @@ EXPORTS = (
     "anpd_cache_pool_bytes", "anpd_cache_create", "anpd_attention_workspace_bytes", "anpd_attention",
     "anpd_key_mass_workspace_bytes", "anpd_key_mass", "anpd_kv_evict",
     "anpd_kv_observe_workspace_bytes", "anpd_kv_observe",
+    "anpd_kv_store", "anpd_kv_load", "anpd_tree_attention_workspace_bytes", "anpd_tree_attention", "anpd_kv_commit",
+    "anpd_sample", "anpd_verify_sample",
 )
 PROF_CATEGORIES = ("gemm_qkv", "gemm_o", "gemm_gate_up", "gemm_down", "gemm_lm_head", "attn", "other", "step")
 
@@ -61,6 +65,11 @@ class CacheCfg(C.Structure):
 class AttnRules(C.Structure):
     _fields_ = [("scale", C.c_float), ("cap", C.c_float), ("window", C.c_int32), ("prefix", C.c_int32),
                 ("slopes", C.c_void_p), ("first_key", C.c_void_p)]
+
+
+class SampleRules(C.Structure):
+    _fields_ = [("temperature", C.c_float), ("top_k", C.c_int32), ("top_p", C.c_float), ("min_p", C.c_float)] + \
+               [(n, C.c_void_p) for n in ("temperatures", "top_ks", "top_ps", "min_ps")]
 
 
 class Weights(C.Structure):
@@ -177,6 +186,21 @@ def lib():
     L.anpd_kv_observe_workspace_bytes.argtypes = [vp, C.c_int32]
     L.anpd_kv_observe.restype = C.c_int32
     L.anpd_kv_observe.argtypes = [vp, vp, C.c_int64, C.c_int32, vp, C.c_size_t]
+    rows = seqs + [C.c_int32, vp, C.c_int64, vp, C.c_int64, C.c_int32, vp]
+    L.anpd_kv_store.restype = C.c_int32
+    L.anpd_kv_store.argtypes = rows
+    L.anpd_kv_load.restype = C.c_int32
+    L.anpd_kv_load.argtypes = rows
+    L.anpd_tree_attention_workspace_bytes.restype = C.c_size_t
+    L.anpd_tree_attention_workspace_bytes.argtypes = seqs + [vp]
+    L.anpd_tree_attention.restype = C.c_int32
+    L.anpd_tree_attention.argtypes = seqs + [C.c_int32, vp, C.c_int64, C.c_int32, vp, vp, vp, C.c_int64, vp, vp, C.c_size_t, vp]
+    L.anpd_kv_commit.restype = C.c_int32
+    L.anpd_kv_commit.argtypes = [vp, i32p, C.c_int32, vp]
+    L.anpd_sample.restype = C.c_int32
+    L.anpd_sample.argtypes = [vp, C.c_int64, C.c_int32, C.c_int32, C.c_int32, vp, vp, vp, vp, vp]
+    L.anpd_verify_sample.restype = C.c_int32
+    L.anpd_verify_sample.argtypes = [vp, vp, i32p, C.c_int32, vp, vp, i32p, i32p, i32p, vp, vp]
     _lib = L
     return L
 
@@ -413,6 +437,10 @@ class KVCache:
         _check(lib().anpd_kv_read(self._h, layer, pos0, n, k.data_ptr(), v.data_ptr(), _stream_ptr(stream)))
         return k, v
 
+    def commit(self, rows: Sequence[int], stream=None) -> None:
+        """anpd_kv_commit: the rows of a tree that were accepted (a path from the root) move together behind the committed positions."""
+        _check(lib().anpd_kv_commit(self._h, _ints(rows), len(rows), _stream_of(self.pool.device, stream)))
+
     def observe(self, mass, rows: int = 32) -> None:
         """anpd_kv_observe: prompts into this cache add the weights of their last rows to mass, CUDA float32
         [n_layers][n_kv_heads][positions that they may reach], contiguous (None: no longer)."""
@@ -542,15 +570,16 @@ def linear_static(X, packed, N: int, Y, stream=None):
 
 class LayerCache(KVCache):
     """anpd_cache_create: a paged cache without a model, for programs whose layers are their own.  All of KVCache's
-    methods; verify and prefill do not take it."""
+    methods; verify and prefill do not take it.  dtype "int8": keys and values as 8-bit codes with a scale for every position and
+    head, which are quantised as they are written."""
 
     def __init__(self, n_layers: int, n_heads: int, head_dim: int, max_tokens: int, n_kv_heads: int = 0, dtype: str = "bf16",
                  page_tokens: int = 16, device="cuda"):
         import torch
         from types import SimpleNamespace
-        types = {"bf16": BF16, "f32": F32}
+        types = {"bf16": BF16, "f32": F32, "int8": INT8}
         if dtype not in types:
-            raise ValueError("dtype must be 'bf16' or 'f32'")
+            raise ValueError("dtype must be 'bf16', 'f32' or 'int8'")
         cfg = CacheCfg(n_layers, n_heads, head_dim, n_kv_heads, types[dtype], page_tokens)
         nbytes = lib().anpd_cache_pool_bytes(C.byref(cfg), max_tokens)
         if nbytes == 0:
@@ -673,6 +702,23 @@ def attention(kvs, layer: int, q, n_rows: Optional[Sequence[int]] = None, pos0: 
               rules: Optional[AttentionRules] = None, out=None, lse=None, want_lse: bool = False, workspace=None, stream=None):
     """anpd_attention: new rows of one cache or of a list of caches over what is cached.  q: CUDA float32 or bfloat16
     [rows of all sequences][n_heads * head_dim].  Returns out, or (out, lse) where lse was given or asked for."""
+    L = lib()
+    return _attend(L.anpd_attention, L.anpd_attention_workspace_bytes, kvs, layer, q, (), n_rows, pos0, rules, out, lse, want_lse, workspace, stream)
+
+
+def tree_attention(kvs, layer: int, q, parent, n_rows: Optional[Sequence[int]] = None, pos0: Optional[Sequence[int]] = None,
+                   rules: Optional[AttentionRules] = None, out=None, lse=None, want_lse: bool = False, workspace=None, stream=None):
+    """anpd_tree_attention: as attention(), where the new rows of every sequence are a tree of drafts.  parent: CUDA int32, for every
+    row the row of its sequence that it continues, -1 for the root."""
+    import torch
+    if not (parent.device == q.device and parent.dtype == torch.int32 and parent.is_contiguous() and parent.dim() == 1 and parent.shape[0] == q.shape[0]):
+        raise ValueError("parent: contiguous int32, one per row, on the caches' device")
+    L = lib()
+    return _attend(L.anpd_tree_attention, L.anpd_tree_attention_workspace_bytes, kvs, layer, q, (parent.data_ptr(),), n_rows, pos0, rules, out, lse, want_lse,
+                   workspace, stream)
+
+
+def _attend(fn, bytes_of, kvs, layer, q, tree, n_rows, pos0, rules, out, lse, want_lse, workspace, stream):
     import torch
     shape, n, handles, counts, at = _sequences(kvs, q, n_rows, pos0, rules)
     rows = q.shape[0]
@@ -685,9 +731,8 @@ def attention(kvs, layer: int, q, n_rows: Optional[Sequence[int]] = None, pos0: 
             raise ValueError("lse: contiguous float32 [rows][n_heads]")
     elif want_lse:
         lse = _empty((rows, shape.n_heads), torch.float32, q.device, stream)
-    L, ref = lib(), None if rules is None else rules.ref
-    _with_workspace(L.anpd_attention, L.anpd_attention_workspace_bytes, (handles, n, counts, at), ref,
-                    (layer, q.data_ptr(), _pitch(q), F32 if q.dtype == torch.float32 else BF16, ref),
+    ref = None if rules is None else rules.ref
+    _with_workspace(fn, bytes_of, (handles, n, counts, at), ref, (layer, q.data_ptr(), _pitch(q), F32 if q.dtype == torch.float32 else BF16, *tree, ref),
                     (out.data_ptr(), _pitch(out), None if lse is None else lse.data_ptr()), workspace, q.device, stream)
     return out if lse is None else (out, lse)
 
@@ -735,6 +780,135 @@ def evict(src: KVCache, mass, keep: int, first: int = 0, last: int = 0, into: Op
     _check(lib().anpd_kv_evict(src._h, dst._h, mass.data_ptr(), ld, keep, first, last, rope_base, kept.data_ptr(), out.data_ptr(), max(0, keep),
                                _stream_of(mass.device, stream)))
     return kept, out
+
+
+def _span_of(kvs, n_rows, pos0):
+    """(caches, n_seq, handles, rows, positions or None) of store() and load()."""
+    if isinstance(kvs, KVCache):
+        kvs = (kvs,)
+    n = len(kvs)
+    if n == 0 or len(n_rows) != n or min(n_rows) < 0:
+        raise ValueError("n_rows: one number per cache")
+    if pos0 is not None and (len(pos0) != n or max(pos0) >= 1 << 31 or min(pos0) < 0):
+        raise ValueError("pos0: one position per sequence")
+    return kvs, n, (C.c_void_p * n)(*[kv._h.value for kv in kvs]), (C.c_int32 * n)(*n_rows), None if pos0 is None else (C.c_int32 * n)(*pos0)
+
+
+def _check_rows(t, rows: int, kv, dtype) -> None:
+    if not (t.device == kv.pool.device and t.dtype == dtype and t.dim() == 2 and tuple(t.shape) == (rows, kv.n_kv_heads * kv.model.shape.head_dim)
+            and (t.stride(1) == 1 or rows == 0)):
+        raise ValueError("k and v: float32 or bfloat16 [rows][n_kv_heads * head_dim] on the caches' device, alike")
+
+
+def store(kvs, layer: int, k, v, n_rows: Optional[Sequence[int]] = None, pos0: Optional[Sequence[int]] = None, stream=None) -> None:
+    """anpd_kv_store: new rows' keys and values into one cache or a list of caches, rounded to their type or quantised.  k, v: CUDA
+    float32 or bfloat16 [rows of all sequences][n_kv_heads * head_dim]."""
+    import torch
+    if n_rows is None:      # the same number of each sequence
+        n = 1 if isinstance(kvs, KVCache) else len(kvs)
+        if n == 0 or k.shape[0] % n:
+            raise ValueError("n_rows is needed: %d rows do not divide among %d sequences" % (k.shape[0], n))
+        n_rows = [k.shape[0] // n] * n
+    kvs, n, handles, counts, at = _span_of(kvs, n_rows, pos0)
+    if k.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError("k and v must be float32 or bfloat16")
+    rows = sum(counts)
+    for t in (k, v):
+        _check_rows(t, rows, kvs[0], k.dtype)
+    _check(lib().anpd_kv_store(handles, n, counts, at, layer, k.data_ptr(), _pitch(k), v.data_ptr(), _pitch(v), F32 if k.dtype == torch.float32 else BF16,
+                               _stream_of(kvs[0].pool.device, stream)))
+
+
+def load(kvs, layer: int, n_rows: Sequence[int], pos0: Optional[Sequence[int]] = None, dtype=None, k=None, v=None, stream=None):
+    """anpd_kv_load: (k, v) of n_rows positions of each cache from its committed length (or pos0) on, in dtype (float32 if absent), into
+    k and v where given."""
+    import torch
+    kvs, n, handles, counts, at = _span_of(kvs, n_rows, pos0)
+    if dtype is None:
+        dtype = torch.float32 if k is None else k.dtype
+    if dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError("dtype must be float32 or bfloat16")
+    rows, first = sum(counts), kvs[0]
+    shape = (rows, first.n_kv_heads * first.model.shape.head_dim)
+    k, v = (_empty(shape, dtype, first.pool.device, stream) if t is None else t for t in (k, v))
+    for t in (k, v):
+        _check_rows(t, rows, first, dtype)
+    _check(lib().anpd_kv_load(handles, n, counts, at, layer, k.data_ptr(), _pitch(k), v.data_ptr(), _pitch(v), F32 if dtype == torch.float32 else BF16,
+                              _stream_of(first.pool.device, stream)))
+    return k, v
+
+
+# --------------------------------------------------------- drawing of tokens
+
+class SamplingRules:
+    """anpd_sample_rules: which tokens may be drawn.  A number for all rows, or a CUDA tensor with one for each (float32, top_k int32); keeps
+    its tensors alive."""
+
+    def __init__(self, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
+        import torch
+        self.struct, self.tensors = SampleRules(1.0, 0, 1.0, 0.0), {}
+        for name, value in (("temperature", temperature), ("top_k", top_k), ("top_p", top_p), ("min_p", min_p)):
+            if isinstance(value, torch.Tensor):
+                if not (value.is_cuda and value.is_contiguous() and value.dim() == 1 and value.dtype == (torch.int32 if name == "top_k" else torch.float32)):
+                    raise ValueError("%s: contiguous CUDA %s, one per row" % (name, "int32" if name == "top_k" else "float32"))
+                self.tensors[name] = value
+                setattr(self.struct, name + "s", value.data_ptr())
+            elif name == "top_k" and not 0 <= value < 1 << 31:      # (the struct would take its last 32 bits)
+                raise ValueError("top_k must be in 0..2^31 - 1")
+            else:
+                setattr(self.struct, name, value)
+        self.ref = C.addressof(self.struct)
+
+    def check(self, rows: int, device) -> None:
+        for name, t in self.tensors.items():
+            if t.numel() < rows or t.device != device:
+                raise ValueError("%s: one per row, on the logits' device" % name)
+
+
+def sample(logits, uniform, rules: Optional[SamplingRules] = None, tokens=None, logprob=None, want_logprob: bool = False, stream=None):
+    """anpd_sample: a token for each row of logits (CUDA float32 or bfloat16 [rows][vocab]) by random numbers in [0, 1) (float32 [rows]).
+    Returns int32 tokens, or (tokens, logprob) where logprob was given or asked for."""
+    import torch
+    if logits.dim() != 2 or not logits.is_cuda or logits.dtype not in (torch.float32, torch.bfloat16) or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        raise ValueError("logits must be a 2-d CUDA float32 or bfloat16 tensor, tokens side by side")
+    rows, device = logits.shape[0], logits.device
+    if not (uniform.device == device and uniform.dtype == torch.float32 and uniform.is_contiguous() and tuple(uniform.shape) == (rows,)):
+        raise ValueError("uniform: contiguous float32, one per row, on the logits' device")
+    if rules is not None:
+        rules.check(rows, device)
+    if tokens is None:
+        tokens = _empty((rows,), torch.int32, device, stream)
+    elif not (tokens.device == device and tokens.dtype == torch.int32 and tokens.is_contiguous() and tuple(tokens.shape) == (rows,)):
+        raise ValueError("tokens: contiguous int32, one per row")
+    if logprob is not None:
+        if not (logprob.device == device and logprob.dtype == torch.float32 and logprob.is_contiguous() and tuple(logprob.shape) == (rows,)):
+            raise ValueError("logprob: contiguous float32, one per row")
+    elif want_logprob:
+        logprob = _empty((rows,), torch.float32, device, stream)
+    _check(lib().anpd_sample(logits.data_ptr(), _pitch(logits), F32 if logits.dtype == torch.float32 else BF16, rows, logits.shape[1],
+                             None if rules is None else rules.ref, uniform.data_ptr(), tokens.data_ptr(), None if logprob is None else logprob.data_ptr(),
+                             _stream_of(device, stream)))
+    return tokens if logprob is None else (tokens, logprob)
+
+
+def verify_sample(model: Model, kv: KVCache, window: Sequence[int], uniform, rules: Optional[SamplingRules] = None, out_logits=None, stream=None):
+    """anpd_verify_sample: a verification step that draws its tokens.  uniform: CUDA float32, one per window row.  Returns
+    (accepted, next, tokens drawn after every row)."""
+    import torch
+    n = len(window)
+    device = kv.pool.device
+    if not (uniform.device == device and uniform.dtype == torch.float32 and uniform.is_contiguous() and tuple(uniform.shape) == (n,)):
+        raise ValueError("uniform: contiguous float32, one per window row, on the cache's device")
+    if rules is not None:
+        rules.check(n, device)
+    if out_logits is None:
+        out_logits = _empty((n, model.vocab), torch.float32, device, stream)
+    elif not (out_logits.device == device and out_logits.dtype == torch.float32 and out_logits.is_contiguous() and out_logits.numel() >= n * model.vocab):
+        raise ValueError("out_logits: contiguous float32 [window rows][vocab] on the cache's device")
+    acc, nxt, drawn = C.c_int32(0), C.c_int32(0), (C.c_int32 * max(1, n))()
+    _check(lib().anpd_verify_sample(model._h, kv._h, _ints(window), n, None if rules is None else rules.ref, uniform.data_ptr(), C.byref(acc), C.byref(nxt), drawn,
+                                    out_logits.data_ptr(), _stream_of(device, stream)))
+    return acc.value, nxt.value, list(drawn[:n])
 
 
 # ------------------------------------------------------------ decode loops
@@ -820,13 +994,24 @@ def anpd_generate_multi(model: Model, kv: KVCache, table: NgramTable, prompt: Se
 
 
 def anpd_generate(model: Model, kv: KVCache, table: NgramTable, prompt: Sequence[int], K: int, n_tokens: int,
-                  stream=None, drafter=None, adaptive: bool = False) -> Dict[str, object]:
+                  stream=None, drafter=None, adaptive: bool = False, sampling: Optional[SamplingRules] = None, generator=None) -> Dict[str, object]:
     """Algorithm 1: commit, draft K tokens from the table, verify, accept the
     matching prefix, continue from the LLM's own token.  ``adaptive`` cuts the
-    drafts of a step to adaptive_draft_length()."""
+    drafts of a step to adaptive_draft_length().  ``sampling``: tokens are drawn by these rules (numbers, not tensors per row) instead of
+    taken greedily, with random numbers from ``generator`` (torch, of the model's device; absent: its default one)."""
+    import torch
+    if sampling is not None and sampling.tensors:
+        raise ValueError("sampling: the same rules for all rows")
+    side = contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
     table.reset()
     table.update(prompt)
-    c = prefill(model, kv, prompt, stream)
+    if sampling is None:
+        c = prefill(model, kv, prompt, stream)
+    else:
+        with side:
+            logits = torch.empty(max(1, model.max_window), model.vocab, dtype=torch.float32, device=kv.pool.device)
+            prefill(model, kv, prompt, stream, out_logits=logits[0])
+            c = int(sample(logits[:1], torch.rand(1, generator=generator, device=kv.pool.device), sampling, stream=stream))
     out: List[int] = []
     steps = proposed = accepted = 0
     while len(out) < n_tokens:
@@ -838,7 +1023,12 @@ def anpd_generate(model: Model, kv: KVCache, table: NgramTable, prompt: Sequence
             drafts, levels = table.propose(K)
             if adaptive:
                 drafts = drafts[:adaptive_draft_length(levels, K)]
-        a, nxt = verify(model, kv, [c] + drafts, VERIFY, stream=stream)
+        if sampling is None:
+            a, nxt = verify(model, kv, [c] + drafts, VERIFY, stream=stream)
+        else:
+            with side:
+                a, nxt, _ = verify_sample(model, kv, [c] + drafts, torch.rand(1 + len(drafts), generator=generator, device=kv.pool.device), sampling,
+                                          out_logits=logits, stream=stream)
         if a:
             table.update(drafts[:a])
             out.extend(drafts[:a])

@@ -10,7 +10,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libanpd.so")
-SOURCES = ["anpd_device.hip", "anpd_operators.hip", "anpd_ngram.cpp"]
+SOURCES = ["anpd_device.hip", "anpd_operators.hip", "anpd_cache_rows.hip", "anpd_sample.hip", "anpd_ngram.cpp"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-Wall", "-Wno-unused-function", "-I", os.path.join(ROOT, "include"), "-I", CSRC]

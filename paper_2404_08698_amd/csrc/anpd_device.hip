@@ -1747,6 +1747,12 @@ static int32_t kv_copy(anpd_kv *kv, int32_t layer, int32_t pos0, int32_t n, floa
         for (int lp = pos0 / pt; lp <= (pos0 + n - 1) / pt; ++lp)
             if (kv->table[(size_t)lp] < 0) return fail(ANPD_E_INVAL, "anpd_kv_read: position %d has no page", lp * pt);
     }
+    if (c.dtype == ANPD_INT8) {
+        const int32_t rc = copy_rows8(kv, layer, pos0, n, k, v, to_cache, st);
+        if (rc != ANPD_OK) return rc;
+        HIP_TRY(hipStreamSynchronize(st));
+        return ANPD_OK;
+    }
 #define KV_COPY(KT, TO)                                                                                          \
     hipLaunchKernelGGL((kv_copy_kernel<KT, TO>), dim3(n), dim3(256), 0, st, (KT *)kv->pool, kv->d_table, k, v, pos0, \
                        layer, c.n_layers, c.n_kv_heads, c.head_dim, c.page_tokens)
@@ -1814,6 +1820,40 @@ int32_t anpd_verify(anpd_model_t *m, anpd_kv_t *kv, const int32_t *window, int32
     if (out_predicts) std::memcpy(out_predicts, res + 2, sizeof(int32_t) * (size_t)n_window);
     kv->len += 1 + res[0];
     release_pages(kv, kv->len);
+    return ANPD_OK;
+}
+
+int32_t anpd_verify_sample(anpd_model_t *m, anpd_kv_t *kv, const int32_t *window, int32_t n_window, const anpd_sample_rules *rules,
+                           const float *uniform, int32_t *out_accepted, int32_t *out_next, int32_t *out_tokens, float *logits, void *stream)
+{
+    if (!m || !kv || !window || !uniform || !out_accepted || !out_next || !logits) return fail(ANPD_E_INVAL, "anpd_verify_sample: NULL argument");
+    if ((((uintptr_t)uniform | (uintptr_t)logits) & 3) != 0) return fail(ANPD_E_INVAL, "anpd_verify_sample: an argument is not aligned to its type");
+    // (the rules, before anything is launched)
+    int32_t rc = anpd_sample(logits, m->cfg.vocab, ANPD_F32, 0, m->cfg.vocab, rules, uniform, nullptr, nullptr, stream);
+    if (rc != ANPD_OK) return rc;
+    const int32_t len0 = kv->len;
+    int32_t appended, next;
+    if ((rc = anpd_verify(m, kv, window, n_window, ANPD_APPEND, &appended, &next, nullptr, logits, stream)) != ANPD_OK) return rc;
+    // (the kernel stores the tokens where the step has left its argmaxes, in pinned memory)
+    hipStream_t st = (hipStream_t)stream;
+    const int32_t *drawn = m->pin + 34;
+    rc = anpd_sample(logits, m->cfg.vocab, ANPD_F32, n_window, m->cfg.vocab, rules, uniform, m->pin_dev + 34, nullptr, stream);
+    if (rc == ANPD_OK && hipStreamSynchronize(st) != hipSuccess) rc = fail(ANPD_E_HIP, "anpd_verify_sample: the draw failed");
+    int32_t a = 0;
+    if (rc == ANPD_OK) {
+        while (a + 1 < n_window && drawn[a] == window[a + 1]) ++a;
+        for (int i = 0; i <= a; ++i)
+            if (drawn[i] < 0) rc = fail(ANPD_E_RANGE, "anpd_verify_sample: row %d has no token to draw", i);
+    }
+    if (rc != ANPD_OK) {
+        (void)anpd_kv_truncate(kv, len0, stream);
+        return rc;
+    }
+    const int32_t first_next = drawn[a];
+    if (out_tokens) std::memcpy(out_tokens, drawn, sizeof(int32_t) * (size_t)n_window);
+    if (a + 1 < n_window && (rc = anpd_kv_truncate(kv, len0 + 1 + a, stream)) != ANPD_OK) return rc;
+    *out_accepted = a;
+    *out_next = first_next;
     return ANPD_OK;
 }
 

@@ -61,4 +61,22 @@ __host__ __device__ __forceinline__ size_t vf_elem(int tok, int dim)
     return ((size_t)(dim >> 4) * 64 + (size_t)(tok >> 2) * 16 + (dim & 15)) * 4 + (tok & 3);
 }
 
+// ------------------------------------------------------ caches of 8 bits
+//
+// Block of 16 tokens of a (page, layer, k|v, head): 16 x head_dim signed codes, then 16 fp32 scales; a value is code * scale.
+//   K: [dim / 32][(dim % 32) / 16][token][dim % 16]
+//   V: [dim / 64][half][dim % 64][key], half = (token / 4) % 2, key = token % 4 + 4 (token / 8)
+// A lane's 16 bytes are two operands of a 32x32x16 product: 16 dims of a key, or of two adjacent dims the eight keys whose weights its half of
+// the wave holds (tokens 4 half .. and 8 + 4 half ..).
+__host__ __device__ constexpr size_t kv8_block_bytes(int head_dim) { return (size_t)16 * head_dim + 64; }
+__host__ __device__ __forceinline__ size_t kv8_base(int page, int layer, int n_layers, int kv, int head, int n_heads, int head_dim)
+{
+    return ((((size_t)page * n_layers + layer) * 2 + kv) * n_heads + head) * kv8_block_bytes(head_dim);
+}
+__host__ __device__ __forceinline__ size_t k8_elem(int tok, int dim) { return (size_t)(dim >> 4) * 256 + tok * 16 + (dim & 15); }
+__host__ __device__ __forceinline__ size_t v8_elem(int tok, int dim)
+{
+    return (size_t)(dim >> 6) * 1024 + ((tok >> 2) & 1) * 512 + (dim & 63) * 8 + (tok & 3) + 4 * (tok >> 3);
+}
+
 }  // namespace anpd

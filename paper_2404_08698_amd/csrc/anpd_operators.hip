@@ -7,40 +7,16 @@
 
 #include "anpd_cache.h"
 #include "anpd_cache_attn.h"
+#include "anpd_cache_attn8.h"
 #include "anpd_cache_evict.h"
 
 using namespace anpd;
 
 namespace {
 
-// The caches' device is the current one while a call lasts.
-struct OnDevice {
-    int before = -1;
-    int32_t enter(const char *who, int device)
-    {
-        int cur = 0;
-        hipError_t e = hipGetDevice(&cur);
-        if (e == hipSuccess && cur != device) {
-            e = hipSetDevice(device);
-            if (e == hipSuccess) before = cur;
-        }
-        return e == hipSuccess ? ANPD_OK : fail(ANPD_E_HIP, "%s: %s", who, hipGetErrorString(e));
-    }
-    ~OnDevice()
-    {
-        if (before >= 0) (void)hipSetDevice(before);
-    }
-};
-
-bool same_shape(const CacheShape &a, const CacheShape &b)
-{
-    return a.n_layers == b.n_layers && a.n_heads == b.n_heads && a.n_kv_heads == b.n_kv_heads && a.head_dim == b.head_dim && a.dtype == b.dtype &&
-           a.page_tokens == b.page_tokens && a.fragments == b.fragments;
-}
-
 // What anpd_attention and anpd_key_mass have in common: the sequences and rules, checked, as the kernels take them.
-int32_t gather(const char *who, const anpd_kv *const *kvs, int32_t n_seq, const int32_t *n_rows, const int32_t *pos0, const anpd_attn_rules *rules,
-               AttnArgs &a, int64_t &rows)
+int32_t gather(const char *who, const anpd_kv *const *kvs, int32_t n_seq, const int32_t *n_rows, const int32_t *pos0, const int32_t *parent,
+               const anpd_attn_rules *rules, AttnArgs &a, int64_t &rows)
 {
     if (!kvs || !n_rows) return fail(ANPD_E_INVAL, "%s: NULL argument", who);
     if (n_seq < 1 || n_seq > kAttnMaxSeqs) return fail(ANPD_E_INVAL, "%s: n_seq must be in 1..%d", who, kAttnMaxSeqs);
@@ -55,10 +31,11 @@ int32_t gather(const char *who, const anpd_kv *const *kvs, int32_t n_seq, const 
     a.group = c.n_heads / c.n_kv_heads;
     a.page_tokens = c.page_tokens;
     a.scale = 1.0f / std::sqrt((float)c.head_dim);
+    a.parent = parent;
     rows = 0;
     for (int s = 0; s < n_seq; ++s) {
         const anpd_kv *kv = kvs[s];
-        if (!same_shape(kv->shape, c) || kv->device != kvs[0]->device) return fail(ANPD_E_INVAL, "%s: cache %d has another shape or device than the first", who, s);
+        if (!(kv->shape == c) || kv->device != kvs[0]->device) return fail(ANPD_E_INVAL, "%s: cache %d has another shape or device than the first", who, s);
         const int32_t n = n_rows[s], at = pos0 ? pos0[s] : kv->len;
         if (n < 0 || at < 0) return fail(ANPD_E_INVAL, "%s: sequence %d: %d rows from position %d on", who, s, n, at);
         if ((int64_t)at + n > kv->max_tokens)
@@ -67,6 +44,7 @@ int32_t gather(const char *who, const anpd_kv *const *kvs, int32_t n_seq, const 
         if (n > 0 && kv->table[(size_t)((at + n - 1) / c.page_tokens)] < 0)
             return fail(ANPD_E_INVAL, "%s: sequence %d: position %d has no page", who, s, at + n - 1);
         if ((int64_t)n * a.group >= (1 << 30)) return fail(ANPD_E_CAPACITY, "%s: sequence %d has too many rows", who, s);
+        if (parent && n > kTreeRows) return fail(ANPD_E_CAPACITY, "%s: sequence %d: a tree of %d rows, %d at most", who, s, n, kTreeRows);
         a.seq[s] = {kv->pool, kv->d_table, at, n, (int32_t)rows, 0};
         rows += n;
     }
@@ -117,13 +95,13 @@ struct Plan {
 void count_tiles(const AttnArgs &a, const SeqView &v, int row_block, int key_tile, int64_t &blocks, int64_t &tiles, int &most)
 {
     const int64_t rows = (int64_t)v.n * a.group;
-    const int total = v.pos0 + v.n, span = row_block / a.group;
+    const int total = v.pos0 + v.n, span = a.parent ? v.n : row_block / a.group;
     blocks = (rows + row_block - 1) / row_block;
     const int64_t samples = blocks < 2 ? blocks : (a.window > 0 && blocks > 2 ? (blocks < 8 ? blocks : 8) : 2);
     tiles = 0;
     for (int64_t i = 0; i < samples; ++i) {
         const int64_t from = (samples > 1 ? (blocks - 1) * i / (samples - 1) : 0) * row_block, to = from + row_block < rows ? from + row_block : rows;
-        tiles += key_tiles(v.pos0 + (int)(from / a.group), v.pos0 + (int)((to - 1) / a.group), total, a.window, a.prefix, key_tile).n;
+        tiles += key_tiles(a, v, v.pos0 + (int)(from / a.group), v.pos0 + (int)((to - 1) / a.group), key_tile).n;
     }
     tiles = blocks * tiles / samples;
     // (a window's tiles depend on where it begins inside the first one)
@@ -175,7 +153,7 @@ Plan plan_attention(AttnArgs &a, const CacheShape &c, int n_cu)
     if (splits > 1) shared_us += 6.0 + (double)rows * c.n_heads * splits * c.head_dim * 4 / 4.5e6;
     if (a.window > 0) shared_us += (a.q_f32 ? 2.5 : 1.6) * (shared_rows / a.group / 32.0 + 1.0);
     if (a.first_key) shared_us *= 1.4;
-    p.shared = c.fragments && !(a.cap > 0.f || a.slopes) && !(a.q_f32 && a.first_key) && shared_us < (a.q_f32 ? 1.7 : 0.95) * (double)tiles[0] / n_cu + 4.0;
+    p.shared = c.fragments && !a.parent && !(a.cap > 0.f || a.slopes) && !(a.q_f32 && a.first_key) && shared_us < (a.q_f32 ? 1.7 : 0.95) * (double)tiles[0] / n_cu + 4.0;
     p.row_block = p.shared ? shared_rows : kRowTile;
     p.key_tile = p.shared ? kTileKeys : kStreamTile;
     a.n_blocks = 0;
@@ -214,30 +192,37 @@ size_t attention_part_bytes(AttnArgs a, const CacheShape &c, int n_cu)
     return need;
 }
 
-template <int DH, int TERMS, bool RULES>
+template <int DH, int TERMS, int RULES>
 int32_t launch_fragments(const AttnArgs &a, const Plan &p, hipStream_t st)
 {
     const dim3 grid((unsigned)((int64_t)a.n_blocks * a.n_splits * a.n_kv_heads));
-    if (p.shared) {
+    if constexpr (RULES != kTree) if (p.shared) {
         constexpr size_t lds = tile_lds_bytes(DH);
         // (at every call: the attribute is the current device's)
         if (lds > 65536) HIP_TRY(hipFuncSetAttribute((const void *)cache_attn_tile_kernel<DH, TERMS, RULES>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
         hipLaunchKernelGGL((cache_attn_tile_kernel<DH, TERMS, RULES>), grid, dim3(tile_waves(TERMS) * 64), lds, st, a);
-    } else hipLaunchKernelGGL((cache_attn_stream_kernel<DH, TERMS, RULES>), grid, dim3(256), 0, st, a);
+        return ANPD_OK;
+    }
+    hipLaunchKernelGGL((cache_attn_stream_kernel<DH, TERMS, RULES>), grid, dim3(256), 0, st, a);
     return ANPD_OK;
 }
 template <int DH>
 int32_t launch_attention(const AttnArgs &a, const Plan &p, const CacheShape &c, hipStream_t st)
 {
-    const bool rules = ruled(a);
+    const Seen rules = a.parent ? kTree : ruled(a) ? kRuled : kCausal;
     if (c.fragments) {
-        const int32_t rc = a.q_f32 ? (rules ? launch_fragments<DH, 3, true>(a, p, st) : launch_fragments<DH, 3, false>(a, p, st))
-                                   : (rules ? launch_fragments<DH, 1, true>(a, p, st) : launch_fragments<DH, 1, false>(a, p, st));
+#define ANPD_ATTEND(RULES) (a.q_f32 ? launch_fragments<DH, 3, RULES>(a, p, st) : launch_fragments<DH, 1, RULES>(a, p, st))
+        const int32_t rc = rules == kTree ? ANPD_ATTEND(kTree) : rules == kRuled ? ANPD_ATTEND(kRuled) : ANPD_ATTEND(kCausal);
+#undef ANPD_ATTEND
         if (rc != ANPD_OK) return rc;
-    } else {
+    } else if (c.dtype == ANPD_INT8) launch_attention8(a, rules, c.head_dim, st);
+    else {
         const dim3 grid((unsigned)((int64_t)a.n_blocks * a.n_splits * a.n_kv_heads));
-        if (c.dtype == ANPD_BF16) hipLaunchKernelGGL((cache_attn_plain_kernel<bf16_t, DH>), grid, dim3(256), 0, st, a);
-        else hipLaunchKernelGGL((cache_attn_plain_kernel<float, DH>), grid, dim3(256), 0, st, a);
+#define ANPD_ATTEND(KT) \
+    if (rules == kTree) hipLaunchKernelGGL((cache_attn_plain_kernel<KT, DH, kTree>), grid, dim3(256), 0, st, a); \
+    else hipLaunchKernelGGL((cache_attn_plain_kernel<KT, DH, kRuled>), grid, dim3(256), 0, st, a)
+        if (c.dtype == ANPD_BF16) { ANPD_ATTEND(bf16_t); } else { ANPD_ATTEND(float); }
+#undef ANPD_ATTEND
     }
     HIP_TRY(hipGetLastError());
     if (a.part) {
@@ -347,7 +332,8 @@ bool cache_cfg_ok(const char *who, const anpd_cache_cfg *c, int32_t max_tokens, 
     REQ(c->n_kv_heads >= 0 && (c->n_kv_heads == 0 || c->n_heads % c->n_kv_heads == 0), "n_kv_heads must be 0 or divide n_heads");
     REQ(c->n_heads <= (1 << 16) && c->n_layers <= (1 << 16), "more than 2^16 heads or layers");
     REQ(c->head_dim == 64 || c->head_dim == 128, "head_dim must be 64 or 128");
-    REQ(c->dtype == ANPD_F32 || c->dtype == ANPD_BF16, "dtype must be ANPD_F32 or ANPD_BF16");
+    REQ(c->dtype == ANPD_F32 || c->dtype == ANPD_BF16 || c->dtype == ANPD_INT8, "dtype must be ANPD_F32, ANPD_BF16 or ANPD_INT8");
+    REQ(c->dtype != ANPD_INT8 || c->page_tokens == 16, "page_tokens must be 16 for ANPD_INT8");
     REQ(c->page_tokens >= 8 && c->page_tokens <= 256 && (c->page_tokens & (c->page_tokens - 1)) == 0, "page_tokens must be a power of two in 8..256");
     REQ(max_tokens >= 1 && max_tokens <= (1 << 20), "max_tokens must be in 1..2^20");
 #undef REQ
@@ -380,6 +366,42 @@ ObserveLayout observe_layout(const CacheShape &c, int max_tokens, int rows, int 
     L.work = take(L.work_bytes);
     L.total = o;
     return L;
+}
+
+// anpd_attention and anpd_tree_attention (parent: the new rows are trees).
+size_t attention_workspace(const char *who, const anpd_kv *const *kvs, int32_t n_seq, const int32_t *n_rows, const int32_t *pos0, const int32_t *parent,
+                           const anpd_attn_rules *rules)
+{
+    AttnArgs a;
+    int64_t rows;
+    if (gather(who, kvs, n_seq, n_rows, pos0, parent, rules, a, rows) != ANPD_OK) return 0;
+    return attention_part_bytes(a, kvs[0]->shape, kvs[0]->n_cu);
+}
+
+int32_t attend(const char *who, const anpd_kv *const *kvs, int32_t n_seq, const int32_t *n_rows, const int32_t *pos0, int32_t layer, const void *q, int64_t ldq,
+               int32_t dtype, const int32_t *parent, const anpd_attn_rules *rules, void *out, int64_t ldo, float *lse, void *workspace, size_t workspace_bytes,
+               void *stream)
+{
+    AttnArgs a;
+    int64_t rows;
+    int32_t rc = gather(who, kvs, n_seq, n_rows, pos0, parent, rules, a, rows);
+    if (rc != ANPD_OK) return rc;
+    const CacheShape &c = kvs[0]->shape;
+    if ((rc = rows_in(who, c, layer, q, ldq, dtype, a)) != ANPD_OK) return rc;
+    if (ldo < (int64_t)c.n_heads * c.head_dim) return fail(ANPD_E_INVAL, "%s: ldo %lld is less than a row", who, (long long)ldo);
+    if (rows == 0) return ANPD_OK;
+    if (!q || !out) return fail(ANPD_E_INVAL, "%s: NULL rows", who);
+    if (((uintptr_t)lse & 3) != 0) return fail(ANPD_E_INVAL, "%s: lse is not aligned to its type", who);
+    if (((uintptr_t)out & (a.q_f32 ? 3 : 1)) != 0) return fail(ANPD_E_INVAL, "%s: out is not aligned to its type", who);
+    a.out = out;
+    a.ldo = ldo;
+    a.lse = lse;
+    a.q_wide = a.q_wide && ((uintptr_t)out & 15) == 0 && ldo % (a.q_f32 ? 4 : 8) == 0;
+    const Plan p = plan_attention(a, c, kvs[0]->n_cu);
+    if ((rc = workspace_of(who, a, p.part_bytes, workspace, workspace_bytes)) != ANPD_OK) return rc;
+    OnDevice on;
+    if ((rc = on.enter(who, kvs[0]->device)) != ANPD_OK) return rc;
+    return c.head_dim == 128 ? launch_attention<128>(a, p, c, (hipStream_t)stream) : launch_attention<64>(a, p, c, (hipStream_t)stream);
 }
 
 }  // namespace
@@ -423,43 +445,36 @@ int32_t anpd_cache_create(const anpd_cache_cfg *cfg, void *pool, size_t pool_byt
 
 size_t anpd_attention_workspace_bytes(const anpd_kv_t *const *kvs, int32_t n_seq, const int32_t *n_rows, const int32_t *pos0, const anpd_attn_rules *rules)
 {
-    AttnArgs a;
-    int64_t rows;
-    if (gather("anpd_attention_workspace_bytes", kvs, n_seq, n_rows, pos0, rules, a, rows) != ANPD_OK) return 0;
-    return attention_part_bytes(a, kvs[0]->shape, kvs[0]->n_cu);
+    return attention_workspace("anpd_attention_workspace_bytes", kvs, n_seq, n_rows, pos0, nullptr, rules);
 }
 
 int32_t anpd_attention(const anpd_kv_t *const *kvs, int32_t n_seq, const int32_t *n_rows, const int32_t *pos0, int32_t layer, const void *q, int64_t ldq,
                        int32_t dtype, const anpd_attn_rules *rules, void *out, int64_t ldo, float *lse, void *workspace, size_t workspace_bytes, void *stream)
 {
-    const char *who = "anpd_attention";
-    AttnArgs a;
-    int64_t rows;
-    int32_t rc = gather(who, kvs, n_seq, n_rows, pos0, rules, a, rows);
-    if (rc != ANPD_OK) return rc;
-    const CacheShape &c = kvs[0]->shape;
-    if ((rc = rows_in(who, c, layer, q, ldq, dtype, a)) != ANPD_OK) return rc;
-    if (ldo < (int64_t)c.n_heads * c.head_dim) return fail(ANPD_E_INVAL, "%s: ldo %lld is less than a row", who, (long long)ldo);
-    if (rows == 0) return ANPD_OK;
-    if (!q || !out) return fail(ANPD_E_INVAL, "%s: NULL rows", who);
-    if (((uintptr_t)lse & 3) != 0) return fail(ANPD_E_INVAL, "%s: lse is not aligned to its type", who);
-    if (((uintptr_t)out & (a.q_f32 ? 3 : 1)) != 0) return fail(ANPD_E_INVAL, "%s: out is not aligned to its type", who);
-    a.out = out;
-    a.ldo = ldo;
-    a.lse = lse;
-    a.q_wide = a.q_wide && ((uintptr_t)out & 15) == 0 && ldo % (a.q_f32 ? 4 : 8) == 0;
-    const Plan p = plan_attention(a, c, kvs[0]->n_cu);
-    if ((rc = workspace_of(who, a, p.part_bytes, workspace, workspace_bytes)) != ANPD_OK) return rc;
-    OnDevice on;
-    if ((rc = on.enter(who, kvs[0]->device)) != ANPD_OK) return rc;
-    return c.head_dim == 128 ? launch_attention<128>(a, p, c, (hipStream_t)stream) : launch_attention<64>(a, p, c, (hipStream_t)stream);
+    return attend("anpd_attention", kvs, n_seq, n_rows, pos0, layer, q, ldq, dtype, nullptr, rules, out, ldo, lse, workspace, workspace_bytes, stream);
+}
+
+size_t anpd_tree_attention_workspace_bytes(const anpd_kv_t *const *kvs, int32_t n_seq, const int32_t *n_rows, const int32_t *pos0, const anpd_attn_rules *rules)
+{
+    static const int32_t some = -1;   // (a tree; which one is not looked at)
+    return attention_workspace("anpd_tree_attention_workspace_bytes", kvs, n_seq, n_rows, pos0, &some, rules);
+}
+
+int32_t anpd_tree_attention(const anpd_kv_t *const *kvs, int32_t n_seq, const int32_t *n_rows, const int32_t *pos0, int32_t layer, const void *q, int64_t ldq,
+                            int32_t dtype, const int32_t *parent, const anpd_attn_rules *rules, void *out, int64_t ldo, float *lse, void *workspace,
+                            size_t workspace_bytes, void *stream)
+{
+    const char *who = "anpd_tree_attention";
+    if (!parent) return fail(ANPD_E_INVAL, "%s: NULL parent", who);
+    if (((uintptr_t)parent & 3) != 0) return fail(ANPD_E_INVAL, "%s: parent is not aligned to its type", who);
+    return attend(who, kvs, n_seq, n_rows, pos0, layer, q, ldq, dtype, parent, rules, out, ldo, lse, workspace, workspace_bytes, stream);
 }
 
 size_t anpd_key_mass_workspace_bytes(const anpd_kv_t *const *kvs, int32_t n_seq, const int32_t *n_rows, const int32_t *pos0, const anpd_attn_rules *rules)
 {
     AttnArgs a;
     int64_t rows;
-    if (gather("anpd_key_mass_workspace_bytes", kvs, n_seq, n_rows, pos0, rules, a, rows) != ANPD_OK) return 0;
+    if (gather("anpd_key_mass_workspace_bytes", kvs, n_seq, n_rows, pos0, nullptr, rules, a, rows) != ANPD_OK) return 0;
     int sets;
     return plan_mass(a, kvs[0]->shape, kvs[0]->n_cu, sets);
 }
@@ -471,9 +486,10 @@ int32_t anpd_key_mass(const anpd_kv_t *const *kvs, int32_t n_seq, const int32_t 
     const char *who = "anpd_key_mass";
     AttnArgs a;
     int64_t rows;
-    int32_t rc = gather(who, kvs, n_seq, n_rows, pos0, rules, a, rows);
+    int32_t rc = gather(who, kvs, n_seq, n_rows, pos0, nullptr, rules, a, rows);
     if (rc != ANPD_OK) return rc;
     const CacheShape &c = kvs[0]->shape;
+    if (c.dtype == ANPD_INT8) return fail(ANPD_E_UNIMPLEMENTED, "%s: caches of 8 bits are not taken", who);
     if ((rc = rows_in(who, c, layer, q, ldq, dtype, a)) != ANPD_OK) return rc;
     if (rows == 0) return ANPD_OK;
     if (!q || !lse || !mass) return fail(ANPD_E_INVAL, "%s: NULL argument", who);
@@ -540,7 +556,8 @@ int32_t anpd_kv_evict(const anpd_kv_t *src, anpd_kv_t *dst, const float *mass, i
     const char *who = "anpd_kv_evict";
     if (!src || !dst) return fail(ANPD_E_INVAL, "%s: NULL cache", who);
     const CacheShape &c = src->shape;
-    if (!same_shape(c, dst->shape) || src->device != dst->device) return fail(ANPD_E_INVAL, "%s: the caches have different shapes or devices", who);
+    if (!(c == dst->shape) || src->device != dst->device) return fail(ANPD_E_INVAL, "%s: the caches have different shapes or devices", who);
+    if (c.dtype == ANPD_INT8) return fail(ANPD_E_UNIMPLEMENTED, "%s: caches of 8 bits are not taken", who);
     const int len = src->len;
     if (first < 0 || last < 0 || keep < 0 || (int64_t)first + last > keep) return fail(ANPD_E_INVAL, "%s: need 0 <= first + last <= keep", who);
     if (keep > len || keep > dst->max_tokens) return fail(ANPD_E_CAPACITY, "%s: %d positions of %d, into a cache of %d", who, keep, len, dst->max_tokens);
