@@ -518,19 +518,24 @@ typedef struct {
  *   out_token: DEVICE, rows ints: the lowest index i at which the weights of the tokens that remain, added up by index, exceed uniform times
  *     their sum; -1 where a row holds no token at all.
  *   out_logprob (nullable, DEVICE, rows floats): the logarithm of the probability with which it is drawn (temperature 0: 0; no token: NaN).
- * Weights are formed in 64 bits and held as multiples of 2^-51 of the largest (2^-43 for vocabularies near 2^20), whose sums are exact: the same inputs give the same tokens.
+ *   workspace: DEVICE, 256-byte aligned, >= anpd_sample_workspace_bytes() (0 for vocabularies of up to 8192, then it may be NULL), used during the
+ *   call only: calls that may overlap need one each, replays of captured calls included.
+ * Weights are formed in 64 bits and held as multiples of 2^-51 of the largest (2^-42 for vocabularies near 2^20): the same inputs give the same tokens.
  * Asynchronous on stream; may be captured.  Errors: ANPD_E_INVAL, ANPD_E_HIP. */
+size_t anpd_sample_workspace_bytes(int32_t rows, int32_t vocab);
 int32_t anpd_sample(const void *logits, int64_t ld, int32_t dtype, int32_t rows, int32_t vocab, const anpd_sample_rules *rules, const float *uniform,
-                    int32_t *out_token, float *out_logprob, void *stream);
+                    int32_t *out_token, float *out_logprob, void *workspace, size_t workspace_bytes, void *stream);
 
 /* One verification step that draws instead of taking the argmax.  The drafts of a table are certain, not drawn, so a token is drawn after every row,
  * and draft j is accepted while it is the token drawn after row j - 1; the first that is not is the next token.  What is
  * generated is distributed as if every token had been drawn by itself.
  *   Arguments as in anpd_verify (ANPD_VERIFY).  uniform: DEVICE, n_window floats.  logits: DEVICE, n_window * vocab floats, written.
+ *   workspace: as in anpd_sample, for n_window rows.
  *   out_tokens (nullable, host, n_window ints): the token drawn after every row.
  * Errors as anpd_verify and anpd_sample; ANPD_E_RANGE if a row has no token (all NaN): nothing is committed. */
 int32_t anpd_verify_sample(anpd_model_t *m, anpd_kv_t *kv, const int32_t *window, int32_t n_window, const anpd_sample_rules *rules,
-                           const float *uniform, int32_t *out_accepted, int32_t *out_next, int32_t *out_tokens, float *logits, void *stream);
+                           const float *uniform, int32_t *out_accepted, int32_t *out_next, int32_t *out_tokens, float *logits, void *workspace,
+                           size_t workspace_bytes, void *stream);
 
 #ifdef __cplusplus
 }

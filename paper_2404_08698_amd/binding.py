@@ -39,7 +39,7 @@ EXPORTS = (
     "anpd_key_mass_workspace_bytes", "anpd_key_mass", "anpd_kv_evict",
     "anpd_kv_observe_workspace_bytes", "anpd_kv_observe",
     "anpd_kv_store", "anpd_kv_load", "anpd_tree_attention_workspace_bytes", "anpd_tree_attention", "anpd_kv_commit",
-    "anpd_sample", "anpd_verify_sample",
+    "anpd_sample_workspace_bytes", "anpd_sample", "anpd_verify_sample",
 )
 PROF_CATEGORIES = ("gemm_qkv", "gemm_o", "gemm_gate_up", "gemm_down", "gemm_lm_head", "attn", "other", "step")
 
@@ -197,10 +197,12 @@ def lib():
     L.anpd_tree_attention.argtypes = seqs + [C.c_int32, vp, C.c_int64, C.c_int32, vp, vp, vp, C.c_int64, vp, vp, C.c_size_t, vp]
     L.anpd_kv_commit.restype = C.c_int32
     L.anpd_kv_commit.argtypes = [vp, i32p, C.c_int32, vp]
+    L.anpd_sample_workspace_bytes.restype = C.c_size_t
+    L.anpd_sample_workspace_bytes.argtypes = [C.c_int32, C.c_int32]
     L.anpd_sample.restype = C.c_int32
-    L.anpd_sample.argtypes = [vp, C.c_int64, C.c_int32, C.c_int32, C.c_int32, vp, vp, vp, vp, vp]
+    L.anpd_sample.argtypes = [vp, C.c_int64, C.c_int32, C.c_int32, C.c_int32, vp, vp, vp, vp, vp, C.c_size_t, vp]
     L.anpd_verify_sample.restype = C.c_int32
-    L.anpd_verify_sample.argtypes = [vp, vp, i32p, C.c_int32, vp, vp, i32p, i32p, i32p, vp, vp]
+    L.anpd_verify_sample.argtypes = [vp, vp, i32p, C.c_int32, vp, vp, i32p, i32p, i32p, vp, vp, C.c_size_t, vp]
     _lib = L
     return L
 
@@ -865,7 +867,25 @@ class SamplingRules:
                 raise ValueError("%s: one per row, on the logits' device" % name)
 
 
-def sample(logits, uniform, rules: Optional[SamplingRules] = None, tokens=None, logprob=None, want_logprob: bool = False, stream=None):
+def sample_workspace_bytes(rows: int, vocab: int) -> int:
+    """anpd_sample_workspace_bytes (0: none is needed)."""
+    return int(lib().anpd_sample_workspace_bytes(rows, vocab))
+
+
+def _sample_workspace(workspace, rows: int, vocab: int, device, stream):
+    """(kept alive, pointer, bytes) of the given workspace, or of one from the call's stream's memory."""
+    if workspace is None:
+        nbytes = sample_workspace_bytes(rows, vocab) if vocab > 8192 else 0
+        if nbytes == 0:
+            return None, None, 0
+        import torch
+        workspace = _empty(nbytes, torch.uint8, device, stream)
+    elif workspace.device != device or not workspace.is_contiguous():
+        raise ValueError("workspace: contiguous, on the logits' device")
+    return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def sample(logits, uniform, rules: Optional[SamplingRules] = None, tokens=None, logprob=None, want_logprob: bool = False, workspace=None, stream=None):
     """anpd_sample: a token for each row of logits (CUDA float32 or bfloat16 [rows][vocab]) by random numbers in [0, 1) (float32 [rows]).
     Returns int32 tokens, or (tokens, logprob) where logprob was given or asked for."""
     import torch
@@ -885,13 +905,15 @@ def sample(logits, uniform, rules: Optional[SamplingRules] = None, tokens=None, 
             raise ValueError("logprob: contiguous float32, one per row")
     elif want_logprob:
         logprob = _empty((rows,), torch.float32, device, stream)
+    _keep, at, nbytes = _sample_workspace(workspace, rows, logits.shape[1], device, stream)
     _check(lib().anpd_sample(logits.data_ptr(), _pitch(logits), F32 if logits.dtype == torch.float32 else BF16, rows, logits.shape[1],
                              None if rules is None else rules.ref, uniform.data_ptr(), tokens.data_ptr(), None if logprob is None else logprob.data_ptr(),
-                             _stream_of(device, stream)))
+                             at, nbytes, _stream_of(device, stream)))
     return tokens if logprob is None else (tokens, logprob)
 
 
-def verify_sample(model: Model, kv: KVCache, window: Sequence[int], uniform, rules: Optional[SamplingRules] = None, out_logits=None, stream=None):
+def verify_sample(model: Model, kv: KVCache, window: Sequence[int], uniform, rules: Optional[SamplingRules] = None, out_logits=None, workspace=None,
+                  stream=None):
     """anpd_verify_sample: a verification step that draws its tokens.  uniform: CUDA float32, one per window row.  Returns
     (accepted, next, tokens drawn after every row)."""
     import torch
@@ -905,9 +927,10 @@ def verify_sample(model: Model, kv: KVCache, window: Sequence[int], uniform, rul
         out_logits = _empty((n, model.vocab), torch.float32, device, stream)
     elif not (out_logits.device == device and out_logits.dtype == torch.float32 and out_logits.is_contiguous() and out_logits.numel() >= n * model.vocab):
         raise ValueError("out_logits: contiguous float32 [window rows][vocab] on the cache's device")
+    _keep, at, nbytes = _sample_workspace(workspace, n, model.vocab, device, stream)
     acc, nxt, drawn = C.c_int32(0), C.c_int32(0), (C.c_int32 * max(1, n))()
     _check(lib().anpd_verify_sample(model._h, kv._h, _ints(window), n, None if rules is None else rules.ref, uniform.data_ptr(), C.byref(acc), C.byref(nxt), drawn,
-                                    out_logits.data_ptr(), _stream_of(device, stream)))
+                                    out_logits.data_ptr(), at, nbytes, _stream_of(device, stream)))
     return acc.value, nxt.value, list(drawn[:n])
 
 

@@ -1824,20 +1824,24 @@ int32_t anpd_verify(anpd_model_t *m, anpd_kv_t *kv, const int32_t *window, int32
 }
 
 int32_t anpd_verify_sample(anpd_model_t *m, anpd_kv_t *kv, const int32_t *window, int32_t n_window, const anpd_sample_rules *rules,
-                           const float *uniform, int32_t *out_accepted, int32_t *out_next, int32_t *out_tokens, float *logits, void *stream)
+                           const float *uniform, int32_t *out_accepted, int32_t *out_next, int32_t *out_tokens, float *logits, void *workspace,
+                           size_t workspace_bytes, void *stream)
 {
     if (!m || !kv || !window || !uniform || !out_accepted || !out_next || !logits) return fail(ANPD_E_INVAL, "anpd_verify_sample: NULL argument");
     if ((((uintptr_t)uniform | (uintptr_t)logits) & 3) != 0) return fail(ANPD_E_INVAL, "anpd_verify_sample: an argument is not aligned to its type");
     // (the rules, before anything is launched)
-    int32_t rc = anpd_sample(logits, m->cfg.vocab, ANPD_F32, 0, m->cfg.vocab, rules, uniform, nullptr, nullptr, stream);
+    int32_t rc = anpd_sample(logits, m->cfg.vocab, ANPD_F32, 0, m->cfg.vocab, rules, uniform, nullptr, nullptr, nullptr, 0, stream);
     if (rc != ANPD_OK) return rc;
+    const size_t need = n_window > 0 ? anpd_sample_workspace_bytes(n_window, m->cfg.vocab) : 0;
+    if (need > 0 && (!workspace || ((uintptr_t)workspace & 255) != 0)) return fail(ANPD_E_INVAL, "anpd_verify_sample: workspace must be a 256-byte aligned device buffer");
+    if (workspace_bytes < need) return fail(ANPD_E_CAPACITY, "anpd_verify_sample: workspace has %zu bytes, %zu needed", workspace_bytes, need);
     const int32_t len0 = kv->len;
     int32_t appended, next;
     if ((rc = anpd_verify(m, kv, window, n_window, ANPD_APPEND, &appended, &next, nullptr, logits, stream)) != ANPD_OK) return rc;
     // (the kernel stores the tokens where the step has left its argmaxes, in pinned memory)
     hipStream_t st = (hipStream_t)stream;
     const int32_t *drawn = m->pin + 34;
-    rc = anpd_sample(logits, m->cfg.vocab, ANPD_F32, n_window, m->cfg.vocab, rules, uniform, m->pin_dev + 34, nullptr, stream);
+    rc = anpd_sample(logits, m->cfg.vocab, ANPD_F32, n_window, m->cfg.vocab, rules, uniform, m->pin_dev + 34, nullptr, workspace, workspace_bytes, stream);
     if (rc == ANPD_OK && hipStreamSynchronize(st) != hipSuccess) rc = fail(ANPD_E_HIP, "anpd_verify_sample: the draw failed");
     int32_t a = 0;
     if (rc == ANPD_OK) {

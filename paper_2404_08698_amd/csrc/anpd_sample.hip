@@ -9,10 +9,42 @@
 
 using namespace anpd;
 
+namespace {
+
+constexpr int kGroup = 256;   // rows of a launch, whose slices the workspace holds
+
+template <bool FUSED>
+void launch_rows(const SampleArgs &a, unsigned rows, hipStream_t st)
+{
+    if (a.f32) hipLaunchKernelGGL((sample_rows_kernel<float, FUSED>), dim3(rows), dim3(kRowThreads), 0, st, a);
+    else hipLaunchKernelGGL((sample_rows_kernel<bf16_t, FUSED>), dim3(rows), dim3(kRowThreads), 0, st, a);
+}
+template <int THREADS>
+void launch_slices(const SampleArgs &a, unsigned rows, hipStream_t st)
+{
+    const dim3 grid((unsigned)a.n_slices, rows);
+    if (a.f32) hipLaunchKernelGGL((sample_slices_kernel<float, THREADS>), grid, dim3(THREADS), 0, st, a);
+    else hipLaunchKernelGGL((sample_slices_kernel<bf16_t, THREADS>), grid, dim3(THREADS), 0, st, a);
+}
+
+int slices_of(int32_t vocab) { return ((vocab - 1) >> slice_shift(vocab)) + 1; }
+
+}  // namespace
+
 extern "C" {
 
+size_t anpd_sample_workspace_bytes(int32_t rows, int32_t vocab)
+{
+    if (rows < 0 || vocab < 1 || vocab > kSampleMaxVocab) {
+        fail(ANPD_E_INVAL, "anpd_sample_workspace_bytes: rows must be >= 0, vocab in 1..%d", kSampleMaxVocab);
+        return 0;
+    }
+    const int n = slices_of(vocab);
+    return n <= kFusedSlices ? 0 : align_up((size_t)(rows < kGroup ? rows : kGroup) * n * sizeof(Slice));
+}
+
 int32_t anpd_sample(const void *logits, int64_t ld, int32_t dtype, int32_t rows, int32_t vocab, const anpd_sample_rules *rules, const float *uniform,
-                    int32_t *out_token, float *out_logprob, void *stream)
+                    int32_t *out_token, float *out_logprob, void *workspace, size_t workspace_bytes, void *stream)
 {
     const char *who = "anpd_sample";
     if (dtype != ANPD_F32 && dtype != ANPD_BF16) return fail(ANPD_E_INVAL, "%s: unknown dtype", who);
@@ -46,21 +78,46 @@ int32_t anpd_sample(const void *logits, int64_t ld, int32_t dtype, int32_t rows,
     a.uniform = uniform;
     a.token = out_token;
     a.logprob = out_logprob;
-    a.rows = rows;
     a.vocab = vocab;
     a.f32 = dtype == ANPD_F32;
     a.wide = ((uintptr_t)logits & (a.f32 ? 15 : 7)) == 0 && ld % 4 == 0;
-    // (all weights of a row fit in 63 bits)
+    a.n_slices = slices_of(vocab);
+    a.slice_shift = slice_shift(vocab);
+    // (a row's weights add up to less than 2^62)
     a.shift = 51;
     while (((uint64_t)vocab << a.shift) > (1ull << 62)) --a.shift;
+    const size_t need = anpd_sample_workspace_bytes(rows, vocab);
+    if (need > 0) {
+        if (!workspace || ((uintptr_t)workspace & 255) != 0) return fail(ANPD_E_INVAL, "%s: workspace must be a 256-byte aligned device buffer", who);
+        if (workspace_bytes < need) return fail(ANPD_E_CAPACITY, "%s: workspace has %zu bytes, %zu needed", who, workspace_bytes, need);
+    }
     OnDevice on;
     int32_t rc = on.enter_of(who, logits);
     if (rc != ANPD_OK) return rc;
     hipStream_t st = (hipStream_t)stream;
-    const dim3 grid((unsigned)rows);
-    if (vocab <= 256 * kSampleHeld) hipLaunchKernelGGL((sample_kernel<256, true>), grid, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((sample_kernel<1024, false>), grid, dim3(1024), 0, st, a);
-    HIP_TRY(hipGetLastError());
+    if (need == 0) {
+        launch_rows<true>(a, (unsigned)rows, st);
+        HIP_TRY(hipGetLastError());
+        return ANPD_OK;
+    }
+    a.slices = (Slice *)workspace;
+    for (int32_t row = 0; row < rows; row += kGroup) {
+        const unsigned n = (unsigned)(rows - row < kGroup ? rows - row : kGroup);
+        SampleArgs g = a;
+        g.logits = (const char *)logits + (size_t)row * ld * (a.f32 ? 4 : 2);
+        g.uniform += row;
+        g.token += row;
+        if (g.logprob) g.logprob += row;
+        if (g.temperatures) g.temperatures += row;
+        if (g.top_ks) g.top_ks += row;
+        if (g.top_ps) g.top_ps += row;
+        if (g.min_ps) g.min_ps += row;
+        if (a.slice_shift == 12) launch_slices<256>(g, n, st);
+        else launch_slices<1024>(g, n, st);
+        HIP_TRY(hipGetLastError());
+        launch_rows<false>(g, n, st);
+        HIP_TRY(hipGetLastError());
+    }
     return ANPD_OK;
 }
 
