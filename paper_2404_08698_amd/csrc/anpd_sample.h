@@ -96,6 +96,22 @@ __device__ __forceinline__ whole_t whole_exp2(double z)
     return (whole_t)__double_as_longlong(__longlong_as_double((long long)power) + 0x1p52) & 0xfffffffffffffull;
 }
 
+// The same with a table of 2^(j / 128) at hand (LDS): Taylor's sum to the power of 4 around one of its entries, for the many weights of a slice: 15
+// instructions of 64 bits, which take 8 cycles each, instead of 23.
+constexpr int kPowers = 128;
+__device__ __forceinline__ whole_t whole_exp2(double z, const double *powers)
+{
+    z = fmax(z, -2.0);
+    const double magic = 0x1.8p52 / kPowers, n = z + magic, t = (z - (n - magic)) * 0.693147180559945309417232;
+    const uint32_t parts = (uint32_t)__double_as_longlong(n);
+    double p = fma(1.0 / 24.0, t, 1.0 / 6.0);
+    p = fma(p, t, 0.5);
+    p = fma(p, t, 1.0);
+    p = fma(p, t, 1.0) * powers[parts % kPowers];
+    const whole_t power = (whole_t)__double_as_longlong(p) + ((whole_t)(parts / kPowers) << 52);
+    return (whole_t)__double_as_longlong(__longlong_as_double((long long)power) + 0x1p52) & 0xfffffffffffffull;
+}
+
 // Weights relative to `top`, and intervals of logits (any ascending function will do, so it is one of 32 bits); per: log2(e) / T.
 struct Scale {
     double top, per, shift;
@@ -103,6 +119,7 @@ struct Scale {
     __device__ __forceinline__ Scale(float most, float temperature, int shift_by) : top(most), per(1.44269504088896340735992 / (double)temperature), shift(shift_by),
                                                                                     bins(fminf((float)kBinsPerNat / temperature, 0x1p120f)) { first = interval(most); }
     __device__ __forceinline__ whole_t weight(float x) const { return whole_exp2(fma((double)x - top, per, shift)); }   // (-infinity: 0)
+    __device__ __forceinline__ whole_t weight(float x, const double *powers) const { return whole_exp2(fma((double)x - top, per, shift), powers); }
     __device__ __forceinline__ float interval(float x) const { return floorf(fminf(fmaxf(x * bins, -0x1p22f), 0x1p22f)); }
     // intervals below the top's, the last one for all that lie behind
     __device__ __forceinline__ int bin(float x) const { return (int)fminf(first - interval(x), (float)(kSampleBins - 1)); }
@@ -151,25 +168,27 @@ __device__ __forceinline__ float as_logit(float x, bool infinite)
     if (infinite) return x == INFINITY ? 0.f : -INFINITY;
     return x >= -INFINITY ? x : -INFINITY;
 }
+// Four adjacent logits that are all there, as they come.
 template <typename T>
-__device__ __forceinline__ void load_wide(const T *p, float (&x)[4])   // (four adjacent ones that are all there)
-{
-    if constexpr (std::is_same<T, float>::value) {
-        const f32x4 v = *(const f32x4 *)p;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = v[e];
-    } else {
-        const uint2 v = *(const uint2 *)p;
-        x[0] = __uint_as_float(v.x << 16); x[1] = __uint_as_float(v.x & 0xffff0000u);
-        x[2] = __uint_as_float(v.y << 16); x[3] = __uint_as_float(v.y & 0xffff0000u);
+struct Four {
+    typename std::conditional<std::is_same<T, float>::value, f32x4, uint2>::type v;
+    __device__ __forceinline__ void load(const T *p) { v = *(const decltype(v) *)p; }
+    __device__ __forceinline__ float operator[](int e) const
+    {
+        if constexpr (std::is_same<T, float>::value) return v[e];
+        else return __uint_as_float(e & 1 ? (e < 2 ? v.x : v.y) & 0xffff0000u : (e < 2 ? v.x : v.y) << 16);
     }
-}
+};
 // Four adjacent logits from place i on; behind the last one: minus infinity.
 template <typename T>
 __device__ __forceinline__ void load4(const SampleArgs &a, const T *of_row, int i, bool infinite, float (&x)[4])
 {
-    if (a.wide && i + 4 <= a.vocab) load_wide<T>(of_row + i, x);
-    else {
+    if (a.wide && i + 4 <= a.vocab) {
+        Four<T> v;
+        v.load(of_row + i);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = v[e];
+    } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e) x[e] = i + e < a.vocab ? load_f32(of_row, (size_t)(i + e)) : -INFINITY;
     }
@@ -181,6 +200,7 @@ __device__ __forceinline__ void load4(const SampleArgs &a, const T *of_row, int 
 template <int THREADS>
 struct SliceShared {
     whole_t bins[kSampleBins], sum[THREADS / 64];
+    double powers[kPowers];
     float most[THREADS / 64];
 };
 template <typename T, int THREADS, int EACH>
@@ -196,6 +216,7 @@ __device__ __forceinline__ void look_at_slice(const SampleArgs &a, const RowRule
 #pragma unroll
         for (int e = 0; e < 4; ++e) most = fmaxf(most, x[c][e]);
     for (int i = threadIdx.x; i < kSampleBins; i += THREADS) s.bins[i] = 0;
+    if (threadIdx.x < kPowers) s.powers[threadIdx.x] = exp2((double)threadIdx.x / kPowers);
     most = wave_max(most);
     if (lane == 0) s.most[wave] = most;
     __syncthreads();
@@ -212,7 +233,7 @@ __device__ __forceinline__ void look_at_slice(const SampleArgs &a, const RowRule
             for (int e = 0; e < 4; ++e) {
                 const float v = infinite ? (x[c][e] == INFINITY ? 0.f : -INFINITY) : x[c][e];
                 if (!(v > -INFINITY)) continue;
-                const whole_t m = rules.top_k ? 1 : scale.weight(v);
+                const whole_t m = rules.top_k ? 1 : scale.weight(v, s.powers);
                 sum += m;
                 const int b = scale.bin(v);
                 if (b < kSampleBins - 1 && m != 0) atomicAdd(&s.bins[b], m);   // (most logits of a peaked row lie in the last one, which nobody asks for)
@@ -258,7 +279,7 @@ struct RowShared {
     float most[kWaves];
     double before, all;
     whole_t whole_before, total;
-    int at, place, count;
+    int at, place, count, found, found_at[kRowThreads];   // (found: those that may be in an interval)
     float border;
 };
 
@@ -281,48 +302,50 @@ struct RowSampler {
         : a(args), s(shared), slices(of), of_row((const T *)args.logits + (size_t)at * args.ld), rules(r), lane(threadIdx.x & 63), wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)), row(at), infinite(most == INFINITY),
           scale(most == INFINITY ? 0.f : most, r.temperature, args.shift) {}
 
-    // f(logit, index) for the logits from low to high.  A thread compares 32 of them at a time, all requested before the first; those that f is for are few
-    // and read again, so that there is one place for it (a block runs through this code once, and what is not in the instruction cache yet it waits for).
+    // f(logit, index) for the logits from low to high.
     template <typename F>
     __device__ __forceinline__ void sweep(float low, float high, F f) const
     {
-        const bool wide = a.wide && !infinite;
-        for (int c = 0; c < a.vocab; c += 32 * kRowThreads) {
-            uint32_t hit = 0;
-            if (wide) {
-                const T *p = of_row + c + 4 * (int)threadIdx.x;
-                const int left = a.vocab - 3 - c - 4 * (int)threadIdx.x;   // (a vocabulary's last ones, up to three: below)
-                float x[8][4];
-#pragma unroll
-                for (int u = 0; u < 8; ++u) {
-                    if (u * 4 * kRowThreads < left) load_wide<T>(p + u * 4 * kRowThreads, x[u]);
-                    else x[u][0] = x[u][1] = x[u][2] = x[u][3] = __uint_as_float(0x7fc00000u);
-                }
-#pragma unroll
-                for (int u = 0; u < 8; ++u)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) hit |= x[u][e] >= low && x[u][e] <= high ? 1u << (4 * u + e) : 0u;
-            } else {
 #pragma unroll 4
-                for (int u = 0; u < 32; ++u) {
-                    const int i = c + u * kRowThreads + (int)threadIdx.x;
-                    const float v = i < a.vocab ? as_logit(load_f32(of_row, (size_t)i), infinite) : -INFINITY;
-                    if (v >= low && v <= high && v > -INFINITY) hit |= 1u << u;
-                }
-            }
+        for (int i = threadIdx.x; i < a.vocab; i += kRowThreads) {
+            const float v = as_logit(load_f32(of_row, (size_t)i), infinite);
+            if (v >= low && v <= high && v > -INFINITY) f(v, i);
+        }
+    }
+    // found(index) for the logits from low to high and no others, but that infinities and NaN may be missed; rows that may be read four logits at a time.  A thread
+    // compares 32 at a time, the next ones requested before.
+    static constexpr int kSweep = 32 * kRowThreads;
+    __device__ __forceinline__ void request(int c, Four<T> (&x)[8]) const
+    {
+        // (a vocabulary's last logits, up to three, are left for the end; behind it the first ones of the row, for nothing)
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            const int i = c + 4 * (u * kRowThreads + (int)threadIdx.x);
+            x[u].load(of_row + (i + 4 <= a.vocab ? i : 0));
+        }
+    }
+    template <typename F>
+    __device__ __forceinline__ void sweep_wide(float low, float high, F found) const
+    {
+        Four<T> x[8];
+        request(0, x);
+#pragma unroll 1
+        for (int c = 0; c < a.vocab; c += kSweep) {
+            uint32_t hit = 0;
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) hit |= x[u][e] >= low && x[u][e] <= high ? 1u << (4 * u + e) : 0u;
+            if (c + kSweep < a.vocab) request(c + kSweep, x);
+            const int left = (a.vocab & ~3) - c - 4 * (int)threadIdx.x, fours = left <= 0 ? 0 : (left + 4 * kRowThreads - 1) / (4 * kRowThreads);
+            hit = fours >= 8 ? hit : hit & ((1u << (4 * fours)) - 1);
             while (hit) {
                 const int bit = __builtin_ctz(hit);
                 hit &= hit - 1;
-                const int i = c + (wide ? (bit >> 2) * 4 * kRowThreads + 4 * (int)threadIdx.x + (bit & 3) : bit * kRowThreads + (int)threadIdx.x);
-                const float v = as_logit(load_f32(of_row, (size_t)i), infinite);
-                if (v > -INFINITY) f(v, i);
+                found(c + (bit >> 2) * 4 * kRowThreads + 4 * (int)threadIdx.x + (bit & 3));
             }
         }
-        if (wide && (int)threadIdx.x < (a.vocab & 3)) {
-            const int i = (a.vocab & ~3) + (int)threadIdx.x;
-            const float v = load_f32(of_row, (size_t)i);
-            if (v >= low && v <= high && v > -INFINITY) f(v, i);
-        }
+        if ((int)threadIdx.x < (a.vocab & 3)) found((a.vocab & ~3) + (int)threadIdx.x);   // (to be looked at)
     }
     __device__ __forceinline__ bool inside(float v, int i) const { return v > border || (v == border && i <= last && v > -INFINITY); }
 
@@ -380,35 +403,59 @@ struct RowSampler {
             if (!(fabsf(at) < 0x1p21f)) high = INFINITY;   // (where the numbers of intervals end)
         }
     };
-    // Those of the row that `which` names: into `few` as far as they fit; their number, smallest and largest.
+    // Those of the row from low to high that `which` names: into `few` as far as they fit; their number, and, if they do not fit, smallest and largest.
     template <typename Which>
-    __device__ __forceinline__ int collect(float from, float to, Which which, float &lo, float &hi)
+    __device__ __forceinline__ int collect(float low, float high, Which which, float &lo, float &hi)
     {
         __syncthreads();
-        if (threadIdx.x == 0) s.count = 0;
+        if (threadIdx.x == 0) s.count = s.found = 0;
         __syncthreads();
-        float low = INFINITY, high = -INFINITY;
-        sweep(from, to, [&](float v, int i) __attribute__((always_inline)) {
+        int m = kSampleFew + 1;
+        if (a.wide && !infinite && a.vocab >= 4) {
+            // (which ones first; their logits are read again side by side)
+            sweep_wide(low, high, [&](int i) __attribute__((always_inline)) {
+                const int at = atomicAdd(&s.found, 1);
+                if (at < kRowThreads) s.found_at[at] = i;
+            });
+            __syncthreads();
+            const int n = s.found;
+            if (n <= kRowThreads) {
+                if ((int)threadIdx.x < n) {
+                    const int i = s.found_at[threadIdx.x];
+                    const float v = load_f32(of_row, (size_t)i);
+                    if (v >= low && v <= high && v > -INFINITY && which(v, i)) {
+                        const int at = atomicAdd(&s.count, 1);
+                        if (at < kSampleFew) { s.few[at] = v; s.few_at[at] = i; }
+                    }
+                }
+                __syncthreads();
+                m = s.count;
+                if (m <= kSampleFew) return m;
+                __syncthreads();
+                if (threadIdx.x == 0) s.count = 0;
+                __syncthreads();
+            }
+        }
+        float least = INFINITY, most = -INFINITY;
+        sweep(low, high, [&](float v, int i) __attribute__((always_inline)) {
             if (!which(v, i)) return;
             const int at = atomicAdd(&s.count, 1);
             if (at < kSampleFew) { s.few[at] = v; s.few_at[at] = i; }
-            low = fminf(low, v);
-            high = fmaxf(high, v);
+            least = fminf(least, v);
+            most = fmaxf(most, v);
         });
+        least = -wave_max(-least);
+        most = wave_max(most);
+        float *l = (float *)s.part, *h = l + kWaves;
         __syncthreads();
-        const int m = s.count;
-        if (m > kSampleFew) {   // (the same for all)
-            low = -wave_max(-low);
-            high = wave_max(high);
-            float *l = (float *)s.part, *h = l + kWaves;
-            if (lane == 0) { l[wave] = low; h[wave] = high; }
-            __syncthreads();
+        if (lane == 0) { l[wave] = least; h[wave] = most; }
+        __syncthreads();
 #pragma unroll
-            for (int i = 0; i < kWaves; ++i) { low = fminf(low, l[i]); high = fmaxf(high, h[i]); }
-            __syncthreads();
-            lo = low;
-            hi = high;
-        }
+        for (int i = 0; i < kWaves; ++i) { least = fminf(least, l[i]); most = fmaxf(most, h[i]); }
+        m = s.count;
+        __syncthreads();
+        lo = least;
+        hi = most;
         return m;
     }
     // The pairs of m numbers, dealt to the threads: i with those from .. to - 1.
