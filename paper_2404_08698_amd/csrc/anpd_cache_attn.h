@@ -75,6 +75,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_stream_kernel(const AttnArg
         const int page = tiles.at(t) * (kStreamTile / 16) + 2 * wave;
         ida = s.table[page < last_page ? page : last_page];
         idb = s.table[page + 1 < last_page ? page + 1 : last_page];
+        asm volatile("" : "+v"(ida), "+v"(idb));   // (waited for here: in front of their use all loads in flight would be, at every tile)
     };
     u32x4 kf[NKS], vf[2][NDB][2];   // values: [page][64 dims][keys 4 half.., 8 + 4 half..], two dims side by side
     auto load_k = [&](int pa, int pb) __attribute__((always_inline)) {

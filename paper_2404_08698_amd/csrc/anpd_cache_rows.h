@@ -183,10 +183,11 @@ __device__ __forceinline__ void quantise(const RowsArgs &a, const Span &w, uint3
         for (int o = 1; o < LANES; o <<= 1) { const uint32_t b = (uint32_t)__shfl_xor((int)bits, o, 64); bits = b > bits ? b : bits; }
         const float top = __uint_as_float(bits), per = 127.0f / top;
         const bool finite = bits < 0x7f800000u;
-        uint32_t c[2] = {0, 0};
+        uint32_t c[2] = {0x80808080u, 0x80808080u};
         if (finite && bits != 0) {
+            c[0] = c[1] = 0;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) c[e >> 2] |= ((uint32_t)code_of(x[i][e], top, per) & 0xffu) << (8 * (e & 3));
+            for (int e = 0; e < 8; ++e) c[e >> 2] |= (uint32_t)(code_of(x[i][e], top, per) + 128) << (8 * (e & 3));
         }
         if (t >= w.from && t < w.to) {
             if (lane % LANES == 0) scales[t] = finite ? top / 127.0f : __uint_as_float(0x7fc00000u);
@@ -257,7 +258,7 @@ __device__ __forceinline__ void read_back(const RowsArgs &a, const Span &w, uint
         const float s = scales[t];
         float x[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = (float)(int8_t)((e < 4 ? c.x : c.y) >> (8 * (e & 3))) * s;
+        for (int e = 0; e < 8; ++e) x[e] = (float)((int)((e < 4 ? c.x : c.y) >> (8 * (e & 3)) & 0xffu) - 128) * s;
         store_row8(a, rows, (size_t)(w.s.row0 + w.first + t - w.s.pos0) * ld + (size_t)w.head * DH + dim, x);
     }
 }

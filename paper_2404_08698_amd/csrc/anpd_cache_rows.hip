@@ -110,8 +110,8 @@ namespace anpd {
 
 void launch_attention8(const AttnArgs &a, Seen rules, int head_dim, hipStream_t st)
 {
-    if (head_dim == 128) { if (a.q_f32) launch8<128, 3>(a, rules, st); else launch8<128, 1>(a, rules, st); }
-    else if (a.q_f32) launch8<64, 3>(a, rules, st);
+    if (head_dim == 128) { if (a.q_f32) launch8<128, 2>(a, rules, st); else launch8<128, 1>(a, rules, st); }
+    else if (a.q_f32) launch8<64, 2>(a, rules, st);
     else launch8<64, 1>(a, rules, st);
 }
 

@@ -63,7 +63,7 @@ __host__ __device__ __forceinline__ size_t vf_elem(int tok, int dim)
 
 // ------------------------------------------------------ caches of 8 bits
 //
-// Block of 16 tokens of a (page, layer, k|v, head): 16 x head_dim signed codes, then 16 fp32 scales; a value is code * scale.
+// Block of 16 tokens of a (page, layer, k|v, head): 16 x head_dim bytes, then 16 fp32 scales; a value is (byte - 128) * scale.
 //   K: [dim / 32][(dim % 32) / 16][token][dim % 16]
 //   V: [dim / 64][half][dim % 64][key], half = (token / 4) % 2, key = token % 4 + 4 (token / 8)
 // A lane's 16 bytes are two operands of a 32x32x16 product: 16 dims of a key, or of two adjacent dims the eight keys whose weights its half of
