@@ -41,7 +41,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_stream_kernel(const AttnArg
     const int begin = split * a.chunk, i1 = begin + a.chunk < tiles.n ? begin + a.chunk : tiles.n;
     if (begin >= tiles.n) return;   // (the whole block; what joins the splits does not look at this one)
     const int i0 = RULES ? first_tile(tiles, wave_min(r.fk), begin, i1, kStreamTile) : begin;   // (the same for all waves)
-    if constexpr (RULES == kTree) tree_info(a, s, pre, depth, r);
+    if constexpr (RULES == kTree) tree_info(a, s, pre, parent_of(a, s), depth, r);
 
     u32x4 q[SHARED_Q ? 1 : NKS][TERMS];
     {
@@ -513,7 +513,7 @@ __global__ __launch_bounds__(256, 1) void cache_attn_plain_kernel(const AttnArgs
     const int begin = split * a.chunk, i1 = begin + a.chunk < tiles.n ? begin + a.chunk : tiles.n;
     if (begin >= tiles.n) return;
     const int i0 = first_tile(tiles, wave_min(r.fk), begin, i1, kStreamTile);
-    if constexpr (RULES == kTree) tree_info(a, s, pre, depth, r);
+    if constexpr (RULES == kTree) tree_info(a, s, pre, parent_of(a, s), depth, r);
     float q[DH / 2];
     {
         const size_t at = (size_t)r.row * a.ldq + (size_t)r.head * DH + half * (DH / 2);

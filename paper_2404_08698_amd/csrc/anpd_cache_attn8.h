@@ -75,44 +75,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn8_kernel(const AttnArgs a)
     const int begin = split * a.chunk, i1 = begin + a.chunk < tiles.n ? begin + a.chunk : tiles.n;
     if (begin >= tiles.n) return;   // (the whole block; what joins the splits does not look at this one)
     const int i0 = RULES ? first_tile(tiles, wave_min(r.fk), begin, i1, kStreamTile) : begin;   // (the same for all waves)
-    if constexpr (RULES == kTree) tree_info(a, s, pre, depth, r);
 
-    // A step of 16 dims: 8 y .. of the 16 that a half of the wave has of every 32.
-    float row_scale;
-    {
-        const size_t at = (size_t)r.row * a.ldq + (size_t)r.head * DH + 16 * half;
-        float x[NKS / kStreamWaves][8], most = 0.f;
-        bool finite = true;
-#pragma unroll
-        for (int y = 0; y < NKS / kStreamWaves; ++y) {
-            const int ks = y * kStreamWaves + wave;
-            load_q8(a, at + 32 * (ks >> 1) + 8 * (ks & 1), x[y]);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) { most = fmaxf(most, fabsf(x[y][e])); finite = finite && fabsf(x[y][e]) <= 3.4028234e38f; }
-        }
-        most = both_halves_max(finite ? most : INFINITY);
-        if (half == 0) most_of[wave][m] = most;
-        __syncthreads();
-#pragma unroll
-        for (int w = 0; w < kStreamWaves; ++w) most = fmaxf(most, most_of[w][m]);
-        int up = most > 0.f && most < INFINITY ? 15 - __builtin_amdgcn_frexp_expf(most) : 0;
-        up = up < 100 ? up : 100;   // (what is smaller has scores of 0)
-        row_scale = most < INFINITY ? ldexpf(1.0f, -up) : __uint_as_float(0x7fc00000u);   // (a row with an infinity or a NaN: all its scores are NaN)
-#pragma unroll
-        for (int y = 0; y < NKS / kStreamWaves; ++y) {
-            u32x4 q[TERMS];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[y][e] = most < INFINITY ? ldexpf(x[y][e], up) : 0.f;
-            split_terms16<TERMS>(x[y], q);
-#pragma unroll
-            for (int t = 0; t < TERMS; ++t) lds.q[y * kStreamWaves + wave][t][lane] = q[t];
-        }
-        __syncthreads();
-    }
-    // Products to exponents: in the factor, or where the rules change the scores, in the products themselves.
-    constexpr Scored HOW = !RULES ? kUnscored : TERMS == 1 ? kScoredRough : kScored;
-    const bool scored = HOW != kUnscored && (a.cap > 0.f || a.slopes);   // (the same for all)
-    const float factor = scored ? score_factor<HOW>(a) : score_factor<HOW>(a) * row_scale;
     Running<NDT> run;
     run.start();
 
@@ -126,7 +89,6 @@ __global__ __launch_bounds__(256, 2) void cache_attn8_kernel(const AttnArgs a)
         const int page = tiles.at(t) * (kStreamTile / 16) + 2 * wave;
         ida = s.table[page < last_page ? page : last_page];
         idb = s.table[page + 1 < last_page ? page + 1 : last_page];
-        asm volatile("" : "+v"(ida), "+v"(idb));   // (waited for here: in front of their use all loads in flight would be, at every tile)
     };
     // Two tiles are on their way while a third is looked at: what 8 bits take of a compute unit's loads in flight would not keep the memory busy otherwise.
     u32x4 kf[2][NKC], vf[2][2][NDB];
@@ -147,9 +109,65 @@ __global__ __launch_bounds__(256, 2) void cache_attn8_kernel(const AttnArgs a)
             for (int d = 0; d < NDB; ++d) vf[b][g][d] = p[d * 64];
         }
     };
+    if (i0 < i1) fetch_ids(i0);
+    // What the first tiles' loads wait for (pages) and what is worked on behind them (the rows, the tree) is requested together.
+    int up = -1;
+    if constexpr (RULES == kTree) up = parent_of(a, s);
+    float x[NKS / kStreamWaves][8];
+#pragma unroll
+    for (int y = 0; y < NKS / kStreamWaves; ++y) {
+        const int ks = y * kStreamWaves + wave;
+        load_q8(a, (size_t)r.row * a.ldq + (size_t)r.head * DH + 16 * half + 32 * (ks >> 1) + 8 * (ks & 1), x[y]);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    if (i0 < i1) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            load_k(b, page_of(i0 + b, 0), page_of(i0 + b, 1));
+            __builtin_amdgcn_sched_barrier(0);   // (in the loop's order, or its waits would be for what comes last here)
+            load_v(b, page_of(i0 + b, 0), page_of(i0 + b, 1));
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+    if constexpr (RULES == kTree) tree_info(a, s, pre, up, depth, r);
+    // The rows' terms.  A step of 16 dims: 8 y .. of the 16 that a half of the wave has of every 32.
+    float row_scale;
+    {
+        float most = 0.f;
+        bool finite = true;
+#pragma unroll
+        for (int y = 0; y < NKS / kStreamWaves; ++y)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) { most = fmaxf(most, fabsf(x[y][e])); finite = finite && fabsf(x[y][e]) <= 3.4028234e38f; }
+        most = both_halves_max(finite ? most : INFINITY);
+        if (half == 0) most_of[wave][m] = most;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kStreamWaves; ++w) most = fmaxf(most, most_of[w][m]);
+        int by = most > 0.f && most < INFINITY ? 15 - __builtin_amdgcn_frexp_expf(most) : 0;
+        by = by < 100 ? by : 100;   // (what is smaller has scores of 0)
+        row_scale = most < INFINITY ? ldexpf(1.0f, -by) : __uint_as_float(0x7fc00000u);   // (a row with an infinity or a NaN: all its scores are NaN)
+#pragma unroll
+        for (int y = 0; y < NKS / kStreamWaves; ++y) {
+            u32x4 q[TERMS];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[y][e] = most < INFINITY ? ldexpf(x[y][e], by) : 0.f;
+            split_terms16<TERMS>(x[y], q);
+#pragma unroll
+            for (int t = 0; t < TERMS; ++t) lds.q[y * kStreamWaves + wave][t][lane] = q[t];
+        }
+        __syncthreads();
+    }
+    // Products to exponents: in the factor, or where the rules change the scores, in the products themselves.
+    constexpr Scored HOW = !RULES ? kUnscored : TERMS == 1 ? kScoredRough : kScored;
+    const bool scored = HOW != kUnscored && (a.cap > 0.f || a.slopes);   // (the same for all)
+    const float factor = scored ? score_factor<HOW>(a) : score_factor<HOW>(a) * row_scale;
     auto tile = [&](int i, int b) __attribute__((always_inline)) {
         const int base = tiles.at(i) * kStreamTile + 32 * wave;
-        if (((i + 2 - i0) & 63) == 0) fetch_ids(i + 2);
+        if (((i + 2 - i0) & 63) == 0) {
+            fetch_ids(i + 2);
+            asm volatile("" : "+v"(ida), "+v"(idb));   // (waited for here: in front of their use all loads in flight would be, at every tile)
+        }
         const size_t na = page_of(i + 2, 0), nb = page_of(i + 2, 1);
         __builtin_amdgcn_wave_barrier();
         scale_of[wave][lane] = scale[b];
@@ -211,14 +229,6 @@ __global__ __launch_bounds__(256, 2) void cache_attn8_kernel(const AttnArgs a)
         load_v(b, na, nb);
     };
     if (i0 < i1) {
-        fetch_ids(i0);
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {
-            load_k(b, page_of(i0 + b, 0), page_of(i0 + b, 1));
-            __builtin_amdgcn_sched_barrier(0);   // (in the loop's order, or its waits would be for what comes last here)
-            load_v(b, page_of(i0 + b, 0), page_of(i0 + b, 1));
-            __builtin_amdgcn_sched_barrier(0);
-        }
         // (one exit, and the same loads on every way through the loop, behind the last tile for nothing: otherwise they could not be counted)
         for (int i = i0; i < i1; i += 2) {
             tile(i, 0);

@@ -17,39 +17,36 @@ struct RowsArgs {
     void *k, *v;                 // the rows (read or written)
     int64_t ldk, ldv;
     int32_t layer, n_layers, n_kv_heads, page_tokens;
-    int32_t f32, wide;           // the rows' type; whether they may be moved 16 bytes at a time
+    int32_t wide;                // whether the rows may be moved 16 bytes at a time
     int32_t n_seq, n_spans;
 };
 
-// Eight dims of a row.
+// Eight dims of a row of type T.
+template <typename T>
 __device__ __forceinline__ void load_row8(const RowsArgs &a, const void *rows, size_t at, float (&x)[8])
 {
-    if (a.f32) {
-        const float *p = (const float *)rows + at;
+    const T *p = (const T *)rows + at;
+    if constexpr (std::is_same<T, float>::value) {
         if (a.wide) {
             const f32x4 u = *(const f32x4 *)p, v = *(const f32x4 *)(p + 4);
 #pragma unroll
             for (int i = 0; i < 4; ++i) { x[i] = u[i]; x[4 + i] = v[i]; }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = p[i];
+            return;
         }
-    } else {
-        const bf16_t *p = (const bf16_t *)rows + at;
-        if (a.wide) {
-            const u32x4 u = *(const u32x4 *)p;
+    } else if (a.wide) {
+        const u32x4 u = *(const u32x4 *)p;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(u[i] << 16); x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u); }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = bf16_to_f32(p[i]);
-        }
+        for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(u[i] << 16); x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u); }
+        return;
     }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = load_f32(p, (size_t)i);
 }
+template <typename T>
 __device__ __forceinline__ void store_row8(const RowsArgs &a, void *rows, size_t at, const float (&x)[8])
 {
-    if (a.f32) {
-        float *p = (float *)rows + at;
+    T *p = (T *)rows + at;
+    if constexpr (std::is_same<T, float>::value) {
         if (a.wide) {
             *(f32x4 *)p = (f32x4){x[0], x[1], x[2], x[3]};
             *(f32x4 *)(p + 4) = (f32x4){x[4], x[5], x[6], x[7]};
@@ -58,7 +55,6 @@ __device__ __forceinline__ void store_row8(const RowsArgs &a, void *rows, size_t
             for (int i = 0; i < 8; ++i) p[i] = x[i];
         }
     } else {
-        bf16_t *p = (bf16_t *)rows + at;
         u32x4 w;
 #pragma unroll
         for (int i = 0; i < 4; ++i) w[i] = pack_bf16(x[2 * i], x[2 * i + 1]);
@@ -81,13 +77,45 @@ __device__ __forceinline__ void transpose4(const uint32_t (&a)[4], uint32_t (&d)
     d[3] = __builtin_amdgcn_perm(w, z, 0x07060302u);
 }
 
-// 127 x / top to the nearest whole number, ties to even; per = 127 / top.  A product in 32 bits decides unless it lies next to the middle between two
-// codes (or per is beyond 32 bits); there the quotient in 64 bits does: one that is not the middle is 2^-33 of it away, and the middle itself comes out exactly.
-__device__ __forceinline__ int code_of(float x, float top, float per)
+// Eight codes + 128, bytes side by side: 127 x / top to the nearest whole number, ties to even; per = 127 / top.  A product in 32 bits is off by 2^-16 at most, so it
+// decides unless it lies next to the middle between two codes (or per is beyond 32 bits); there the quotient in 64 bits does: one that is not the middle
+// is 2^-33 of it away, and the middle itself comes out exactly.
+__device__ __forceinline__ uint2 codes_of(const float (&x)[8], float top, float per)
 {
-    const float t = x * per, k = rintf(t);
-    if (fabsf(fabsf(t - k) - 0.5f) > 0x1p-12f && fabsf(t) < 128.f) return (int)k;
-    return (int)rint(127.0 * (double)x / (double)top);
+    const float magic = 12582912.0f;   // (1.5 2^23: what is added to it is rounded to a whole number, which its lowest bits hold)
+    uint32_t b[8];
+    float far = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const float t = x[e] * per, k = t + magic;
+        far = fmaxf(far, fabsf(t - (k - magic)));
+        b[e] = __float_as_uint(k);
+    }
+    if (!(far < 0.5f - 0x1p-15f) || !(per < 0x1p120f)) {
+        uint32_t near = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float t = x[e] * per;
+            near |= !(fabsf(t - (t + magic - magic)) < 0.5f - 0x1p-15f) || !(per < 0x1p120f) ? 1u << e : 0u;
+        }
+        while (near) {   // (one of them, as a rule)
+            const int e = __builtin_ctz(near);
+            near &= near - 1;
+            float v = x[0];
+#pragma unroll
+            for (int u = 1; u < 8; ++u) v = e == u ? x[u] : v;
+            const uint32_t c = (uint32_t)(int)rint(127.0 * (double)v / (double)top);
+#pragma unroll
+            for (int u = 0; u < 8; ++u) b[u] = e == u ? c : b[u];
+        }
+    }
+    uint32_t w[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const uint32_t lo = __builtin_amdgcn_perm(b[4 * h + 1], b[4 * h], 0x00000400u), hi = __builtin_amdgcn_perm(b[4 * h + 3], b[4 * h + 2], 0x04000000u);
+        w[h] = ((lo & 0xffffu) | (hi & 0xffff0000u)) ^ 0x80808080u;
+    }
+    return make_uint2(w[0], w[1]);
 }
 
 // What a wave of the kernels below is about.
@@ -117,7 +145,7 @@ struct Span {
 };
 
 // Plain and matrix-core order: eight dims of a position by each lane.
-template <int KIND, int DH, bool STORE>
+template <int KIND, int DH, bool STORE, typename T>
 __device__ __forceinline__ void move_rows(const RowsArgs &a, const Span &w)
 {
     constexpr int LANES = DH / 8;
@@ -130,7 +158,7 @@ __device__ __forceinline__ void move_rows(const RowsArgs &a, const Span &w)
         const size_t at = (size_t)(w.s.row0 + p - w.s.pos0) * ld + (size_t)w.head * DH + dim;
         const int page = w.s.table[p / a.page_tokens];
         float x[8];
-        if (STORE) load_row8(a, rows, at, x);
+        if (STORE) load_row8<T>(a, rows, at, x);
         if constexpr (KIND == kCacheFragments) {
             bf16_t *to = (bf16_t *)w.s.pool + kvf_base(page, a.layer, a.n_layers, w.kind, w.head, a.n_kv_heads, DH);
 #pragma unroll
@@ -148,12 +176,12 @@ __device__ __forceinline__ void move_rows(const RowsArgs &a, const Span &w)
                 else { if (STORE) to[i] = (bf16_t)pack_bf16(x[i], 0.f); else x[i] = bf16_to_f32(to[i]); }
             }
         }
-        if (!STORE) store_row8(a, rows, at, x);
+        if (!STORE) store_row8<T>(a, rows, at, x);
     }
 }
 
 // 8 bits.  turn: LDS of the wave, [position][dim].
-template <int DH>
+template <int DH, typename T>
 __device__ __forceinline__ void quantise(const RowsArgs &a, const Span &w, uint32_t (&turn)[16][DH / 4])
 {
     constexpr int LANES = DH / 8, STEP = 64 / LANES;
@@ -163,14 +191,11 @@ __device__ __forceinline__ void quantise(const RowsArgs &a, const Span &w, uint3
     char *block = (char *)w.s.pool + kv8_base(w.s.table[w.first / 16], a.layer, a.n_layers, w.kind, w.head, a.n_kv_heads, DH);
     float *scales = (float *)(block + 16 * DH);
     float x[16 / STEP][8];
+    // (all requested before the first is looked at; positions that are not new read a new one's row again)
 #pragma unroll
     for (int i = 0; i < 16 / STEP; ++i) {
-        const int t = i * STEP + lane / LANES;
-        if (t >= w.from && t < w.to) load_row8(a, rows, (size_t)(w.s.row0 + w.first + t - w.s.pos0) * ld + (size_t)w.head * DH + dim, x[i]);
-        else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[i][e] = 0.f;
-        }
+        const int t = i * STEP + lane / LANES, near = t < w.from ? w.from : t < w.to ? t : w.to - 1;
+        load_row8<T>(a, rows, (size_t)(w.s.row0 + w.first + near - w.s.pos0) * ld + (size_t)w.head * DH + dim, x[i]);
     }
 #pragma unroll
     for (int i = 0; i < 16 / STEP; ++i) {
@@ -183,17 +208,13 @@ __device__ __forceinline__ void quantise(const RowsArgs &a, const Span &w, uint3
         for (int o = 1; o < LANES; o <<= 1) { const uint32_t b = (uint32_t)__shfl_xor((int)bits, o, 64); bits = b > bits ? b : bits; }
         const float top = __uint_as_float(bits), per = 127.0f / top;
         const bool finite = bits < 0x7f800000u;
-        uint32_t c[2] = {0x80808080u, 0x80808080u};
-        if (finite && bits != 0) {
-            c[0] = c[1] = 0;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) c[e >> 2] |= (uint32_t)(code_of(x[i][e], top, per) + 128) << (8 * (e & 3));
-        }
+        uint2 c = make_uint2(0x80808080u, 0x80808080u);
+        if (finite && bits != 0) c = codes_of(x[i], top, per);
         if (t >= w.from && t < w.to) {
             if (lane % LANES == 0) scales[t] = finite ? top / 127.0f : __uint_as_float(0x7fc00000u);
-            if (w.kind == 0) *(uint2 *)(block + k8_elem(t, dim)) = make_uint2(c[0], c[1]);
+            if (w.kind == 0) *(uint2 *)(block + k8_elem(t, dim)) = c;
         }
-        if (w.kind == 1) *(uint2 *)&turn[t][dim / 4] = make_uint2(c[0], c[1]);
+        if (w.kind == 1) *(uint2 *)&turn[t][dim / 4] = c;
     }
     if (w.kind == 0) return;
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
@@ -224,7 +245,7 @@ __device__ __forceinline__ void quantise(const RowsArgs &a, const Span &w, uint3
             for (int e = 0; e < 4; ++e) to[8 * e + 4 * g + t] = (char)(out[g][e] >> (8 * t));
         }
 }
-template <int DH>
+template <int DH, typename T>
 __device__ __forceinline__ void read_back(const RowsArgs &a, const Span &w, uint32_t (&turn)[16][DH / 4])
 {
     constexpr int LANES = DH / 8, STEP = 64 / LANES;
@@ -259,21 +280,21 @@ __device__ __forceinline__ void read_back(const RowsArgs &a, const Span &w, uint
         float x[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = (float)((int)((e < 4 ? c.x : c.y) >> (8 * (e & 3)) & 0xffu) - 128) * s;
-        store_row8(a, rows, (size_t)(w.s.row0 + w.first + t - w.s.pos0) * ld + (size_t)w.head * DH + dim, x);
+        store_row8<T>(a, rows, (size_t)(w.s.row0 + w.first + t - w.s.pos0) * ld + (size_t)w.head * DH + dim, x);
     }
 }
 
 // grid: n_spans * n_kv_heads * 2 waves, four to a block
-template <int KIND, int DH, bool STORE>
+template <int KIND, int DH, bool STORE, typename T>
 __global__ __launch_bounds__(64 * kRowsWaves) void cache_rows_kernel(const RowsArgs a)
 {
     Span w;
     if (!w.find(a)) return;
     if constexpr (KIND == kCache8) {
         __shared__ uint32_t turn[kRowsWaves][16][DH / 4];
-        if (STORE) quantise<DH>(a, w, turn[threadIdx.x >> 6]);
-        else read_back<DH>(a, w, turn[threadIdx.x >> 6]);
-    } else move_rows<KIND, DH, STORE>(a, w);
+        if (STORE) quantise<DH, T>(a, w, turn[threadIdx.x >> 6]);
+        else read_back<DH, T>(a, w, turn[threadIdx.x >> 6]);
+    } else move_rows<KIND, DH, STORE, T>(a, w);
 }
 
 // ------------------------------------------------------------------ the accepted rows move together

@@ -63,29 +63,33 @@ int32_t gather(const char *who, const anpd_kv *const *kvs, int32_t n_seq, const 
     a.n_layers = c.n_layers;
     a.n_kv_heads = c.n_kv_heads;
     a.page_tokens = c.page_tokens;
-    a.f32 = dtype == ANPD_F32;
-    a.wide = (bits & 15) == 0 && (ldk | ldv) % (a.f32 ? 4 : 8) == 0;
+    a.wide = (bits & 15) == 0 && (ldk | ldv) % (dtype == ANPD_F32 ? 4 : 8) == 0;
     return ANPD_OK;
 }
 
-template <int KIND, bool STORE>
+template <int KIND, bool STORE, typename T>
 void launch_kind(const RowsArgs &a, int head_dim, dim3 grid, hipStream_t st)
 {
-    if (head_dim == 128) hipLaunchKernelGGL((cache_rows_kernel<KIND, 128, STORE>), grid, dim3(64 * kRowsWaves), 0, st, a);
-    else hipLaunchKernelGGL((cache_rows_kernel<KIND, 64, STORE>), grid, dim3(64 * kRowsWaves), 0, st, a);
+    if (head_dim == 128) hipLaunchKernelGGL((cache_rows_kernel<KIND, 128, STORE, T>), grid, dim3(64 * kRowsWaves), 0, st, a);
+    else hipLaunchKernelGGL((cache_rows_kernel<KIND, 64, STORE, T>), grid, dim3(64 * kRowsWaves), 0, st, a);
 }
-template <bool STORE>
+template <bool STORE, typename T>
 int32_t launch_rows(const RowsArgs &a, const CacheShape &c, hipStream_t st)
 {
     const dim3 grid((unsigned)(((int64_t)a.n_spans * a.n_kv_heads * 2 + kRowsWaves - 1) / kRowsWaves));
     switch (kind_of(c)) {
-    case kCache8: launch_kind<kCache8, STORE>(a, c.head_dim, grid, st); break;
-    case kCacheFragments: launch_kind<kCacheFragments, STORE>(a, c.head_dim, grid, st); break;
-    case kCacheBf16: launch_kind<kCacheBf16, STORE>(a, c.head_dim, grid, st); break;
-    default: launch_kind<kCacheF32, STORE>(a, c.head_dim, grid, st);
+    case kCache8: launch_kind<kCache8, STORE, T>(a, c.head_dim, grid, st); break;
+    case kCacheFragments: launch_kind<kCacheFragments, STORE, T>(a, c.head_dim, grid, st); break;
+    case kCacheBf16: launch_kind<kCacheBf16, STORE, T>(a, c.head_dim, grid, st); break;
+    default: launch_kind<kCacheF32, STORE, T>(a, c.head_dim, grid, st);
     }
     HIP_TRY(hipGetLastError());
     return ANPD_OK;
+}
+template <bool STORE>
+int32_t launch_rows(const RowsArgs &a, const CacheShape &c, int32_t dtype, hipStream_t st)
+{
+    return dtype == ANPD_F32 ? launch_rows<STORE, float>(a, c, st) : launch_rows<STORE, bf16_t>(a, c, st);
 }
 
 template <int KIND>
@@ -121,7 +125,7 @@ int32_t copy_rows8(const anpd_kv *kv, int32_t layer, int32_t pos0, int32_t n, fl
     const int64_t width = (int64_t)kv->shape.n_kv_heads * kv->shape.head_dim;
     const int32_t rc = gather("anpd_kv_read/write", &kv, 1, &n, &pos0, layer, k, width, v, width, ANPD_F32, to_cache, a);
     if (rc != ANPD_OK) return rc;
-    return to_cache ? launch_rows<true>(a, kv->shape, st) : launch_rows<false>(a, kv->shape, st);
+    return to_cache ? launch_rows<true>(a, kv->shape, ANPD_F32, st) : launch_rows<false>(a, kv->shape, ANPD_F32, st);
 }
 
 }  // namespace anpd
@@ -155,7 +159,7 @@ int32_t anpd_kv_store(anpd_kv_t *const *kvs, int32_t n_seq, const int32_t *n_row
             if ((rc = ensure_pages(kv, v.pos0 + v.n, st)) != ANPD_OK) break;
         }
     }
-    if (rc == ANPD_OK) rc = launch_rows<true>(a, c, st);
+    if (rc == ANPD_OK) rc = launch_rows<true>(a, c, dtype, st);
     if (wait) HIP_TRY(hipStreamSynchronize(st));
     return rc;
 }
@@ -169,7 +173,7 @@ int32_t anpd_kv_load(const anpd_kv_t *const *kvs, int32_t n_seq, const int32_t *
     if (rc != ANPD_OK || a.n_spans == 0) return rc;
     OnDevice on;
     if ((rc = on.enter(who, kvs[0]->device)) != ANPD_OK) return rc;
-    return launch_rows<false>(a, kvs[0]->shape, (hipStream_t)stream);
+    return launch_rows<false>(a, kvs[0]->shape, dtype, (hipStream_t)stream);
 }
 
 int32_t anpd_kv_commit(anpd_kv_t *kv, const int32_t *rows, int32_t n, void *stream)

@@ -108,12 +108,12 @@ __device__ __forceinline__ unsigned long long shuffle64(unsigned long long v, in
     return ((unsigned long long)(uint32_t)__shfl((int)(v >> 32), from, 64) << 32) | (uint32_t)__shfl((int)v, from, 64);
 }
 // The tree of a sequence's new rows, for the lane's row.  Lane l looks at new row l: in step i it has the nearest 2^i of its ancestors, and takes over
-// those of the last one of them.  A parent that is not an earlier row is none: the row follows the cached positions.  depth: LDS,
-// kTreeRows numbers, the same from every wave that writes them.
-__device__ __forceinline__ void tree_info(const AttnArgs &a, const SeqView &s, int pre, int *depth, RowInfo &r)
+// those of the last one of them.  A parent that is not an earlier row is none: the row follows the cached positions.  up: what parent_of says, requested
+// before; depth: LDS, kTreeRows numbers, the same from every wave that writes them.
+__device__ __forceinline__ int parent_of(const AttnArgs &a, const SeqView &s) { return (int)(threadIdx.x & 63) < s.n ? a.parent[s.row0 + (threadIdx.x & 63)] : -1; }
+__device__ __forceinline__ void tree_info(const AttnArgs &a, const SeqView &s, int pre, int up, int *depth, RowInfo &r)
 {
     const int lane = threadIdx.x & 63;
-    int up = lane < s.n ? a.parent[s.row0 + lane] : -1;
     if (up < 0 || up >= lane) up = -1;
     unsigned long long chain = 1ull << lane;
 #pragma unroll
