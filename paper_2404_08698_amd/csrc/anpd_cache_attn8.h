@@ -6,7 +6,7 @@
 // of a conversion to fp32 at a quarter of the rate, a tile took three times as long, and tokens were bound by that and not by the cache's bytes.
 // What fp16 lacks is range.  Rows are scaled by powers of two, so that their largest number is below 2^15 (numbers 2^29 below it are exact, others off by 2^-40 of it); rows of
 // fp32 are two terms, 22 bits.  Weights carry their value's scale, p_rj s'_j, and a row's reference follows the largest of both, so that they are below 2^15: one term
-// is within 2^-12 of a weight (where the output's own rounding to bf16 makes 2^-9), two within 2^-23.  A key whose values are 2^20 times smaller than those of another
+// is within 2^-11 of a weight (where the output's own rounding to bf16 makes 2^-8), two within 2^-22.  A key whose values are 2^20 times smaller than those of another
 // that the row sees begins to lose digits.
 #pragma once
 #include "anpd_cache_softmax.h"

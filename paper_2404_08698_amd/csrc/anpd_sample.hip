@@ -83,9 +83,9 @@ int32_t anpd_sample(const void *logits, int64_t ld, int32_t dtype, int32_t rows,
     a.wide = ((uintptr_t)logits & (a.f32 ? 15 : 7)) == 0 && ld % 4 == 0;
     a.n_slices = slices_of(vocab);
     a.slice_shift = slice_shift(vocab);
-    // (a row's weights add up to less than 2^62)
+    // (a row's weights add up to 2^62 at most)
     a.shift = 51;
-    while (((uint64_t)vocab << a.shift) > (1ull << 62)) --a.shift;
+    while ((1ull << (62 - a.shift)) < (uint64_t)vocab) --a.shift;
     const size_t need = anpd_sample_workspace_bytes(rows, vocab);
     if (need > 0) {
         if (!workspace || ((uintptr_t)workspace & 255) != 0) return fail(ANPD_E_INVAL, "%s: workspace must be a 256-byte aligned device buffer", who);

@@ -1,0 +1,278 @@
+"""Caches of 8-bit keys and values: rows written and read back (into caches of every type), attention over them, the commit of a tree's rows."""
+import math
+import random
+
+import pytest
+import torch
+
+from cache_reference import rows_like
+from draft_reference import Caches, check_attention, codes, empty, held, random_tree
+from paper_2404_08698_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+
+BF16, F32 = torch.bfloat16, torch.float32
+KINDS = [("int8", 16), ("bf16", 16), ("bf16", 32), ("f32", 8), ("f32", 64)]
+
+
+def rows_of(n, width, dtype, seed=0, pitch=0, std=1.0):
+    gen = torch.Generator().manual_seed(seed)
+    return (torch.randn(n, max(width, pitch), generator=gen) * std).to(dtype).cuda()[:, :width]
+
+
+@pytest.mark.parametrize("kind", KINDS, ids=str)
+@pytest.mark.parametrize("rows", [BF16, F32])
+@pytest.mark.parametrize("kv_heads,dim", [(3, 64), (2, 128)])
+@pytest.mark.parametrize("pos0,n", [(0, 1), (0, 16), (5, 3), (15, 2), (16, 17), (31, 100), (7, 500)])
+def test_rows_come_back_as_the_cache_holds_them(kind, rows, kv_heads, dim, pos0, n):
+    kv = empty(2, kv_heads, kv_heads, dim, 640, kind[0], kind[1])
+    width = kv_heads * dim
+    # what lies around stays
+    around = rows_of(pos0 + n + 9, width, F32, 9)
+    kv.write(1, 0, around, around)
+    k, v = rows_of(n, width, rows, 1), rows_of(n, width, rows, 2, std=30.0)
+    B.store(kv, 1, k, v, pos0=[pos0])
+    for dtype in (F32, BF16):
+        got = B.load(kv, 1, [n], pos0=[pos0], dtype=dtype)
+        for have, gave in zip(got, (k, v)):
+            want = held(gave.float().cpu(), kv_heads, kind[0])
+            assert torch.equal(have.cpu(), want.to(dtype))
+    whole = kv.read(1, 0, pos0 + n + 9)
+    for have, gave in zip(whole, (k, v)):
+        want = held(around.cpu(), kv_heads, kind[0])
+        want[pos0:pos0 + n] = held(gave.float().cpu(), kv_heads, kind[0])
+        assert torch.equal(have.cpu(), want)
+    untouched = kv.read(0, 0, pos0 + n + 9)
+    assert not untouched[0].any() and not untouched[1].any()
+
+
+def test_codes_next_to_the_middle_between_two():
+    """Values that are, or nearly are, (c + 1/2) max / 127: ties go to the even code, the others to the nearer."""
+    for seed, top in enumerate((127.0, 254.0, 1.0, 3.0, 0.1, 1.9921875, 1e-30, 7e30)):
+        t = torch.tensor(top)
+        c = torch.arange(-127, 127, dtype=torch.float64) + 0.5
+        mid = (c * t.double() / 127.0).float()
+        x = torch.cat([mid, torch.nextafter(mid, torch.tensor(math.inf)), torch.nextafter(mid, torch.tensor(-math.inf))])
+        x = x[x.abs() <= t]
+        rows = -(-len(x) // 127)
+        full = torch.zeros(rows, 128)
+        full[:, :127].reshape(-1)[:] = 0
+        for r in range(rows):
+            part = x[127 * r:127 * (r + 1)]
+            full[r, 1:1 + len(part)] = part
+            full[r, 0] = t if r % 2 else -t
+        kv = empty(1, 1, 1, 128, 64, "int8")
+        B.store(kv, 0, full.cuda(), full.flip(1).contiguous().cuda())
+        k, v = kv.read(0, 0, rows)
+        assert torch.equal(k.cpu(), held(full, 1, "int8")), top
+        assert torch.equal(v.cpu(), held(full.flip(1), 1, "int8")), top
+        want, scale = codes(full)
+        # half a step, and of a code of up to 127 steps twice 2^-24: the scale's own rounding and the product's
+        assert want.abs().max() == 127 and (k.cpu().double() - full.double()).abs().max() <= scale.max().double() * (0.5 + 254 * 2.0 ** -24)
+
+
+@pytest.mark.parametrize("rows", [BF16, F32])
+def test_extreme_rows(rows):
+    """Zeros, the type's smallest and largest numbers, infinities and NaN: a position's own head alone is touched by them."""
+    kv = empty(1, 3, 3, 64, 64, "int8")
+    k = rows_of(40, 192, rows, 4).float().cpu()
+    tiny = torch.finfo(rows).tiny
+    for i, x in enumerate((0.0, tiny, -tiny, 2 * tiny, torch.finfo(rows).max, -torch.finfo(rows).max, math.inf, -math.inf, math.nan)):
+        k[i, 64:128] = x if i % 2 else torch.where(torch.arange(64) % 3 == 0, torch.tensor(x), torch.tensor(0.0))
+        k[i + 10, 70] = x
+    given = k.to(rows)
+    B.store(kv, 0, given.cuda(), given.flip(0).contiguous().cuda())
+    back = kv.read(0, 0, 40)
+    for have, gave in zip(back, (given, given.flip(0))):
+        want = held(gave.float(), 3, "int8")
+        assert torch.equal(have.cpu().isnan(), want.isnan())
+        assert torch.equal(have.cpu().nan_to_num(0.0), want.nan_to_num(0.0))
+
+
+@pytest.mark.parametrize("kind", KINDS, ids=str)
+def test_strides_sequences_and_streams(kind):
+    spans = [(3, 5), (0, 0), (40, 33), (0, 1), (15, 1)]
+    kvs = [empty(1, 4, 2, 64, 128, kind[0], kind[1], seed=i) for i in range(len(spans))]
+    n = sum(c for _, c in spans)
+    for rows, pitch in ((BF16, 131), (F32, 130), (F32, 128)):
+        k, v = rows_of(n, 128, rows, 1, pitch), rows_of(n, 128, rows, 2, pitch + 8)
+        other = torch.cuda.Stream()
+        other.wait_stream(torch.cuda.current_stream())
+        B.store(kvs, 0, k, v, n_rows=[c for _, c in spans], pos0=[p for p, _ in spans], stream=other)
+        other.synchronize()
+        into = torch.full((n, 140), 5.0, dtype=rows, device="cuda")
+        gk, gv = B.load(kvs, 0, [c for _, c in spans], pos0=[p for p, _ in spans], k=into[:, 3:131], v=torch.empty(n, 128, dtype=rows, device="cuda"))
+        assert torch.equal(gk.cpu(), held(k.float().cpu(), 2, kind[0]).to(rows)) and torch.equal(gv.cpu(), held(v.float().cpu(), 2, kind[0]).to(rows))
+        assert (into[:, :3] == 5).all() and (into[:, 131:] == 5).all()
+    # the same cache twice may be read
+    a, b = B.load([kvs[2], kvs[2]], 0, [3, 3], pos0=[40, 41])
+    assert torch.equal(a[1], a[3]) and torch.equal(b[2], b[4])
+    # no rows at all
+    B.store(kvs, 0, k[:0], v[:0], n_rows=[0] * 5)
+
+
+def test_a_captured_step():
+    """Store, attention and load recorded into a graph: replays see the rows that are there then.  Pages are not added while a stream is captured."""
+    kv = empty(1, 8, 8, 128, 256, "int8")
+    k0, v0 = rows_of(101, 1024, F32, 1), rows_of(101, 1024, F32, 2)
+    kv.write(0, 0, k0, v0)
+    kv.truncate(100)
+    k, v, q = (rows_of(1, 1024, BF16, s) for s in (3, 4, 5))
+    out, back = torch.empty_like(q), (torch.empty_like(k), torch.empty_like(v))
+    ws = torch.empty(8 << 20, dtype=torch.uint8, device="cuda")
+
+    def step():
+        B.store(kv, 0, k, v)
+        B.attention(kv, 0, q, out=out, workspace=ws)
+        B.load(kv, 0, [1], k=back[0], v=back[1])
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for seed in range(4):
+        for t, s in ((k, 10), (v, 20), (q, 30)):
+            t.copy_(rows_of(1, 1024, BF16, s + seed))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = out.clone()
+        assert torch.equal(back[0].cpu(), held(k.float().cpu(), 8, "int8").to(BF16))
+        step()
+        torch.cuda.synchronize()
+        assert torch.equal(got, out)
+    fresh = empty(1, 8, 8, 128, 256, "int8")
+    with torch.cuda.graph(torch.cuda.CUDAGraph()):
+        with pytest.raises(B.AnpdError) as e:
+            B.store(fresh, 0, k, v)
+        out.zero_()
+    assert e.value.code == B.E_INVAL
+    B.store(fresh, 0, k, v)
+    assert torch.equal(fresh.read(0, 0, 1)[0].cpu(), held(k.float().cpu(), 8, "int8"))
+
+
+# --------------------------------------------------------------------------------- attention over them
+
+def attend(filled, q, spans, **rules):
+    r = {k: v for k, v in rules.items() if v is not None}
+    out, lse = B.attention(filled.kvs, 0, q, n_rows=[n for _, n in spans], pos0=[p for p, _ in spans], rules=B.AttentionRules(**r), want_lse=True)
+    check_attention(filled, q, spans, out, lse, **rules)
+    return out, lse
+
+
+@pytest.mark.parametrize("rows", [BF16, F32])
+@pytest.mark.parametrize("heads,kv_heads,dim", [(4, 4, 128), (6, 2, 64), (32, 2, 128), (5, 1, 64)])
+@pytest.mark.parametrize("spans", [[(0, 1)], [(15, 1)], [(127, 2)], [(128, 33)], [(0, 150)], [(1000, 1)], [(9000, 3)], [(100, 1), (0, 0), (513, 5), (0, 40)]], ids=str)
+def test_attention_on_8_bits(rows, heads, kv_heads, dim, spans):
+    filled = Caches(heads, kv_heads, dim, [p + n for p, n in spans], dtype="int8", seed=dim)
+    attend(filled, rows_like(filled, sum(n for _, n in spans), rows), spans)
+
+
+@pytest.mark.parametrize("rows", [BF16, F32])
+@pytest.mark.parametrize("rule", [dict(window=1), dict(window=50, prefix=4), dict(prefix=300), dict(cap=30.0), dict(cap=400.0), dict(slopes=True), dict(first=True), dict(scale=0.5)], ids=str)
+def test_rules_on_8_bits(rows, rule):
+    rule, spans = dict(rule), [(260, 40), (3, 70)]
+    filled = Caches(8, 2, 64, [p + n for p, n in spans], dtype="int8", seed=8)
+    if rule.pop("slopes", False):
+        rule["slopes"] = torch.tensor([2.0 ** (-h) for h in range(8)], device="cuda")
+    if rule.pop("first", False):
+        rule["first_key"] = torch.randint(0, 400, (110,), dtype=torch.int32, generator=torch.Generator().manual_seed(1)).cuda()
+    attend(filled, rows_like(filled, 110, rows), spans, **rule)
+
+
+@pytest.mark.parametrize("rows", [BF16, F32])
+@pytest.mark.parametrize("std", [1e-25, 1e-6, 1e6, 1e25])
+def test_any_magnitude(rows, std):
+    """Keys and values far from 1 (queries so that scores are not): codes and fp16 operands have no range of their own."""
+    filled = Caches(4, 2, 128, [300], dtype="int8", std=std)
+    q = rows_like(filled, 9, F32)
+    q = (q / std).to(rows)
+    attend(filled, q, [(291, 9)])
+
+
+@pytest.mark.parametrize("rows", [BF16, F32])
+def test_some_values_are_larger_than_others(rows):
+    """Values of one position 2^12 times the others', that of another 2^12 smaller."""
+    filled = Caches(4, 4, 64, [200], dtype="int8")
+    filled.fill(0, 50, filled.k[0][50:51], filled.v[0][50:51] * 4096.0)
+    filled.fill(0, 60, filled.k[0][60:61], filled.v[0][60:61] / 4096.0)
+    attend(filled, rows_like(filled, 20, rows), [(180, 20)])
+    # (not seen: as if it were not there)
+    attend(filled, rows_like(filled, 20, rows), [(180, 20)], first_key=torch.full((20,), 61, dtype=torch.int32, device="cuda"))
+
+
+@pytest.mark.parametrize("rows", [BF16, F32])
+def test_rows_that_hold_no_numbers(rows):
+    filled = Caches(4, 2, 64, [140], dtype="int8")
+    q = rows_like(filled, 12, rows)
+    q[3, 70], q[5], q[7, 0] = math.nan, math.inf, 0.0
+    q[8] = 0.0
+    out, lse = B.attention(filled.kvs, 0, q, n_rows=[12], pos0=[128], want_lse=True)
+    assert out[3, 64:128].isnan().all() and out[5].isnan().all() and lse[3, 1].isnan()
+    fine = [0, 1, 2, 4, 6, 7, 8, 9, 10, 11]
+    assert out[fine].isfinite().all() and out[3, :64].isfinite().all()
+    # rows of zeros: the mean of the values
+    want = filled.v[0][:137].reshape(137, 2, 64).double().mean(0).repeat_interleave(2, 0).reshape(-1)
+    assert (out[8].cpu().double() - want).abs().max() <= 2.0 ** -8 * want.abs().max() + 2.0 ** -11
+
+
+def test_far_into_a_large_pool():
+    """Offsets beyond 2^32 bytes."""
+    kv = B.LayerCache(40, 32, 128, 1 << 14, n_kv_heads=32, dtype="int8")
+    assert kv.pool.numel() > 5 << 30
+    order = list(range(kv.num_pages))
+    kv.set_page_order(order[::-1])
+    k, v = rows_of(40, 4096, BF16, 1), rows_of(40, 4096, BF16, 2)
+    B.store(kv, 39, k, v)
+    gk, gv = B.load(kv, 39, [40])
+    assert torch.equal(gk.cpu(), held(k.float().cpu(), 32, "int8")) and torch.equal(gv.cpu(), held(v.float().cpu(), 32, "int8"))
+    q = rows_of(1, 4096, BF16, 3, std=2.0)
+    out = B.attention(kv, 39, q, pos0=[39])
+    small = empty(1, 32, 32, 128, 64, "int8")
+    B.store(small, 0, k, v)
+    assert torch.equal(out, B.attention(small, 0, q, pos0=[39]))
+
+
+def test_what_8_bit_caches_are_not_taken_for():
+    kv = empty(1, 4, 4, 64, 64, "int8")
+    kv.truncate(32)
+    q = rows_of(1, 256, BF16)
+    with pytest.raises(B.AnpdError) as e:
+        B.key_mass(kv, 0, q, torch.zeros(1, 4, device="cuda"), torch.zeros(4, 64, device="cuda"), pos0=[31])
+    assert e.value.code == B.E_UNIMPLEMENTED
+    with pytest.raises(B.AnpdError) as e:
+        B.evict(kv, torch.zeros(1, 4, 64, device="cuda"), 8)
+    assert e.value.code == B.E_UNIMPLEMENTED
+
+
+# ----------------------------------------------------------------------------------------------- commit
+
+@pytest.mark.parametrize("kind", KINDS, ids=str)
+@pytest.mark.parametrize("path", [[], [0], [0, 1, 2], [0, 5], [0, 2, 3, 17, 40, 63], [63], list(range(0, 64, 2)), list(range(64))], ids=lambda p: "%d" % len(p) + "".join("_%d" % i for i in p[1:3]))
+def test_commit_moves_the_path_together(kind, path):
+    kv = empty(3, 4, 2, 64, 128, kind[0], kind[1])
+    k, v = rows_of(110, 128, F32, 1), rows_of(110, 128, F32, 2)
+    for layer in range(3):
+        kv.write(layer, 0, k + layer, v - layer)
+    kv.truncate(45)
+    for layer in range(3):      # (what truncate has given up)
+        B.store(kv, layer, (k + layer)[45:109], (v - layer)[45:109])
+    before = [kv.read(layer, 0, 109) for layer in range(3)]
+    kv.commit(path)
+    assert kv.length == 45 + len(path)
+    for layer in range(3):
+        for have, had in zip(kv.read(layer, 0, kv.length), before[layer]):
+            assert torch.equal(have, had[list(range(45)) + [45 + p for p in path]])
+    # and goes on from there
+    B.store(kv, 0, k[:1], v[:1])
+    assert torch.equal(kv.read(0, kv.length, 1)[0].cpu(), held(k[:1].cpu(), 2, kind[0]))
+
+
+def test_commit_refuses():
+    kv = empty(1, 4, 4, 64, 64, "int8")
+    kv.truncate(20)
+    for rows, code in (([1, 1], B.E_INVAL), ([2, 1], B.E_INVAL), ([-1], B.E_INVAL), ([64], B.E_INVAL), ([0, 44], B.E_CAPACITY), ([0, 30], B.E_INVAL), (list(range(65)), B.E_INVAL)):
+        with pytest.raises(B.AnpdError) as e:
+            kv.commit(rows)
+        assert e.value.code == code, rows
+    assert kv.length == 20

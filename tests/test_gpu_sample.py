@@ -1,0 +1,205 @@
+"""Drawing tokens from logits, against 64 bits."""
+import math
+
+import pytest
+import torch
+
+from draft_reference import check_tokens, draw, kept_tokens
+from paper_2404_08698_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16 = torch.float32, torch.bfloat16
+
+
+def logits_of(rows, vocab, dtype=F32, seed=0, std=2.5, pitch=0):
+    gen = torch.Generator().manual_seed(seed)
+    x = torch.randn(rows, max(vocab, pitch), generator=gen) * std
+    at = torch.stack([torch.randperm(max(vocab, pitch), generator=gen)[:10] for _ in range(rows)])
+    x = x.scatter(1, at, 10.0 * torch.rand(at.shape, generator=gen))
+    return x.to(dtype).cuda()[:, :vocab]
+
+
+def run(x, rules, seed=0, u=None):
+    u = torch.rand(x.shape[0], generator=torch.Generator().manual_seed(seed)).cuda() if u is None else u
+    token, logprob = B.sample(x, u, B.SamplingRules(**rules), want_logprob=True)
+    check_tokens(x, u, token, logprob, **rules)
+    return token, logprob
+
+
+RULES = [dict(), dict(temperature=0.3), dict(temperature=3.0), dict(top_k=1), dict(top_k=7), dict(top_k=60), dict(top_k=900), dict(top_p=0.0), dict(top_p=0.5), dict(top_p=0.95),
+         dict(top_p=0.99999), dict(min_p=0.1), dict(min_p=1.0), dict(temperature=0.0), dict(temperature=0.8, top_k=50, top_p=0.9, min_p=0.02),
+         dict(temperature=1.7, top_k=1500, top_p=0.8), dict(temperature=0.6, top_p=0.9, min_p=0.3), dict(temperature=2.0, top_p=0.97, min_p=1e-6)]
+
+
+@pytest.mark.parametrize("rule", RULES, ids=str)
+@pytest.mark.parametrize("vocab", [1, 2, 3, 31, 100, 1023, 4096, 4097, 8191, 8192, 8193, 32000, 65024, 65536, 65537, 131072])
+def test_vocabularies(vocab, rule):
+    for dtype, rows in ((F32, 3), (BF16, 2)):
+        run(logits_of(rows, vocab, dtype, vocab), rule, seed=vocab)
+
+
+@pytest.mark.parametrize("vocab", [262144, (1 << 20) - 5, 1 << 20])
+def test_the_largest_vocabularies(vocab):
+    x = logits_of(2, vocab, F32, 1)
+    for rule in (dict(), dict(top_p=0.9), dict(top_k=40, temperature=0.7), dict(min_p=0.01), dict(temperature=0.0)):
+        run(x, rule)
+
+
+def test_every_share_of_a_row():
+    """Random numbers all over [0, 1): every kept token is drawn, and no other, each in its share."""
+    x = logits_of(1, 500, F32, 5).expand(4096, 500).contiguous()
+    u = (torch.arange(4096) / 4096.0).cuda()
+    for rule in (dict(top_k=9), dict(top_p=0.7), dict(min_p=0.05)):
+        token, _ = run(x, rule, u=u)
+        at, w = kept_tokens(x[0].cpu().numpy(), rule.get("temperature", 1.0), rule.get("top_k", 0), rule.get("top_p", 1.0), rule.get("min_p", 0.0))
+        seen, count = token.cpu().unique(return_counts=True)
+        assert set(seen.tolist()) <= set(at.tolist())
+        share = {t: n / 4096 for t, n in zip(seen.tolist(), count.tolist())}
+        assert all(abs(share.get(t, 0.0) - p) <= 2 / 4096 for t, p in zip(at.tolist(), (w / w.sum()).tolist()))
+
+
+@pytest.mark.parametrize("vocab", [100, 4096, 9000, 70000])
+def test_equal_logits(vocab):
+    """Ties go to the lowest index: at the border of top_k, of the nucleus, among all."""
+    for x in (torch.zeros(4, vocab), (torch.arange(vocab) % 3).float().repeat(4, 1), (torch.arange(vocab) // 50 * 0.5).float().repeat(4, 1) * 0.01,
+              torch.where(torch.arange(vocab) % 7 == 0, 1.0, 0.9999999).repeat(4, 1)):
+        for rule in (dict(), dict(top_k=5), dict(top_k=vocab - 1), dict(top_k=vocab // 2 + 1), dict(top_p=0.5), dict(top_p=0.001), dict(temperature=0.0), dict(top_k=vocab // 2, top_p=0.3),
+                     dict(min_p=1.0), dict(temperature=100.0, top_p=0.9)):
+            u = torch.tensor([0.0, 0.25, 0.7, 0.9999999]).cuda()
+            run(x.cuda(), rule, u=u)
+
+
+@pytest.mark.parametrize("vocab", [9, 4096, 8200, 66000])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_logits_that_are_no_numbers(vocab, dtype):
+    x = logits_of(8, vocab, dtype, 3)
+    x[0] = -math.inf
+    x[1] = math.nan
+    x[2, :] = -math.inf
+    x[2, vocab - 1] = -5.0
+    x[3, vocab // 2] = math.inf
+    x[4, ::2] = math.inf
+    x[5, 1::3] = math.nan
+    x[6] = torch.finfo(dtype).max
+    x[7, : vocab // 2] = torch.finfo(dtype).min
+    for rule in (dict(), dict(top_k=3), dict(top_k=vocab), dict(top_p=0.8), dict(min_p=0.2), dict(temperature=0.0), dict(temperature=0.5, top_k=30, top_p=0.9, min_p=0.01)):
+        token, logprob = run(x, rule)
+        assert token[0] == -1 and token[1] == -1 and logprob[:2].isnan().all() and token[2] == vocab - 1 and token[3] == vocab // 2
+        assert token[4] % 2 == 0
+
+
+def test_random_numbers_outside_their_range():
+    for vocab in (50, 9000):
+        x = logits_of(6, vocab, F32, 2)
+        u = torch.tensor([-1.0, 1.0, 7.0, math.nan, math.inf, 1.0 - 2.0 ** -24]).cuda()
+        for rule in (dict(), dict(top_k=4), dict(top_p=0.9)):
+            token, _ = B.sample(x, u, B.SamplingRules(**rule), want_logprob=True)
+            for r, low in enumerate((True, False, False, True, False, False)):
+                at, w = kept_tokens(x[r].cpu().numpy(), 1.0, rule.get("top_k", 0), rule.get("top_p", 1.0), 0.0)
+                if low:
+                    assert token[r].item() == at[0]
+                else:
+                    # the last one; or, where its share is below what u leaves, one as near the end
+                    share = w[::-1].cumsum() / w.sum()
+                    assert token[r].item() in at[-1 - int((share < 1e-6).sum()):].tolist()
+
+
+@pytest.mark.parametrize("temperature", [1e-38, 1e-20, 1e-4, 2e-3, 1e4, 1e20, 3e38])
+@pytest.mark.parametrize("vocab", [60, 5000, 20000])
+def test_temperatures(vocab, temperature):
+    x = logits_of(3, vocab, F32, 8)
+    for rule in (dict(), dict(top_k=20), dict(top_p=0.6), dict(min_p=0.5), dict(top_p=0.9, min_p=0.9999)):
+        run(x, dict(rule, temperature=temperature))
+
+
+@pytest.mark.parametrize("std", [1e-30, 1e-3, 300.0, 1e30])
+def test_logits_of_any_size(std):
+    for vocab in (700, 33000):
+        x = logits_of(2, vocab, F32, 4) * std
+        for rule in (dict(), dict(top_k=70), dict(top_p=0.9), dict(min_p=0.3)):
+            run(x, rule)
+
+
+def test_rules_of_each_row():
+    rows = 300
+    for vocab in (777, 12345):
+        x = logits_of(rows, vocab, F32, 6)
+        gen = torch.Generator().manual_seed(0)
+        rules = dict(temperature=torch.rand(rows, generator=gen) * 2, top_k=torch.randint(-1, 90, (rows,), generator=gen, dtype=torch.int32), top_p=torch.rand(rows, generator=gen) * 1.2,
+                     min_p=torch.rand(rows, generator=gen) * 0.1)
+        rules["temperature"][::7] = 0.0
+        rules["temperature"][3] = math.nan
+        rules["top_p"][5], rules["min_p"][5], rules["top_p"][6], rules["min_p"][8] = math.nan, math.nan, -1.0, 4.0
+        on_gpu = {k: v.cuda() for k, v in rules.items()}
+        u = torch.rand(rows, generator=gen).cuda()
+        token, logprob = B.sample(x, u, B.SamplingRules(**on_gpu), want_logprob=True)
+        rules["top_p"] = rules["top_p"].nan_to_num(1.0)
+        rules["min_p"] = rules["min_p"].nan_to_num(0.0)
+        check_tokens(x, u, token, logprob, **rules)
+        # one by one, the same
+        for r in (0, 3, 5, 6, 7, 8, 255, 256, 299):
+            alone = B.sample(x[r:r + 1], u[r:r + 1], B.SamplingRules(**{k: v[r:r + 1].clone() for k, v in on_gpu.items()}))
+            assert alone.item() == token[r].item()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("vocab", [101, 8193, 40001])
+def test_strides_and_streams(vocab, dtype):
+    x = logits_of(5, vocab, dtype, 9, pitch=vocab + 3)
+    u = torch.rand(5, generator=torch.Generator().manual_seed(1)).cuda()
+    rules = B.SamplingRules(top_p=0.9)
+    token, _ = run(x, dict(top_p=0.9), u=u)
+    assert torch.equal(B.sample(x.contiguous(), u, rules), token)
+    other = torch.cuda.Stream()
+    other.wait_stream(torch.cuda.current_stream())
+    into = torch.empty(5, dtype=torch.int32, device="cuda")
+    B.sample(x, u, rules, tokens=into, stream=other)
+    other.synchronize()
+    assert torch.equal(into, token)
+
+
+@pytest.mark.parametrize("vocab", [2000, 32000])
+def test_captured_and_replayed(vocab):
+    x, u = logits_of(17, vocab, F32, 0), torch.rand(17).cuda()
+    rules = B.SamplingRules(temperature=0.9, top_p=0.95, min_p=0.01)
+    token, logprob = torch.empty(17, dtype=torch.int32, device="cuda"), torch.empty(17, device="cuda")
+    ws = torch.empty(max(256, B.sample_workspace_bytes(17, vocab)), dtype=torch.uint8, device="cuda")
+    B.sample(x, u, rules, tokens=token, logprob=logprob, workspace=ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        B.sample(x, u, rules, tokens=token, logprob=logprob, workspace=ws)
+    for seed in range(5):
+        x.copy_(logits_of(17, vocab, F32, 50 + seed))
+        u.copy_(torch.rand(17, generator=torch.Generator().manual_seed(seed)))
+        graph.replay()
+        torch.cuda.synchronize()
+        check_tokens(x, u, token, logprob, temperature=0.9, top_p=0.95, min_p=0.01)
+        again, also = B.sample(x, u, rules, want_logprob=True)
+        assert torch.equal(again, token) and torch.equal(also, logprob)
+
+
+def test_no_rows_and_refusals():
+    x = logits_of(2, 50)
+    u = torch.rand(2).cuda()
+    assert B.sample(x[:0], u[:0]).shape == (0,)
+    for rules in (dict(temperature=-1.0), dict(temperature=math.inf), dict(top_p=1.5), dict(top_p=-0.1), dict(min_p=2.0), dict(min_p=math.nan)):
+        with pytest.raises(B.AnpdError) as e:
+            B.sample(x, u, B.SamplingRules(**rules))
+        assert e.value.code == B.E_INVAL
+    with pytest.raises(ValueError):
+        B.SamplingRules(top_k=1 << 31)
+    with pytest.raises(ValueError):
+        B.sample(x, u[:1])
+    with pytest.raises(ValueError):
+        B.sample(x, u, B.SamplingRules(temperature=torch.ones(1, device="cuda")))
+    big = logits_of(2, 9000)
+    with pytest.raises(B.AnpdError) as e:
+        B.sample(big, u, workspace=torch.empty(256, dtype=torch.uint8, device="cuda"))
+    assert e.value.code == B.E_CAPACITY
+
+
+def test_the_reference_draws_as_a_sum_says():
+    assert draw(torch.tensor([0.0, math.log(2.0), 0.0]).numpy(), 0.3)[0] == 1
+    assert draw(torch.tensor([0.0, math.log(2.0), 0.0]).numpy(), 0.8)[0] == 2
