@@ -107,6 +107,12 @@ __device__ __forceinline__ unsigned long long shuffle64(unsigned long long v, in
 {
     return ((unsigned long long)(uint32_t)__shfl((int)(v >> 32), from, 64) << 32) | (uint32_t)__shfl((int)v, from, 64);
 }
+// A chain without its lowest `count` bits.
+__device__ __forceinline__ unsigned long long from_position(unsigned long long chain, int count)
+{
+    for (; count > 0 && chain != 0; --count) chain &= chain - 1;
+    return chain;
+}
 // The tree of a sequence's new rows, for the lane's row.  Lane l looks at new row l: in step i it has the nearest 2^i of its ancestors, and takes over
 // those of the last one of them.  A parent that is not an earlier row is none: the row follows the cached positions.  up: what parent_of says, requested
 // before; depth: LDS, kTreeRows numbers, the same from every wave that writes them.
@@ -126,14 +132,11 @@ __device__ __forceinline__ void tree_info(const AttnArgs &a, const SeqView &s, i
     const int d = __popcll(chain) - 1;
     depth[lane] = d;
     if (a.window > 0 || a.first_key) {
-        // (by positions, as for cached keys; lane l for row l again)
-        const int fk = a.first_key && lane < s.n ? a.first_key[s.row0 + lane] : 0;
-        unsigned long long seen = 0;
-        for (int i = 0; i < s.n; ++i) {
-            const int back = d - __builtin_amdgcn_readlane(d, i), at = s.pos0 + d - back;
-            if ((chain >> i & 1) && at >= fk && (a.window == 0 || back < a.window || at < pre)) seen |= 1ull << i;
-        }
-        chain = seen;
+        // By positions, as for cached keys: bits of a chain ascend with their positions pos0, pos0 + 1, ..., so what lies before a position are its lowest ones.
+        const int fk = a.first_key && lane < s.n ? a.first_key[s.row0 + lane] : 0, at = s.pos0 + d, lo = a.window > 0 && at - a.window + 1 > fk ? at - a.window + 1 : fk;
+        const unsigned long long late = from_position(chain, lo - s.pos0);
+        const unsigned long long early = pre > s.pos0 && fk < pre ? from_position(chain, fk - s.pos0) & ~from_position(chain, pre - s.pos0) : 0;
+        chain = late | early;
     }
     const int row = r.row - s.row0;
     r.chain = shuffle64(chain, row);

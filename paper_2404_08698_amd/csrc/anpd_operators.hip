@@ -2,6 +2,7 @@
 // anpd_cache_attn.h and anpd_cache_evict.h.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstring>
 
@@ -397,6 +398,8 @@ int32_t attend(const char *who, const anpd_kv *const *kvs, int32_t n_seq, const 
     a.ldo = ldo;
     a.lse = lse;
     a.q_wide = a.q_wide && ((uintptr_t)out & 15) == 0 && ldo % (a.q_f32 ? 4 : 8) == 0;
+    // (blocks of the last sequence begin first: the longest, so that what is left at the end is short.  32 tokens on 8-bit caches of 300 to 700 positions 38.6 -> @@ us)
+    std::stable_sort(a.seq, a.seq + a.n_seq, [](const SeqView &x, const SeqView &y) { return x.pos0 + x.n < y.pos0 + y.n; });
     const Plan p = plan_attention(a, c, kvs[0]->n_cu);
     if ((rc = workspace_of(who, a, p.part_bytes, workspace, workspace_bytes)) != ANPD_OK) return rc;
     OnDevice on;
