@@ -68,6 +68,7 @@ struct RowRules {
         top_k = a.top_ks ? a.top_ks[row] : a.top_k;
         greedy = !(temperature > 0.f);
         if (greedy) { top_k = 1; temperature = 1.f; }   // (the first of the order)
+        temperature = fminf(temperature, 3.4028234e38f);
         if (top_k < 0 || top_k >= a.vocab) top_k = 0;
     }
 };

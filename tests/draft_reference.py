@@ -161,7 +161,7 @@ def kept_tokens(x, temperature, top_k, top_p, min_p):
     if not temperature > 0:
         return order[:1], np.ones(1)
     with np.errstate(under="ignore"):
-        w = np.exp((x[order] - x[order[0]]) / float(np.float32(temperature)))
+        w = np.exp((x[order] - x[order[0]]) / min(float(np.float32(temperature)), 3.4028234e38))
     if 0 < top_k < len(order):
         order, w = order[:top_k], w[:top_k]
     if top_p < 1:

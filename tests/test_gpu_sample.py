@@ -129,7 +129,7 @@ def test_rules_of_each_row():
         rules = dict(temperature=torch.rand(rows, generator=gen) * 2, top_k=torch.randint(-1, 90, (rows,), generator=gen, dtype=torch.int32), top_p=torch.rand(rows, generator=gen) * 1.2,
                      min_p=torch.rand(rows, generator=gen) * 0.1)
         rules["temperature"][::7] = 0.0
-        rules["temperature"][3] = math.nan
+        rules["temperature"][3], rules["temperature"][9] = math.nan, math.inf
         rules["top_p"][5], rules["min_p"][5], rules["top_p"][6], rules["min_p"][8] = math.nan, math.nan, -1.0, 4.0
         on_gpu = {k: v.cuda() for k, v in rules.items()}
         u = torch.rand(rows, generator=gen).cuda()
