@@ -169,9 +169,9 @@ Plan plan_attention(AttnArgs &a, const CacheShape &c, int n_cu)
         // Two blocks for each compute unit, of at least two tiles: a tile is about 1.3 us, joining 2.5 (32 heads of 128, 1 / 32 rows behind
         // 1000 positions 9.1 / 11.3 us, a tile each 9.7 / 14.4).  Caches in plain order, whose tiles take four times that, a tile each, and one block
         // of heads of 128, which fill a unit's registers (fp32, 4 heads of 64, 8 rows behind 1000 16 -> 13, 32 of 128, a row behind 1000 23 -> 19).
-        // Caches of 8 bits the same, but two tiles are not split (32 heads of 128, a row / 32 rows behind 250 positions 9.6 / 10.6 -> 8.0 / 9.3); with two blocks
+        // Caches of 8 bits the same, but up to three tiles are not split (32 heads of 128, a row / 32 rows behind 250 positions 9.6 / 10.6 -> 8.0 / 9.3); with two blocks
         // for each unit and two tiles for each: behind 1000 9.8 / 12.6 -> 10.2 / 12.8, behind 16000 30.1 / 31.0 -> 31.0 / 32.5.
-        const int per_unit = c.fragments || c.head_dim == 64 ? 2 : 1, least = c.fragments || (c.dtype == ANPD_INT8 && longest <= 2) ? 2 : 1;
+        const int per_unit = c.fragments || c.head_dim == 64 ? 2 : 1, least = c.fragments || (c.dtype == ANPD_INT8 && longest <= 3) ? 2 : 1;
         splits = items > 0 ? per_unit * n_cu / items : 1;
         if (splits > longest / least) splits = longest / least;
         if (splits < 1) splits = 1;
