@@ -467,7 +467,7 @@ int32_t anpd_kv_evict(const anpd_kv_t *src, anpd_kv_t *dst, const float *mass, i
  * while the stream is captured (ANPD_E_INVAL): grow the cache before (anpd_kv_truncate), and the call may be captured. */
 int32_t anpd_kv_store(anpd_kv_t *const *kvs, int32_t n_seq, const int32_t *n_rows, const int32_t *pos0, int32_t layer, const void *k, int64_t ldk,
                       const void *v, int64_t ldv, int32_t dtype, void *stream);
-/* ... and back: what the caches hold at those positions, rounded once to dtype.  One cache may occur twice.  Asynchronous on stream; may be captured.
+/* ... and back: what the caches hold at those positions, rounded once to dtype; k and v share no element.  One cache may occur twice.  Asynchronous on stream; may be captured.
  * Both: ANPD_E_CAPACITY (positions), ANPD_E_INVAL (load: also a position without a page), ANPD_E_HIP. */
 int32_t anpd_kv_load(const anpd_kv_t *const *kvs, int32_t n_seq, const int32_t *n_rows, const int32_t *pos0, int32_t layer, void *k, int64_t ldk,
                      void *v, int64_t ldv, int32_t dtype, void *stream);
@@ -501,7 +501,8 @@ int32_t anpd_kv_commit(anpd_kv_t *kv, const int32_t *rows, int32_t n, void *stre
  *   the first top_k of them; of these, those before which less than top_p of their weights' sum has been added up; of these, those with w_i >= min_p.
  * The first token is always among them.  A NULL pointer in place of the struct: temperature 1, all tokens.
  * Arrays (DEVICE, one number per row, or NULL) take the place of the numbers; what they hold is read as the numbers are, values that those may not have
- * as follows: a temperature that is not above 0 is 0, an infinite one the largest number, top_k below 1 and top_p above 1 or NaN are none, top_p below 0 is 0, min_p above 1 is 1, below 0 or NaN 0. */
+ * as follows: a temperature that is not above 0 is 0, an infinite one the largest number; top_k below 1 and top_p above 1 or NaN are none, top_p below 0
+ * is 0; min_p above 1 is 1, below 0 or NaN 0. */
 typedef struct {
     float temperature;           /* finite, >= 0; 0: the largest logit's token, the lowest index among equal ones */
     int32_t top_k;               /* 0 = all */

@@ -441,6 +441,8 @@ class KVCache:
 
     def commit(self, rows: Sequence[int], stream=None) -> None:
         """anpd_kv_commit: the rows of a tree that were accepted (a path from the root) move together behind the committed positions."""
+        if any(not -1 << 31 <= r < 1 << 31 for r in rows):     # (the array would take their last 32 bits)
+            raise ValueError("rows of a tree")
         _check(lib().anpd_kv_commit(self._h, _ints(rows), len(rows), _stream_of(self.pool.device, stream)))
 
     def observe(self, mass, rows: int = 32) -> None:
@@ -789,7 +791,7 @@ def _span_of(kvs, n_rows, pos0):
     if isinstance(kvs, KVCache):
         kvs = (kvs,)
     n = len(kvs)
-    if n == 0 or len(n_rows) != n or min(n_rows) < 0:
+    if n == 0 or len(n_rows) != n or min(n_rows) < 0 or max(n_rows) >= 1 << 31:
         raise ValueError("n_rows: one number per cache")
     if pos0 is not None and (len(pos0) != n or max(pos0) >= 1 << 31 or min(pos0) < 0):
         raise ValueError("pos0: one position per sequence")

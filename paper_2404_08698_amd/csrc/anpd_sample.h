@@ -783,7 +783,7 @@ struct RowSampler {
         const double to = goal(sum);
         // (one that has any: the first whose sum with those before it is above the goal, or the last)
         const whole_t some = __builtin_amdgcn_ballot_w64(of > 0.0), above = __builtin_amdgcn_ballot_w64(of > 0.0 && upto > to);
-        const int slice = above ? __builtin_ctzll(above) : 63 - __builtin_clzll(some);
+        const int slice = above ? __builtin_ctzll(above) : 63 - __builtin_clzll(some | 1);
         const double start = upto - of;
         const double before = __longlong_as_double(((long long)__builtin_amdgcn_readlane((int)(__double_as_longlong(start) >> 32), slice) << 32) |
                                                    (uint32_t)__builtin_amdgcn_readlane((int)__double_as_longlong(start), slice));

@@ -276,3 +276,13 @@ def test_commit_refuses():
             kv.commit(rows)
         assert e.value.code == code, rows
     assert kv.length == 20
+
+
+def test_numbers_beyond_32_bits():
+    kv = empty(1, 4, 4, 64, 64, "int8")
+    kv.truncate(20)
+    k = rows_of(1, 256, BF16)
+    for call in (lambda: kv.commit([0, 1 << 32]), lambda: B.store(kv, 0, k, k, n_rows=[(1 << 32) + 1]), lambda: B.load(kv, 0, [(1 << 32) + 1], pos0=[0])):
+        with pytest.raises(ValueError):
+            call()
+    assert kv.length == 20
