@@ -795,7 +795,7 @@ def _span_of(kvs, n_rows, pos0):
         raise ValueError("n_rows: one number per cache")
     if pos0 is not None and (len(pos0) != n or max(pos0) >= 1 << 31 or min(pos0) < 0):
         raise ValueError("pos0: one position per sequence")
-    return kvs, n, (C.c_void_p * n)(*[kv._h.value for kv in kvs]), (C.c_int32 * n)(*n_rows), None if pos0 is None else (C.c_int32 * n)(*pos0)
+    return kvs, n, (C.c_void_p * n)(*[kv._h for kv in kvs]), (C.c_int32 * n)(*n_rows), None if pos0 is None else (C.c_int32 * n)(*pos0)
 
 
 def _check_rows(t, rows: int, kv, dtype) -> None:
@@ -816,7 +816,7 @@ def store(kvs, layer: int, k, v, n_rows: Optional[Sequence[int]] = None, pos0: O
     kvs, n, handles, counts, at = _span_of(kvs, n_rows, pos0)
     if k.dtype not in (torch.float32, torch.bfloat16):
         raise ValueError("k and v must be float32 or bfloat16")
-    rows = sum(counts)
+    rows = sum(n_rows)
     for t in (k, v):
         _check_rows(t, rows, kvs[0], k.dtype)
     _check(lib().anpd_kv_store(handles, n, counts, at, layer, k.data_ptr(), _pitch(k), v.data_ptr(), _pitch(v), F32 if k.dtype == torch.float32 else BF16,
@@ -832,7 +832,7 @@ def load(kvs, layer: int, n_rows: Sequence[int], pos0: Optional[Sequence[int]] =
         dtype = torch.float32 if k is None else k.dtype
     if dtype not in (torch.float32, torch.bfloat16):
         raise ValueError("dtype must be float32 or bfloat16")
-    rows, first = sum(counts), kvs[0]
+    rows, first = sum(n_rows), kvs[0]
     shape = (rows, first.n_kv_heads * first.model.shape.head_dim)
     k, v = (_empty(shape, dtype, first.pool.device, stream) if t is None else t for t in (k, v))
     for t in (k, v):
