@@ -80,6 +80,12 @@ struct RowInfo {
     unsigned long long chain;    // which of these the row sees, a bit each,
     const int *depth;            // and how many ancestors each of them has
 };
+// (a number below 0 is 0: differences of it and positions stay in 32 bits)
+__device__ __forceinline__ int first_key_of(const AttnArgs &a, int row)
+{
+    const int fk = a.first_key ? a.first_key[row] : 0;
+    return fk > 0 ? fk : 0;
+}
 template <int RULES>
 __device__ __forceinline__ RowInfo row_info(const AttnArgs &a, const SeqView &s, int kvh, int v0)
 {
@@ -96,7 +102,7 @@ __device__ __forceinline__ RowInfo row_info(const AttnArgs &a, const SeqView &s,
     r.slope = 0.f;
     if (RULES) {
         if (a.slopes) r.slope = a.slopes[r.head];
-        if (a.first_key) r.fk = a.first_key[r.row];
+        r.fk = first_key_of(a, r.row);
         r.lo = r.fk;
         if (a.window > 0) { const int lo = r.p - a.window + 1; r.lo = lo > r.fk ? lo : r.fk; }
     }
@@ -134,7 +140,7 @@ __device__ __forceinline__ void tree_info(const AttnArgs &a, const SeqView &s, i
     depth[lane] = d;
     if (a.window > 0 || a.first_key) {
         // By positions, as for cached keys: bits of a chain ascend with their positions pos0, pos0 + 1, ..., so what lies before a position are its lowest ones.
-        const int fk = a.first_key && lane < s.n ? a.first_key[s.row0 + lane] : 0, at = s.pos0 + d, lo = a.window > 0 && at - a.window + 1 > fk ? at - a.window + 1 : fk;
+        const int fk = lane < s.n ? first_key_of(a, s.row0 + lane) : 0, at = s.pos0 + d, lo = a.window > 0 && at - a.window + 1 > fk ? at - a.window + 1 : fk;
         const unsigned long long late = from_position(chain, lo - s.pos0);
         const unsigned long long early = pre > s.pos0 && fk < pre ? from_position(chain, fk - s.pos0) & ~from_position(chain, pre - s.pos0) : 0;
         chain = late | early;

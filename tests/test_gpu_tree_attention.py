@@ -175,3 +175,18 @@ def test_the_model_s_own_tree_step_is_this():
         alone, lse = B.attention(one.kvs, 0, q[branch].contiguous(), n_rows=[len(branch)], pos0=[100], want_lse=True)
         check_attention(one, q[branch], [(100, len(branch))], alone, lse)
         assert (alone.float() - full[branch].float()).abs().max() <= 2.0 ** -6 * full.float().abs().max()
+
+
+@pytest.mark.parametrize("form", FORMS, ids=IDS)
+@pytest.mark.parametrize("tree", [False, True], ids=["rows", "tree"])
+def test_first_keys_at_the_ends_of_32_bits(form, tree):
+    spans = [(150, 29), (0, 9), (333, 64)]
+    filled, q = make(form, 8, 4, 64, spans, seed=4)
+    rng = random.Random(6)
+    first = torch.tensor([rng.choice((-(1 << 31), -(1 << 31) + 200, -1, 0, 152, (1 << 31) - 1)) for _ in range(102)], dtype=torch.int32, device="cuda")
+    for rule in (dict(first_key=first), dict(first_key=first, window=40, prefix=20), dict(first_key=first, window=(1 << 31) - 1)):
+        if tree:
+            run(filled, q, spans, [random_tree(n, rng) for _, n in spans], **rule)
+        else:
+            out, lse = B.attention(filled.kvs, 0, q, n_rows=[n for _, n in spans], pos0=[p for p, _ in spans], rules=B.AttentionRules(**rule), want_lse=True)
+            check_attention(filled, q, spans, out, lse, **rule)
