@@ -11,7 +11,7 @@ namespace anpd {
 // while the keys go by: a wave's loads are the operands, the next keys are requested when this tile's scores are done, its values
 // when its output is, and the waves meet at the end.  This is the form of single tokens, of windows, of prompts whose larger blocks
 // would leave compute units without one, and of scores with caps and biases.
-// A token or a window is bound by the cache's bytes: 32 tokens of 32 sequences, 271 MB in 54 us (5.0 TB/s), one behind 65535 positions of 8 key heads,
+// A token or a window is bound by the cache's bytes: 32 tokens of 32 sequences, 271 MB in 51 us (5.4 TB/s), one behind 65535 positions of 8 key heads,
 // 268 MB in 49 us (5.5); 17 rows behind 2048, 34 MB in 14 us, are start, three tiles one after the other and end.  A prompt is bound by L2: every
 // block reads its keys for 32 rows (512 rows of 32 heads 11 us, 0.19 PFLOP/s).  fp32 rows: three times the matrix instructions; their terms lie in LDS
 // once for the four waves, which leaves a wave 192 registers, not 350, and a SIMD two of them: 512 rows 22 -> 15 us, packed documents 49 -> 26.
