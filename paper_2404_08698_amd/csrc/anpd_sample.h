@@ -352,7 +352,8 @@ struct RowSampler {
     }
     __device__ __forceinline__ bool inside(float v, int i) const { return v > border || (v == border && i <= last && v > -INFINITY); }
 
-    // The first of kSampleBins numbers, one for each thread, whose sum with those before it reaches `want` (none: the last); before: their sum.
+    // The first of kSampleBins numbers, one for each thread, whose sum with those before it reaches `want` (none: the last); before: their sum.  One that is above 0: sums of
+    // 64-bit floating point are formed in another order for every lane, so that a 0 may come out above what lies before it.
     template <typename N>
     __device__ __forceinline__ int first_to_reach(N mine, N want, N &before)
     {
@@ -368,9 +369,9 @@ struct RowSampler {
             if (i == wave) first = now;
             now += parts[i];
         }
-        const whole_t reach = __builtin_amdgcn_ballot_w64(first + upto >= want);
-        const bool here = first < want && first + parts[wave] >= want;   // (one wave's: the next one's first is this sum)
-        if (here ? lane == (reach ? __builtin_ctzll(reach) : 63) : now < want && threadIdx.x == kRowThreads - 1) {
+        const whole_t some = __builtin_amdgcn_ballot_w64(mine > 0), reach = some & __builtin_amdgcn_ballot_w64(first + upto >= want);
+        const bool here = first < want && first + parts[wave] >= want;   // (one wave's: the next one's first is this sum; it has numbers above 0)
+        if (here ? lane == (reach ? __builtin_ctzll(reach) : 63 - __builtin_clzll(some | 1)) : now < want && threadIdx.x == kRowThreads - 1) {
             s.at = threadIdx.x;
             *prev = first + (upto - mine);
         }
