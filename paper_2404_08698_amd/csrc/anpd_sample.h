@@ -537,8 +537,8 @@ struct RowSampler {
             lo = low;
             hi = high;
         }
-        // all are equal: so many of them, by index
-        const whole_t one = amount<MASS>(lo), count = one ? (want + one - 1) / one : 1;
+        // all are equal: so many of them, by index (where rounding asks for more than there are: all)
+        const whole_t one = amount<MASS>(lo), some = one ? (want + one - 1) / one : 1;
         const float old = border;
         const int end = last;
         auto equal = [&](float v, int i) __attribute__((always_inline)) { return v == lo && (lo > old || i <= end); };
@@ -548,10 +548,12 @@ struct RowSampler {
             if (equal(v, i)) atomicAdd(&s.more[i >> a.slice_shift], (whole_t)1);
         });
         __syncthreads();
-        whole_t before;
+        whole_t before, all = 0;
+        for (int i = 0; i < a.n_slices; ++i) all += s.more[i];
+        const whole_t count = some < all ? some : all;
         const int slice = first_to_reach<whole_t>((int)threadIdx.x < a.n_slices ? s.more[threadIdx.x] : 0, count, before);
         border = lo;
-        last = place_in(slice < a.n_slices ? slice : a.n_slices - 1, count - before, [&](float v, int i) __attribute__((always_inline)) { return equal(v, i) ? (whole_t)1 : (whole_t)0; });
+        last = place_in(slice, count - before, [&](float v, int i) __attribute__((always_inline)) { return equal(v, i) ? (whole_t)1 : (whole_t)0; });
     }
     // In a slice: the first index at which numbers f(logit, index), added up, reach `want` (at least 1; or all of them, where rounding leaves them short of it).
     template <typename F>

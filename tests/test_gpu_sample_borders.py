@@ -69,3 +69,20 @@ def test_half_of_a_row_is_not_reached_in_an_empty_interval(seed):
     token, logprob = B.sample(logits, u, B.SamplingRules(top_p=0.5), want_logprob=True)
     check_rows(logits, u, token, logprob, top_p=0.5)
     assert ((token >= len(behind)) & (token < n)).sum() >= 4     # (the largest of those behind may be kept: the sum of the others is half but for a rounding)
+
+
+def test_more_weight_than_equal_logits_have():
+    """Sums of slices are of their own largest logit's resolution, the border's of the row's: a million equal logits of 1000.49 steps each are 1000.49 in the sums that say where
+    top_p ends, and 1000 where they are counted, so that more of them are wanted than there are.  All of them stay, and the last slice, which has none, takes no part."""
+    vocab = 1 << 20
+    x = torch.full((3, vocab), float(TOP) + math.log(1000.49 / 2.0 ** 42))
+    share = 2.0 ** 42 * np.exp(np.float64(x[0, 1].item()) - np.float64(TOP))
+    assert 1000.4 < share < 1000.5
+    x[:, vocab - (1 << 14):] = -math.inf
+    x[:, 0] = float(TOP)
+    u = torch.tensor([0.5, 0.9999, 0.99999]).cuda()
+    logits = x.cuda()
+    rules = dict(top_p=1.0 - 2.0 ** -24)
+    token, logprob = B.sample(logits, u, B.SamplingRules(**rules), want_logprob=True)
+    check_rows(logits, u, token, logprob, **rules)
+    assert token[0] == 0 and (token[1:] > 0).all()
