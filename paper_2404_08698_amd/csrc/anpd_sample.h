@@ -395,13 +395,15 @@ struct RowSampler {
     template <bool MASS>
     __device__ __forceinline__ whole_t amount(float v) const { return MASS ? scale.weight(v) : 1; }
 
-    // Logits that are certainly not in interval b are outside low .. high.
+    // Logits that are certainly not in interval b are outside low .. high.  (At temperatures near the largest number, intervals end beyond it, and the product with a
+    // logit just below 0 may be below the smallest one, which makes it 0.)
     struct Interval {
         float low, high;
         __device__ __forceinline__ Interval(const Scale &scale, int b)
         {
-            const float at = scale.first - (float)b, lo = at / scale.bins, hi = (at + 1.f) / scale.bins;
-            low = lo - fabsf(lo) * 0x1p-20f;
+            constexpr float most = 3.4028234e38f;
+            const float at = scale.first - (float)b, lo = fminf(fmaxf(at / scale.bins, -most), most), hi = fminf(fmaxf((at + 1.f) / scale.bins, -most), most);
+            low = lo - fabsf(lo) * 0x1p-20f - 0x1p-149f / scale.bins;
             high = hi + fabsf(hi) * 0x1p-20f;
             if (b == kSampleBins - 1 || !(fabsf(at) < 0x1p21f)) low = -INFINITY;
             if (!(fabsf(at) < 0x1p21f)) high = INFINITY;   // (where the numbers of intervals end)

@@ -86,3 +86,22 @@ def test_more_weight_than_equal_logits_have():
     token, logprob = B.sample(logits, u, B.SamplingRules(**rules), want_logprob=True)
     check_rows(logits, u, token, logprob, **rules)
     assert token[0] == 0 and (token[1:] > 0).all()
+
+
+@pytest.mark.parametrize("rules", [dict(), dict(top_k=3), dict(top_k=60), dict(top_p=0.5), dict(min_p=0.3), dict(top_p=0.6, min_p=0.2)], ids=str)
+@pytest.mark.parametrize("vocab", [100, 9000])
+def test_the_largest_temperatures(vocab, rules):
+    """Where 64 / temperature times a logit is below the smallest number, and where intervals end beyond the largest one."""
+    largest = torch.finfo(torch.float32).max
+    gen = torch.Generator().manual_seed(vocab)
+    noise = torch.randn(4, vocab, generator=gen)
+    rows = [torch.full((4, vocab), -1e-10), noise * 1e-12, noise * 1e-30, noise.sign() * largest, noise.clamp(-1, 1) * largest, torch.full((4, vocab), -largest), torch.full((4, vocab), largest)]
+    u = torch.tensor([0.0, 0.3, 0.62, 0.97]).cuda()
+    for x in rows:
+        for temperature in (largest, 1e38, 2e37):
+            token, logprob = torch.full((4,), -7, dtype=torch.int32, device="cuda"), torch.full((4,), 9.0, device="cuda")
+            B.sample(x.cuda(), u, B.SamplingRules(temperature=temperature, **rules), tokens=token, logprob=logprob)
+            check_rows(x, u, token, logprob, temperature=temperature, **rules)
+        endless = torch.full((4,), math.inf, device="cuda")
+        token, logprob = B.sample(x.cuda(), u, B.SamplingRules(temperature=endless, **rules), want_logprob=True)
+        check_rows(x, u, token, logprob, temperature=largest, **rules)
