@@ -46,7 +46,9 @@ __device__ __forceinline__ void split_terms16(float (&x)[8], u32x4 (&t)[TERMS])
             if (k + 1 < TERMS) { x[2 * i] -= (float)h[0]; x[2 * i + 1] -= (float)h[1]; }
         }
 }
-constexpr float kSmallestScale = 0x1p-100f;   // of values that a reference follows
+// The smallest scale of values that a reference follows.  An unscaled weight is below 2^15 divided by it, 2^107, and the sum of as many as a cache has positions, 2^20, below
+// 2^127; with 2^-100, 2^17 keys whose values were zeros had an infinite sum.  Smaller scales lose digits from 2^-102 on (fp32 rows) or 2^-113 (bf16).
+constexpr float kSmallestScale = 0x1p-93f;
 
 // Block = (32 virtual rows, kv head, split of the keys), four waves; wave w takes keys 32 w .. of every 128, as in the form for bf16 pages.
 // Tokens: 32 of 32 sequences of 300 to 700 positions, 140 MB in 35 us (4.0 TB/s): a block lives 14.5 us, of which start and end, that nothing overlaps but other
