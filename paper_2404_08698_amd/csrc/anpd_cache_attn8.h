@@ -152,12 +152,12 @@ __global__ __launch_bounds__(256, 2) void cache_attn8_kernel(const AttnArgs a)
         for (int w = 0; w < kStreamWaves; ++w) most = fmaxf(most, most_of[w][m]);
         int by = most > 0.f && most < INFINITY ? 15 - __builtin_amdgcn_frexp_expf(most) : 0;
         by = by < 100 ? by : 100;   // (what is smaller has scores of 0)
-        row_scale = most < INFINITY ? ldexpf(1.0f, -by) : __uint_as_float(0x7fc00000u);   // (a row with an infinity or a NaN: all its scores are NaN)
+        row_scale = ldexpf(1.0f, -by);
 #pragma unroll
         for (int y = 0; y < NKS / kStreamWaves; ++y) {
             u32x4 q[TERMS];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[y][e] = most < INFINITY ? ldexpf(x[y][e], by) : 0.f;
+            for (int e = 0; e < 8; ++e) x[y][e] = most < INFINITY ? ldexpf(x[y][e], by) : __uint_as_float(0x7fc00000u);   // (a row with an infinity or a NaN: NaN, where it sees a key)
             split_terms16<TERMS>(x[y], q);
 #pragma unroll
             for (int t = 0; t < TERMS; ++t) lds.q[y * kStreamWaves + wave][t][lane] = q[t];
