@@ -95,14 +95,11 @@ int32_t anpd_sample(const void *logits, int64_t ld, int32_t dtype, int32_t rows,
     int32_t rc = on.enter_of(who, logits);
     if (rc != ANPD_OK) return rc;
     hipStream_t st = (hipStream_t)stream;
-    if (need == 0) {
-        launch_rows<true>(a, (unsigned)rows, st);
-        HIP_TRY(hipGetLastError());
-        return ANPD_OK;
-    }
     a.slices = (Slice *)workspace;
-    for (int32_t row = 0; row < rows; row += kGroup) {
-        const unsigned n = (unsigned)(rows - row < kGroup ? rows - row : kGroup);
+    // (a launch has fewer than 2^32 threads)
+    const int64_t group = need > 0 ? kGroup : 1 << 21;
+    for (int64_t row = 0; row < rows; row += group) {
+        const unsigned n = (unsigned)(rows - row < group ? rows - row : group);
         SampleArgs g = a;
         g.logits = (const char *)logits + (size_t)row * ld * (a.f32 ? 4 : 2);
         g.uniform += row;
@@ -112,10 +109,13 @@ int32_t anpd_sample(const void *logits, int64_t ld, int32_t dtype, int32_t rows,
         if (g.top_ks) g.top_ks += row;
         if (g.top_ps) g.top_ps += row;
         if (g.min_ps) g.min_ps += row;
-        if (a.slice_shift == 12) launch_slices<256>(g, n, st);
-        else launch_slices<1024>(g, n, st);
-        HIP_TRY(hipGetLastError());
-        launch_rows<false>(g, n, st);
+        if (need == 0) launch_rows<true>(g, n, st);
+        else {
+            if (a.slice_shift == 12) launch_slices<256>(g, n, st);
+            else launch_slices<1024>(g, n, st);
+            HIP_TRY(hipGetLastError());
+            launch_rows<false>(g, n, st);
+        }
         HIP_TRY(hipGetLastError());
     }
     return ANPD_OK;

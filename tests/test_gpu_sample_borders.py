@@ -105,3 +105,13 @@ def test_the_largest_temperatures(vocab, rules):
         endless = torch.full((4,), math.inf, device="cuda")
         token, logprob = B.sample(x.cuda(), u, B.SamplingRules(temperature=endless, **rules), want_logprob=True)
         check_rows(x, u, token, logprob, temperature=largest, **rules)
+
+
+def test_more_rows_than_a_launch_takes():
+    rows = (1 << 22) + 3
+    x = torch.zeros(rows, 2, device="cuda")
+    x[:, 1] = math.log(3.0)
+    u = torch.rand(rows, generator=torch.Generator().manual_seed(0)).cuda()
+    token = B.sample(x, u)
+    near = (u - 0.25).abs() < 1e-6
+    assert torch.equal(token[~near], (u >= 0.25).int()[~near]) and ((token == 0) | (token == 1)).all()
