@@ -695,11 +695,19 @@ def _with_workspace(fn, bytes_of, seqs, ref, head, tail, workspace, device, stre
     _check(rc)
 
 
+def _workspace_bytes(fn, kvs, n_rows, pos0, rules) -> int:
+    kvs = (kvs,) if isinstance(kvs, KVCache) else kvs
+    return int(fn((C.c_void_p * len(kvs))(*[kv._h.value for kv in kvs]), len(kvs), _ints(n_rows), None if pos0 is None else _ints(pos0), None if rules is None else rules.ref))
+
+
 def attention_workspace_bytes(kvs, n_rows: Sequence[int], pos0: Optional[Sequence[int]] = None, rules: Optional[AttentionRules] = None) -> int:
     """anpd_attention_workspace_bytes (0: none is needed)."""
-    kvs = (kvs,) if isinstance(kvs, KVCache) else kvs
-    return int(lib().anpd_attention_workspace_bytes((C.c_void_p * len(kvs))(*[kv._h.value for kv in kvs]), len(kvs), _ints(n_rows),
-                                                    None if pos0 is None else _ints(pos0), None if rules is None else rules.ref))
+    return _workspace_bytes(lib().anpd_attention_workspace_bytes, kvs, n_rows, pos0, rules)
+
+
+def tree_attention_workspace_bytes(kvs, n_rows: Sequence[int], pos0: Optional[Sequence[int]] = None, rules: Optional[AttentionRules] = None) -> int:
+    """anpd_tree_attention_workspace_bytes (0: none is needed)."""
+    return _workspace_bytes(lib().anpd_tree_attention_workspace_bytes, kvs, n_rows, pos0, rules)
 
 
 def attention(kvs, layer: int, q, n_rows: Optional[Sequence[int]] = None, pos0: Optional[Sequence[int]] = None,
