@@ -1036,6 +1036,7 @@ def anpd_generate(model: Model, kv: KVCache, table: NgramTable, prompt: Sequence
     if sampling is not None and sampling.tensors:
         raise ValueError("sampling: the same rules for all rows")
     side = contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+    uniform = lambda n: torch.rand(n, generator=generator, dtype=torch.float32, device=kv.pool.device)  # noqa: E731
     table.reset()
     table.update(prompt)
     if sampling is None:
@@ -1044,7 +1045,7 @@ def anpd_generate(model: Model, kv: KVCache, table: NgramTable, prompt: Sequence
         with side:
             logits = torch.empty(max(1, model.max_window), model.vocab, dtype=torch.float32, device=kv.pool.device)
             prefill(model, kv, prompt, stream, out_logits=logits[0])
-            c = int(sample(logits[:1], torch.rand(1, generator=generator, device=kv.pool.device), sampling, stream=stream))
+            c = int(sample(logits[:1], uniform(1), sampling, stream=stream))
     out: List[int] = []
     steps = proposed = accepted = 0
     while len(out) < n_tokens:
@@ -1060,7 +1061,7 @@ def anpd_generate(model: Model, kv: KVCache, table: NgramTable, prompt: Sequence
             a, nxt = verify(model, kv, [c] + drafts, VERIFY, stream=stream)
         else:
             with side:
-                a, nxt, _ = verify_sample(model, kv, [c] + drafts, torch.rand(1 + len(drafts), generator=generator, device=kv.pool.device), sampling,
+                a, nxt, _ = verify_sample(model, kv, [c] + drafts, uniform(1 + len(drafts)), sampling,
                                           out_logits=logits, stream=stream)
         if a:
             table.update(drafts[:a])
