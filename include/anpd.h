@@ -470,7 +470,7 @@ int32_t anpd_kv_evict(const anpd_kv_t *src, anpd_kv_t *dst, const float *mass, i
 int32_t anpd_kv_store(anpd_kv_t *const *kvs, int32_t n_seq, const int32_t *n_rows, const int32_t *pos0, int32_t layer, const void *k, int64_t ldk,
                       const void *v, int64_t ldv, int32_t dtype, void *stream);
 /* ... and back: what the caches hold at those positions, rounded once to dtype; k and v share no element.  One cache may occur twice.  Asynchronous on stream; may be captured.
- * Both: ANPD_E_CAPACITY (positions), ANPD_E_INVAL (load: also a position without a page), ANPD_E_HIP. */
+ * Both: ANPD_E_CAPACITY (positions; 2^29 positions of a head and more in one call), ANPD_E_INVAL (load: also a position without a page), ANPD_E_HIP. */
 int32_t anpd_kv_load(const anpd_kv_t *const *kvs, int32_t n_seq, const int32_t *n_rows, const int32_t *pos0, int32_t layer, void *k, int64_t ldk,
                      void *v, int64_t ldv, int32_t dtype, void *stream);
 

@@ -48,7 +48,8 @@ int32_t gather(const char *who, const anpd_kv *const *kvs, int32_t n_seq, const 
         rows += n;
         if (n > 0) spans += (at + n - 1) / 16 - at / 16 + 1;
     }
-    if (rows >= (1 << 30) || spans * c.n_kv_heads >= (1ll << 31)) return fail(ANPD_E_CAPACITY, "%s: too many rows", who);
+    // (fewer than 2^32 threads: two waves for each span and head)
+    if (rows >= (1 << 30) || spans * c.n_kv_heads > (1ll << 25) - 2) return fail(ANPD_E_CAPACITY, "%s: too many rows", who);
     a.n_seq = n_seq;
     a.n_spans = (int32_t)spans;
     if (rows == 0) return ANPD_OK;
