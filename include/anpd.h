@@ -523,8 +523,10 @@ typedef struct {
  *   out_logprob (nullable, DEVICE, rows floats): the logarithm of the probability with which it is drawn (temperature 0: 0; no token: NaN).
  *   workspace: DEVICE, 256-byte aligned, >= anpd_sample_workspace_bytes() (0 for vocabularies of up to 8192, then it may be NULL), used during the
  *   call only: calls that may overlap need one each, replays of captured calls included.
- * Weights are formed in 64 bits and held as multiples of 2^-51 of the largest (2^-42 for vocabularies near 2^20): the same inputs give the same tokens.
- * Asynchronous on stream; may be captured.  Errors: ANPD_E_INVAL, ANPD_E_HIP. */
+ * Weights are formed in 64 bits and rounded to whole steps, whose sums are exact: the same inputs give the same tokens.  A step is 2^-(62 - b) of the largest weight, where 2^b is the first
+ * power of two that is not below vocab, but 2^-51 at the least: 2^-51 for up to 2048 tokens, 2^-47 for 32000, 2^-45 for 131072, 2^-42 for 2^20.  Weights of less than half a step
+ * are 0, and a row's sums are off by up to a step for each token, 2^(2 b - 62) of the largest weight: 2.3e-10 for 32000 tokens, 3.7e-9 for 131072.  Equal logits lose nothing.
+ * Asynchronous on stream; may be captured.  Errors: ANPD_E_INVAL, ANPD_E_CAPACITY (workspace), ANPD_E_HIP. */
 size_t anpd_sample_workspace_bytes(int32_t rows, int32_t vocab);
 int32_t anpd_sample(const void *logits, int64_t ld, int32_t dtype, int32_t rows, int32_t vocab, const anpd_sample_rules *rules, const float *uniform,
                     int32_t *out_token, float *out_logprob, void *workspace, size_t workspace_bytes, void *stream);

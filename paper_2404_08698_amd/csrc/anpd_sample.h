@@ -5,7 +5,8 @@
 //   kept = K, P and M together;  token = the lowest index i with sum_{j <= i, kept} w_j > u sum_kept w;  log p = a_token - log sum_kept w
 //
 // Sums.  Which token a random number falls on is decided by sums that are compared, so weights are formed in 64 bits and rounded once to whole multiples of
-// 2^-shift of the largest, whose sums are exact in any order: histograms may be filled by atomics.  Sums of different slices of a row are joined in
+// 2^-shift of the largest, whose sums are exact in any order: histograms may be filled by atomics.  shift is 51, or what keeps a row's sum below 2^62: 47 for 32000 tokens, 45
+// for 131072, 42 for 2^20; a sum is off by a step for each token at most (half of one in a slice's, half in the row's).  Sums of different slices of a row are joined in
 // 64-bit floating point, in the slices' order: the same inputs give the same token.
 //
 // Order.  The kept tokens are the first ones of an order, so they are told from the others by one logit and an index among its equals (the border).  It is

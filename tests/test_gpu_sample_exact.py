@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from paper_2404_08698_amd import binding as B
-from sample_check import check_rows
+from sample_check import check_rows, resolution
 
 pytestmark = pytest.mark.gpu
 
@@ -37,3 +37,15 @@ def test_equal_logits_are_exact(vocab):
         for rules in (dict(), dict(temperature=0.37), dict(top_k=4), dict(top_k=vocab // 2 + 1), dict(top_p=0.5), dict(top_p=0.25, temperature=3.0), dict(top_p=0.7), dict(min_p=1.0),
                       dict(top_k=vocab // 2 + 1, top_p=0.5), dict(temperature=0.0)):
             run(x.repeat(len(u), 1).cuda(), u, **rules)
+
+
+@pytest.mark.parametrize("vocab", [2000, 20000, 131072])
+def test_the_resolution_of_weights(vocab):
+    """One logit far above all others, which are equal: where their weights are below half a step, none of them is drawn; from half a step on they are.  A sum over the
+    row is off by half a step for each at most."""
+    step = 2 * resolution(vocab)
+    for part, drawn in ((0.4, False), (0.6, True), (2.0 ** 10 + 0.3, True)):
+        x = torch.full((2, vocab), math.log(part * step))
+        x[:, vocab - 1] = 0.0
+        token = run(x.cuda(), torch.tensor([0.0, 0.5]).cuda())
+        assert token.tolist() == [0 if drawn else vocab - 1, vocab - 1], part
