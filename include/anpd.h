@@ -481,7 +481,7 @@ int32_t anpd_kv_load(const anpd_kv_t *const *kvs, int32_t n_seq, const int32_t *
  *   does (-1).  At most ANPD_TREE_MAX_ROWS rows per sequence (ANPD_E_CAPACITY).
  *   Row r's keys and values lie in slot pos0 + r of the cache; its position is pos0 + the number of its ancestors.  The rules
  *   go by positions: a row at position p sees, of those keys, the ones at positions that anpd_attention would show it.  A chain (parent = row - 1)
- *   is anpd_attention.
+ *   is anpd_attention, but for a prefix that reaches into the new rows: no row of a tree sees one behind it.
  * Errors and asynchrony as anpd_attention; parent is read when the kernels run, so a captured call takes the tree that is there then. */
 #define ANPD_TREE_MAX_ROWS 64
 size_t anpd_tree_attention_workspace_bytes(const anpd_kv_t *const *kvs, int32_t n_seq, const int32_t *n_rows, const int32_t *pos0,

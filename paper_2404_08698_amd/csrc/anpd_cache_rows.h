@@ -3,9 +3,9 @@
 //   8 bits, per position and head, keys and values apart:  s = max |x| / 127 in fp32,  code = 127 x / max |x| to the nearest, ties to even;  value = code s
 //
 // A wave has 16 positions of a sequence (those of a page, where pages are 16 long), one key / value head, keys or values: no 32-bit word of a cache is written by two
-// waves, and its values, which lie key beside key, are turned around in the wave.  Bound by the bytes read and written: 3584 rows of 32 heads of 128 in bf16, into
-// 8 bits 26 us (3.4 TB/s of what is read and written; back to back 22), back 15 (5.9 TB/s, from L2 in part); a row for each of 32 caches 6.2 and 4.5, a
-// launch's length.
+// waves, and its values, which lie key beside key, are turned around in the wave.  Into 8 bits and plain order bound by the bytes read and written: 3584 rows of 32 heads of 128 in
+// bf16, into 8 bits 26 us (3.4 TB/s of what is read and written; back to back 22), back 15 (5.9 TB/s, from L2 in part); into fp32 in plain order 28 and back 27 (6.3 and 6.5);
+// a row for each of 32 caches into 8 bits 6.2 and 4.5, a launch's length.  Into matrix-core order (bf16, pages of 16) bound by its accesses, which are 2 bytes each: 55 and 57 us (2.1 TB/s).
 #pragma once
 #include "anpd_cache_softmax.h"
 
